@@ -72,6 +72,42 @@ int stage_kernel_rope_table(int s, int hd, float theta, float* table, void* hip_
 int stage_kernel_rope(int dtype, int b, int s, int n_heads, int hd, int inverse, void* x, int64_t ld, const float* table,
                       void* hip_stream);
 
+/* Rotary positions on several axes (for image and video tokens: time, height, width).  Pair p of a head belongs to one axis
+ * and turns by pos[axis][row] * frequency(p); the axes take the hd/2 pairs in order, section[a] of them each.  n_axes = 1 is
+ * ordinary rotary embedding with positions of the caller's own (several documents in a row, positions that start late). */
+typedef struct {
+  int32_t n_axes;            /* 1 .. 4 */
+  int32_t section[4];        /* pairs of each axis, >= 1; they add up to hd/2 (entries behind n_axes are not read) */
+  int32_t halves;            /* 0: pairs (2p, 2p+1), as in stage_kernel_rope; 1: pairs (p, p + hd/2) */
+  int32_t restart;           /* 0: frequency theta^(-2p/hd) by the pair's place in the head; 1: theta^(-q/n) for the q-th of its axis' n pairs */
+  float theta;               /* > 0 */
+  const int32_t* pos;        /* device, [n_axes] rows of pos_stride: the position of every row on each axis, any int32 */
+  int64_t pos_stride;        /* >= rows */
+} stage_rope_axes_t;
+
+/* y = the first n_heads heads of every row of x [rows, ldx] rotated (inverse != 0: by the negative angles, which is the transpose
+ * and the backward pass).  y may be x (with ldy = ldx); otherwise the two must not overlap.  hd 64 or 128; rows, n_heads >= 1, rows at
+ * most 2^23; x and y 16-byte aligned, ldx and ldy multiples of 16 bytes' worth of elements. */
+int stage_kernel_rope_axes(int dtype, int rows, int n_heads, int hd, const stage_rope_axes_t* axes, int inverse, const void* x,
+                           int64_t ldx, void* y, int64_t ldy, void* hip_stream);
+
+/* RMS norm of every query and key head, each over its own hd columns, and the rotation behind it, in one pass: of the first h + hkv
+ * heads of every row of x [rows, ldx] (q | k of a qkv buffer; what lies behind them is neither read nor written),
+ * y = rotate(x * rstd * gamma) with rstd = (mean of x^2 over the head + eps)^(-1/2) and gamma gamma_q [hd] for the first h heads,
+ * gamma_k [hd] for the others.  axes NULL: no rotation.  rstd: [rows, h + hkv] fp32, or NULL when there is no backward.
+ * y may be x (with ldy = ldx; the backward then needs a copy of x).  Sizes, alignment and strides as in stage_kernel_rope_axes; gammas
+ * 16-byte aligned. */
+int stage_kernel_qk_norm_rope_fwd(int dtype, int rows, int h, int hkv, int hd, float eps, const stage_rope_axes_t* axes, const void* x,
+                                  int64_t ldx, const void* gamma_q, const void* gamma_k, void* y, int64_t ldy, float* rstd,
+                                  void* hip_stream);
+/* Its gradients: dx (may be dy, with lddx = lddy) from dy, and dgamma_q, dgamma_k fp32 [hd] += , summed over rows and heads in a fixed
+ * order.  x, rstd and axes as in the forward; partial: scratch of stage_kernel_qk_norm_rope_partial_bytes(hd) bytes, which calls on
+ * different streams must not share. */
+int stage_kernel_qk_norm_rope_bwd(int dtype, int rows, int h, int hkv, int hd, const stage_rope_axes_t* axes, const void* x, int64_t ldx,
+                                  const float* rstd, const void* gamma_q, const void* gamma_k, const void* dy, int64_t lddy, void* dx,
+                                  int64_t lddx, float* dgamma_q, float* dgamma_k, float* partial, void* hip_stream);
+size_t stage_kernel_qk_norm_rope_partial_bytes(int hd);
+
 /* qkv: [b*s, (h + 2*hkv)*hd] rows of q | k | v;  o: [b*s, h*hd];  lse: [b, h, s] fp32. */
 int stage_kernel_attention_fwd(int dtype, int b, int s, int h, int hkv, int hd, int causal, const void* qkv, void* o,
                                float* lse, int kernel_set, void* hip_stream);
@@ -87,6 +123,40 @@ size_t stage_kernel_attention_bwd_scratch_bytes(int b, int s, int h, int hkv, in
 int stage_kernel_attention_bwd_ws(int dtype, int b, int s, int h, int hkv, int hd, int causal, const void* qkv,
                                   const void* o, const float* lse, const void* dout, void* dqkv, float* delta,
                                   void* scratch, size_t scratch_bytes, int kernel_set, void* hip_stream);
+
+/* Attention whose scores are shaped, over sequences of any lengths packed one behind the other into `rows` rows:
+ *   s = scale * q.k,  with softcap c > 0 c * tanh(s / c),  with slopes minus slope[head] * |query row - key row|;
+ *   a query sees the keys of its own sequence: all of them, or (causal) those up to itself and the sequence's prefix.
+ * Sequence i is rows seq_start[i] .. seq_start[i+1] - 1; empty ones are allowed.  Rows before the first or behind the last are not read,
+ * and what belongs to them in the outputs is left as it was. */
+typedef struct {
+  int32_t dtype;
+  int32_t rows;              /* >= 1, at most 2^23 */
+  int32_t n_seq;             /* >= 1, at most 2^20 */
+  int32_t h, hkv, hd;        /* h a multiple of hkv; hd 64 or 128 */
+  int32_t causal;            /* 0 or 1 */
+  float scale;               /* > 0, or 0 for hd^(-1/2) */
+  float softcap;             /* > 0, or 0 for none */
+  const float* slope;        /* device, [h], finite; or NULL for no distance bias (the slopes are constants: they get no gradient) */
+  const int32_t* seq_start;  /* device, [n_seq + 1], ascending, within [0, rows] (what leaves that order gives undefined results, but touches
+                                nothing outside the rows); or NULL for n_seq sequences of rows / n_seq rows each, without remainder */
+  const int32_t* prefix;     /* device, [n_seq]: the leading keys of a sequence that all of its queries see (0: none; more than the sequence
+                                has: all); causal only; or NULL */
+} stage_score_attention_t;
+
+/* q, o: [rows, h*hd]; k, v: [rows, hkv*hd], each with a row stride of its own (elements), so that they may be columns of one buffer.
+ * lse: [h, rows] fp32, or NULL when there is no backward.  The tuned bf16 kernels want 16-byte aligned pointers and strides; what they do
+ * not take, the plain kernels do. */
+int stage_kernel_score_attention_fwd(const stage_score_attention_t* p, const void* q, int64_t ldq, const void* k, int64_t ldk,
+                                     const void* v, int64_t ldv, void* o, int64_t ldo, float* lse, int kernel_set, void* hip_stream);
+/* dq, dk, dv overlap no input and not each other.  scratch: stage_kernel_score_attention_bwd_scratch_bytes(p) bytes, 16-byte aligned, not
+ * shared by calls on different streams.  Results are the same bits from call to call. */
+int stage_kernel_score_attention_bwd(const stage_score_attention_t* p, const void* q, int64_t ldq, const void* k, int64_t ldk,
+                                     const void* v, int64_t ldv, const void* o, int64_t ldo, const float* lse, const void* dout,
+                                     int64_t lddo, void* dq, int64_t lddq, void* dk, int64_t lddk, void* dv, int64_t lddv, void* scratch,
+                                     size_t scratch_bytes, int kernel_set, void* hip_stream);
+/* 0 for a p that the two entries refuse. */
+size_t stage_kernel_score_attention_bwd_scratch_bytes(const stage_score_attention_t* p);
 
 /* stats: [rows, 2] fp32 (mean, rstd). beta ignored for RMSNorm. */
 int stage_kernel_norm_fwd(int dtype, int norm, int rows, int d, float eps, const void* x, const void* gamma,

@@ -59,6 +59,46 @@ struct AttnArgs {
 int attn_bwd_splits(int b, int s, int h, int hkv);
 size_t attn_bwd_part_bytes(int b, int s, int h, int hkv, int hd);
 
+// Attention of shaped scores over packed sequences (stage_kernel_score_attention_*): strides in elements.
+struct ScoreArgs {
+  int rows, n_seq, h, hkv, hd, causal;
+  float scale, cap;              // scores scale * q.k, then (cap > 0) cap * tanh(score / cap)
+  const float* slope;            // [h] or null: slope[j] * |query - key| is subtracted
+  const int* seq_start;          // [n_seq + 1] or null: n_seq sequences of rows / n_seq rows
+  const int* prefix;             // [n_seq] or null: keys that every query of the sequence sees (causal only)
+  const void* q; int64_t ldq;    // [rows, h * hd]
+  const void* k; int64_t ldk;    // [rows, hkv * hd]
+  const void* v; int64_t ldv;
+  void* o; int64_t ldo;          // [rows, h * hd]
+  float* lse;                    // [h, rows], forward: or null
+  // backward only
+  const void* dout; int64_t lddo;
+  void* dq; int64_t lddq;
+  void* dk; int64_t lddk;
+  void* dv; int64_t lddv;
+  float* delta;                  // [h, rows] scratch: rowsum(dout * o)
+};
+
+// Rotation by positions on several axes (stage_kernel_rope_axes), alone or behind the norm of every head
+constexpr int ROPE_MAX_PAIRS = 64;
+struct RotateArgs {
+  double turn[ROPE_MAX_PAIRS];   // frequency of every pair, in turns per position
+  int axis[ROPE_MAX_PAIRS];      // its axis
+  int halves;                    // pairs (p, p + hd / 2) instead of (2p, 2p + 1)
+  const int* pos; int64_t pos_stride;      // [axes][pos_stride], or null: no rotation
+};
+struct HeadNormArgs {
+  int rows, h, hkv, hd, inverse;
+  float eps;
+  const void* x; int64_t ldx;    // [rows, (h + hkv) * hd]
+  void* y; int64_t ldy;          // forward: out; backward: dx
+  const void* gq; const void* gk;
+  float* rstd;                   // [rows, h + hkv] (forward: or null)
+  const void* dy; int64_t lddy;  // backward only
+  float* dgq; float* dgk;        // fp32, added to
+  float* partial;                // [HEAD_NORM_PARTS][2][hd]
+};
+
 struct NormArgs {
   int kind;                      // 0 LayerNorm, 1 RMSNorm
   int rows, d;
@@ -131,6 +171,15 @@ hipError_t copy_bytes(void* dst, const void* src, size_t bytes, hipStream_t s);
 hipError_t rope_table(float* table, int s, int hd, double theta, hipStream_t st);
 hipError_t rope_apply(DType dt, void* x, int64_t ld, int64_t rows, int s, int nh, int hd, const float* table, int inverse,
                       hipStream_t st);
+
+// per-head norm and rotation of q and k
+size_t head_norm_partial_bytes(int hd);
+hipError_t rope_axes(DType dt, const HeadNormArgs& n, const RotateArgs& r, hipStream_t s);
+hipError_t qk_norm_rope_fwd(DType dt, const HeadNormArgs& n, const RotateArgs& r, hipStream_t s);
+hipError_t qk_norm_rope_bwd(DType dt, const HeadNormArgs& n, const RotateArgs& r, hipStream_t s);
+// attention of shaped scores: plain kernels
+hipError_t score_fwd_ref(DType dt, const ScoreArgs& a, hipStream_t s);
+hipError_t score_bwd_ref(DType dt, const ScoreArgs& a, hipStream_t s);
 
 // tuned gfx950 kernels (bf16 MFMA)
 bool gemm_mfma_supported(const GemmArgs& g);

@@ -1116,6 +1116,113 @@ int stage_kernel_attention_bwd_ws(int dtype, int b, int s, int h, int hkv, int h
   return hip_rc(attn_bwd_ref((DType)dtype, a, (hipStream_t)hip_stream));
 }
 
+// the host's half of the rotation: every pair's axis and frequency, in turns per position
+static bool rotate_args(const stage_rope_axes_t* x, int rows, int hd, RotateArgs* r) {
+  *r = RotateArgs{};
+  if (!x) return true;
+  if (x->n_axes < 1 || x->n_axes > 4 || (x->halves != 0 && x->halves != 1) || (x->restart != 0 && x->restart != 1) || !(x->theta > 0.f) ||
+      !std::isfinite(x->theta) || !x->pos || x->pos_stride < rows)
+    return false;
+  int p = 0;
+  for (int a = 0; a < x->n_axes; ++a) {
+    const int n = x->section[a];
+    if (n < 1 || n > hd / 2 - p) return false;
+    for (int q = 0; q < n; ++q, ++p) {
+      r->axis[p] = a;
+      r->turn[p] = pow((double)x->theta, x->restart ? -(double)q / n : -2.0 * p / hd) / (2.0 * M_PI);
+    }
+  }
+  r->halves = x->halves; r->pos = x->pos; r->pos_stride = x->pos_stride;
+  return p == hd / 2;
+}
+static bool head_rows(int dtype, int rows, int heads, int hd, const void* x, int64_t ld) {
+  return ld >= (int64_t)heads * hd && ld % (dtype == STAGE_DTYPE_FP32 ? 4 : 8) == 0 && x && ((uintptr_t)x & 15) == 0;
+}
+static bool head_shape(int dtype, int rows, int64_t heads, int hd) {
+  return dtype_ok(dtype) && rows >= 1 && rows <= 1 << 23 && heads >= 1 && heads <= 65535 && (hd == 64 || hd == 128);
+}
+
+int stage_kernel_rope_axes(int dtype, int rows, int n_heads, int hd, const stage_rope_axes_t* axes, int inverse, const void* x,
+                           int64_t ldx, void* y, int64_t ldy, void* hip_stream) {
+  RotateArgs r;
+  if (!head_shape(dtype, rows, n_heads, hd) || !axes || !rotate_args(axes, rows, hd, &r) || !head_rows(dtype, rows, n_heads, hd, x, ldx) ||
+      !head_rows(dtype, rows, n_heads, hd, y, ldy) || (x == y && ldx != ldy))
+    return STAGE_E_INVAL;
+  HeadNormArgs n{}; n.rows = rows; n.h = n_heads; n.hd = hd; n.inverse = inverse != 0; n.x = x; n.ldx = ldx; n.y = y; n.ldy = ldy;
+  return hip_rc(rope_axes((DType)dtype, n, r, (hipStream_t)hip_stream));
+}
+
+int stage_kernel_qk_norm_rope_fwd(int dtype, int rows, int h, int hkv, int hd, float eps, const stage_rope_axes_t* axes, const void* x,
+                                  int64_t ldx, const void* gamma_q, const void* gamma_k, void* y, int64_t ldy, float* rstd,
+                                  void* hip_stream) {
+  RotateArgs r;
+  if (h < 1 || hkv < 1 || !head_shape(dtype, rows, (int64_t)h + hkv, hd) || !(eps >= 0.f) || !std::isfinite(eps) || !rotate_args(axes, rows, hd, &r) ||
+      !head_rows(dtype, rows, h + hkv, hd, x, ldx) || !head_rows(dtype, rows, h + hkv, hd, y, ldy) || (x == y && ldx != ldy) || !gamma_q ||
+      !gamma_k || ((uintptr_t)gamma_q & 15) || ((uintptr_t)gamma_k & 15))
+    return STAGE_E_INVAL;
+  HeadNormArgs n{}; n.rows = rows; n.h = h; n.hkv = hkv; n.hd = hd; n.eps = eps; n.x = x; n.ldx = ldx; n.y = y; n.ldy = ldy;
+  n.gq = gamma_q; n.gk = gamma_k; n.rstd = rstd;
+  return hip_rc(qk_norm_rope_fwd((DType)dtype, n, r, (hipStream_t)hip_stream));
+}
+
+int stage_kernel_qk_norm_rope_bwd(int dtype, int rows, int h, int hkv, int hd, const stage_rope_axes_t* axes, const void* x, int64_t ldx,
+                                  const float* rstd, const void* gamma_q, const void* gamma_k, const void* dy, int64_t lddy, void* dx,
+                                  int64_t lddx, float* dgamma_q, float* dgamma_k, float* partial, void* hip_stream) {
+  RotateArgs r;
+  if (h < 1 || hkv < 1 || !head_shape(dtype, rows, (int64_t)h + hkv, hd) || !rotate_args(axes, rows, hd, &r) ||
+      !head_rows(dtype, rows, h + hkv, hd, x, ldx) || !head_rows(dtype, rows, h + hkv, hd, dy, lddy) || !head_rows(dtype, rows, h + hkv, hd, dx, lddx) ||
+      (dx == dy && lddx != lddy) || dx == x || !rstd || !gamma_q || !gamma_k || ((uintptr_t)gamma_q & 15) || ((uintptr_t)gamma_k & 15) || !dgamma_q ||
+      !dgamma_k || dgamma_q == dgamma_k || !partial)
+    return STAGE_E_INVAL;
+  HeadNormArgs n{}; n.rows = rows; n.h = h; n.hkv = hkv; n.hd = hd; n.x = x; n.ldx = ldx; n.y = dx; n.ldy = lddx; n.gq = gamma_q; n.gk = gamma_k;
+  n.rstd = (float*)rstd; n.dy = dy; n.lddy = lddy; n.dgq = dgamma_q; n.dgk = dgamma_k; n.partial = partial;
+  return hip_rc(qk_norm_rope_bwd((DType)dtype, n, r, (hipStream_t)hip_stream));
+}
+
+size_t stage_kernel_qk_norm_rope_partial_bytes(int hd) { return hd == 64 || hd == 128 ? head_norm_partial_bytes(hd) : 0; }
+
+static bool score_args(const stage_score_attention_t* p, ScoreArgs* a) {
+  if (!p || !dtype_ok(p->dtype) || p->rows < 1 || p->rows > 1 << 23 || p->n_seq < 1 || p->n_seq > 1 << 20 || p->h < 1 || p->h > 65535 || p->hkv < 1 ||
+      p->h % p->hkv || (p->hd != 64 && p->hd != 128) || (p->causal != 0 && p->causal != 1) || !(p->scale >= 0.f) || !std::isfinite(p->scale) ||
+      !(p->softcap >= 0.f) || !std::isfinite(p->softcap) || (!p->seq_start && p->rows % p->n_seq) || (p->prefix && !p->causal))
+    return false;
+  *a = ScoreArgs{};
+  a->rows = p->rows; a->n_seq = p->n_seq; a->h = p->h; a->hkv = p->hkv; a->hd = p->hd; a->causal = p->causal;
+  a->scale = p->scale > 0.f ? p->scale : 1.f / sqrtf((float)p->hd);
+  a->cap = p->softcap; a->slope = p->slope; a->seq_start = p->seq_start; a->prefix = p->prefix;
+  return true;
+}
+
+int stage_kernel_score_attention_fwd(const stage_score_attention_t* p, const void* q, int64_t ldq, const void* k, int64_t ldk,
+                                     const void* v, int64_t ldv, void* o, int64_t ldo, float* lse, int kernel_set, void* hip_stream) {
+  ScoreArgs a;
+  if (!score_args(p, &a) || !q || !k || !v || !o) return STAGE_E_INVAL;
+  const int64_t d = (int64_t)a.h * a.hd, dkv = (int64_t)a.hkv * a.hd;
+  if (ldq < d || ldk < dkv || ldv < dkv || ldo < d) return STAGE_E_INVAL;
+  a.q = q; a.ldq = ldq; a.k = k; a.ldk = ldk; a.v = v; a.ldv = ldv; a.o = o; a.ldo = ldo; a.lse = lse;
+  return hip_rc(score_fwd_ref((DType)p->dtype, a, (hipStream_t)hip_stream));
+}
+
+size_t stage_kernel_score_attention_bwd_scratch_bytes(const stage_score_attention_t* p) {
+  ScoreArgs a;
+  return score_args(p, &a) ? ((size_t)a.h * a.rows * sizeof(float) + 15) / 16 * 16 : 0;
+}
+
+int stage_kernel_score_attention_bwd(const stage_score_attention_t* p, const void* q, int64_t ldq, const void* k, int64_t ldk,
+                                     const void* v, int64_t ldv, const void* o, int64_t ldo, const float* lse, const void* dout,
+                                     int64_t lddo, void* dq, int64_t lddq, void* dk, int64_t lddk, void* dv, int64_t lddv, void* scratch,
+                                     size_t scratch_bytes, int kernel_set, void* hip_stream) {
+  ScoreArgs a;
+  if (!score_args(p, &a) || !q || !k || !v || !o || !lse || !dout || !dq || !dk || !dv || !scratch || ((uintptr_t)scratch & 15) ||
+      scratch_bytes < stage_kernel_score_attention_bwd_scratch_bytes(p))
+    return STAGE_E_INVAL;
+  const int64_t d = (int64_t)a.h * a.hd, dkv = (int64_t)a.hkv * a.hd;
+  if (ldq < d || ldk < dkv || ldv < dkv || ldo < d || lddo < d || lddq < d || lddk < dkv || lddv < dkv) return STAGE_E_INVAL;
+  a.q = q; a.ldq = ldq; a.k = k; a.ldk = ldk; a.v = v; a.ldv = ldv; a.o = (void*)o; a.ldo = ldo; a.lse = (float*)lse;
+  a.dout = dout; a.lddo = lddo; a.dq = dq; a.lddq = lddq; a.dk = dk; a.lddk = lddk; a.dv = dv; a.lddv = lddv; a.delta = (float*)scratch;
+  return hip_rc(score_bwd_ref((DType)p->dtype, a, (hipStream_t)hip_stream));
+}
+
 int stage_kernel_norm_fwd(int dtype, int norm, int rows, int d, float eps, const void* x, const void* gamma,
                           const void* beta, void* out, float* stats, void* hip_stream) {
   if (!dtype_ok(dtype) || (norm != 0 && norm != 1) || rows <= 0 || d <= 0 || !x || !gamma || (norm == 0 && !beta) || !out || !stats)

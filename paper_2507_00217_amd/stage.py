@@ -44,6 +44,18 @@ class StageOp(C.Structure):
     _fields_ = [("kind", C.c_int32), ("mb", C.c_int32)]
 
 
+class RopeAxes(C.Structure):
+    """stage_rope_axes_t of include/stage_kernels.h; `pos` is the address of a device tensor that the caller keeps."""
+    _fields_ = [("n_axes", C.c_int32), ("section", C.c_int32 * 4), ("halves", C.c_int32), ("restart", C.c_int32), ("theta", C.c_float),
+                ("pos", C.c_void_p), ("pos_stride", C.c_int64)]
+
+
+class ScoreAttention(C.Structure):
+    """stage_score_attention_t of include/stage_kernels.h; the pointers are addresses of device tensors that the caller keeps."""
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "rows", "n_seq", "h", "hkv", "hd", "causal")] + [
+        ("scale", C.c_float), ("softcap", C.c_float), ("slope", C.c_void_p), ("seq_start", C.c_void_p), ("prefix", C.c_void_p)]
+
+
 class StageSizes(C.Structure):
     _fields_ = [(n, C.c_size_t) for n in ("weights", "grads", "stash", "workspace")]
 
@@ -68,6 +80,7 @@ def lib() -> C.CDLL:
         L = C.CDLL(LIB_PATH)
         vp, ip = C.c_void_p, C.POINTER(C.c_int)
         cfgp, opp, sopp = C.POINTER(StageConfig), C.POINTER(StageOp), C.POINTER(StageSubOp)
+        axp, scp, mat = C.POINTER(RopeAxes), C.POINTER(ScoreAttention), [vp, C.c_int64]      # a matrix: address and row stride
         sig = {
             "stage_query_sizes": (C.c_int, [cfgp, C.POINTER(StageSizes)]),
             "stage_validate_schedule": (C.c_int, [cfgp, opp, C.c_int, ip, ip]),
@@ -95,6 +108,13 @@ def lib() -> C.CDLL:
             "stage_profile_read": (C.c_int, [vp, C.c_int, C.POINTER(C.c_double), C.POINTER(C.c_int64), C.POINTER(C.c_double)]),
             "stage_destroy": (None, [vp]),
             "stage_strerror": (C.c_char_p, [C.c_int]),
+            "stage_kernel_rope_axes": (C.c_int, [C.c_int] * 4 + [axp, C.c_int] + mat * 2 + [vp]),
+            "stage_kernel_qk_norm_rope_fwd": (C.c_int, [C.c_int] * 5 + [C.c_float, axp] + mat + [vp, vp] + mat + [vp, vp]),
+            "stage_kernel_qk_norm_rope_bwd": (C.c_int, [C.c_int] * 5 + [axp] + mat + [vp, vp, vp] + mat * 2 + [vp] * 4),
+            "stage_kernel_qk_norm_rope_partial_bytes": (C.c_size_t, [C.c_int]),
+            "stage_kernel_score_attention_fwd": (C.c_int, [scp] + mat * 4 + [vp, C.c_int, vp]),
+            "stage_kernel_score_attention_bwd": (C.c_int, [scp] + mat * 4 + [vp] + mat * 4 + [vp, C.c_size_t, C.c_int, vp]),
+            "stage_kernel_score_attention_bwd_scratch_bytes": (C.c_size_t, [scp]),
             "stage_probe_mfma_ceiling": (C.c_int, [C.c_int, C.c_int, vp, C.c_size_t, C.POINTER(C.c_double), C.POINTER(C.c_double), vp]),
         }
         for name, (res, args) in sig.items():
