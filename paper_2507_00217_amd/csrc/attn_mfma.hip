@@ -46,16 +46,6 @@ namespace {
 constexpr int FWD_WIDE = 512, FWD_NARROW = 256;
 constexpr int fwd_bq(int nthr, int ks = 1) { return (nthr / 64) * 32 / ks; }
 
-// Which query tile (forward, dQ: the later, the more keys it sees) the workgroup of dispatch rank `rank` takes.
-// Plain order is heaviest first.  `fold`: the heavier half first, heaviest first, then the lighter half, lightest
-// first -- for grids that are resident all at once with two workgroups per CU, so that a CU's second workgroup is as
-// light as its first is heavy (ranks r and r + nh add up to the same work) instead of the chip waiting for the CUs that
-// drew two heavy ones.
-__device__ __forceinline__ int tile_of_rank(int rank, int n, int fold) {
-  const int nh = (n + 1) >> 1;
-  return (!fold || rank < nh) ? n - 1 - rank : rank - nh;
-}
-
 // One key tile of the forward for one wavefront (32 queries x 64 keys).  LDS fragment reads run ahead of the MFMAs
 // that consume them (K fragments three k-steps ahead; the first V^T fragments are fetched before the softmax
 // arithmetic and land while it runs), so a wavefront does not sit out one LDS round trip per MFMA.
@@ -507,51 +497,6 @@ __global__ __launch_bounds__(FWD_THREADS, 2) void attn_dq_kernel(AttnArgs a, int
 // (4 wavefronts, two workgroups per CU: twice as many workgroups for the same number of resident wavefronts).  QS = 2: two pairs
 // of wavefronts per key block, one on the even and one on the odd 32-query blocks, their sums added through LDS at the end.
 constexpr int DKV_TQ = 128, DKV_TQ_SMALL = 64;
-// early key tiles see the most queries: plain order is kt = rank; folded (see tile_of_rank) the heavy half first, then
-// the light half, lightest first
-__device__ __forceinline__ int key_tile_of_rank(int rank, int n, int fold) { return n - 1 - tile_of_rank(rank, n, fold); }
-
-// acc = (ADD: acc +) sum over head_dim of rows(tile `TILE`, rows rb..rb+31) x bfr (the wavefront's K or V fragments); fragment
-// reads run three k-steps ahead
-template <int HD, int TILE, bool ADD = false>
-__device__ __forceinline__ void dkv_rows_product(lds_char* lds, const FragOff<HD>& fo, int rb, const bf16x8 (&bfr)[HD / 16], f32x16& acc) {
-  using G = Geo<HD>;
-  constexpr int AHEAD = 3;
-  bf16x8 f[AHEAD + 1];
-#pragma unroll
-  for (int kk = 0; kk < AHEAD; ++kk) f[kk] = frag_rows<HD>(lds, fo, TILE, rb, kk);
-#pragma unroll
-  for (int kk = 0; kk < G::NKK; ++kk) {
-    if (kk + AHEAD < G::NKK) f[(kk + AHEAD) % (AHEAD + 1)] = frag_rows<HD>(lds, fo, TILE, rb, kk + AHEAD);
-    if (kk == 0 && !ADD) acc = mfma0(f[0], bfr[0]);
-    else acc = MFMA(f[kk % (AHEAD + 1)], bfr[kk], acc);
-    SCHED_FENCE;
-  }
-}
-// out[hb]^T += (tile `TILE`, rows rb..rb+31)^T . w, w = the 32 x 32 block of P or dS held as two bf16 fragments;
-// the first transposed fragments must already be in tf[] (read before the vector arithmetic that made w)
-template <int HD, int TILE>
-__device__ __forceinline__ void dkv_tr_read(lds_char* lds, const FragOff<HD>& fo, int rb, bf16x8 (&tf)[4]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) tf[i] = frag_cols_tr<HD>(lds, fo, TILE, rb + (i / Geo<HD>::NHB) * 16, i % Geo<HD>::NHB);
-}
-template <int HD, int TILE>
-__device__ __forceinline__ void dkv_tr_product(lds_char* lds, const FragOff<HD>& fo, int rb, bf16x8 (&tf)[4], const bf16x8 (&w)[2],
-                                               f32x16 (&out)[HD / 32]) {
-  using G = Geo<HD>;
-  constexpr int N = G::NHB * 2, VA = 4;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const bf16x8 v = tf[i % VA];
-    if (i + VA < N) {
-      const int n = i + VA;
-      tf[i % VA] = frag_cols_tr<HD>(lds, fo, TILE, rb + (n / G::NHB) * 16, n % G::NHB);
-    }
-    out[i % G::NHB] = MFMA(v, w[i / G::NHB], out[i % G::NHB]);
-    SCHED_FENCE;
-  }
-}
-
 // OWN_DELTA: delta is formed here, from dO and O (which the dQ pass, running at the same time, cannot provide)
 template <int HD, int TQ, int QS, bool OWN_DELTA>
 __device__ __forceinline__ void dkv_workgroup(const AttnArgs& a, int nsplit, int fold, lds_char* lds, int bx, int by) {

@@ -185,5 +185,60 @@ __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_ex
 
 #define SCHED_FENCE __builtin_amdgcn_sched_barrier(0)
 
+// Which query tile (forward, dQ: the later, the more keys it sees) the workgroup of dispatch rank `rank` takes.
+// Plain order is heaviest first.  `fold`: the heavier half first, heaviest first, then the lighter half, lightest
+// first -- for grids that are resident all at once with two workgroups per CU, so that a CU's second workgroup is as
+// light as its first is heavy (ranks r and r + nh add up to the same work) instead of the chip waiting for the CUs that
+// drew two heavy ones.
+__device__ __forceinline__ int tile_of_rank(int rank, int n, int fold) {
+  const int nh = (n + 1) >> 1;
+  return (!fold || rank < nh) ? n - 1 - rank : rank - nh;
+}
+
+// early key tiles see the most queries: plain order is kt = rank; folded (see tile_of_rank) the heavy half first, then
+// the light half, lightest first
+__device__ __forceinline__ int key_tile_of_rank(int rank, int n, int fold) { return n - 1 - tile_of_rank(rank, n, fold); }
+
+// acc = (ADD: acc +) sum over head_dim of rows(tile `TILE`, rows rb..rb+31) x bfr (the wavefront's K or V fragments); fragment
+// reads run three k-steps ahead
+template <int HD, int TILE, bool ADD = false>
+__device__ __forceinline__ void dkv_rows_product(lds_char* lds, const FragOff<HD>& fo, int rb, const bf16x8 (&bfr)[HD / 16], f32x16& acc) {
+  using G = Geo<HD>;
+  constexpr int AHEAD = 3;
+  bf16x8 f[AHEAD + 1];
+#pragma unroll
+  for (int kk = 0; kk < AHEAD; ++kk) f[kk] = frag_rows<HD>(lds, fo, TILE, rb, kk);
+#pragma unroll
+  for (int kk = 0; kk < G::NKK; ++kk) {
+    if (kk + AHEAD < G::NKK) f[(kk + AHEAD) % (AHEAD + 1)] = frag_rows<HD>(lds, fo, TILE, rb, kk + AHEAD);
+    if (kk == 0 && !ADD) acc = mfma0(f[0], bfr[0]);
+    else acc = MFMA(f[kk % (AHEAD + 1)], bfr[kk], acc);
+    SCHED_FENCE;
+  }
+}
+// out[hb]^T += (tile `TILE`, rows rb..rb+31)^T . w, w = the 32 x 32 block of P or dS held as two bf16 fragments;
+// the first transposed fragments must already be in tf[] (read before the vector arithmetic that made w)
+template <int HD, int TILE>
+__device__ __forceinline__ void dkv_tr_read(lds_char* lds, const FragOff<HD>& fo, int rb, bf16x8 (&tf)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) tf[i] = frag_cols_tr<HD>(lds, fo, TILE, rb + (i / Geo<HD>::NHB) * 16, i % Geo<HD>::NHB);
+}
+template <int HD, int TILE>
+__device__ __forceinline__ void dkv_tr_product(lds_char* lds, const FragOff<HD>& fo, int rb, bf16x8 (&tf)[4], const bf16x8 (&w)[2],
+                                               f32x16 (&out)[HD / 32]) {
+  using G = Geo<HD>;
+  constexpr int N = G::NHB * 2, VA = 4;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const bf16x8 v = tf[i % VA];
+    if (i + VA < N) {
+      const int n = i + VA;
+      tf[i % VA] = frag_cols_tr<HD>(lds, fo, TILE, rb + (n / G::NHB) * 16, n % G::NHB);
+    }
+    out[i % G::NHB] = MFMA(v, w[i / G::NHB], out[i % G::NHB]);
+    SCHED_FENCE;
+  }
+}
+
 }  // namespace
 }  // namespace stg

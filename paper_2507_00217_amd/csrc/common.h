@@ -180,6 +180,11 @@ hipError_t qk_norm_rope_bwd(DType dt, const HeadNormArgs& n, const RotateArgs& r
 // attention of shaped scores: plain kernels
 hipError_t score_fwd_ref(DType dt, const ScoreArgs& a, hipStream_t s);
 hipError_t score_bwd_ref(DType dt, const ScoreArgs& a, hipStream_t s);
+// and on the matrix cores, bf16; width as in AttnArgs
+bool score_mfma_supported(const ScoreArgs& a);
+size_t score_part_bytes(const ScoreArgs& a);
+hipError_t score_fwd_mfma(const ScoreArgs& a, int width, hipStream_t s);
+hipError_t score_bwd_mfma(const ScoreArgs& a, float* part, int width, hipStream_t s);
 
 // tuned gfx950 kernels (bf16 MFMA)
 bool gemm_mfma_supported(const GemmArgs& g);

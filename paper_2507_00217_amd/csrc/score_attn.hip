@@ -1,0 +1,1025 @@
+// Attention of shaped scores over packed sequences for gfx950 in bf16 with fp32 softmax: the tiles, fragments and the split of the
+// backward into dQ and dK/dV of attn_mfma.hip, with
+//   s_ij = scale q_i.k_j,  capped c tanh(s / c),  minus slope_h |i - j|,
+// a causal mask that a sequence's prefix opens, operands in buffers of their own, and sequences of any lengths one behind the other.
+//
+// Packing: tiles are cut per sequence, so no tile holds rows of two (their descriptors end with the sequence, rows past it read as
+// zeros) and a mask is the bound of one interval.  A packed sequence i whose first row is b takes the slots b / BQ + i .. of the grid,
+// BQ rows each: that is never less than it needs, so rows / BQ + n_seq slots are enough for any lengths, a workgroup finds its
+// sequence by a search over the offsets (64 at a time), and no list of tiles has to be made beforehand.
+//
+// Exponents are in units of log 2 throughout.  The distance bias of a 32 x 32 block is a scalar per lane (its query or key against the
+// block's first row) plus a multiple of the row inside the block, which is the same for all lanes of a half: 16 scalar registers.
+#include "attn_tile.h"
+#include "score.h"
+
+#include <type_traits>
+
+namespace stg {
+namespace {
+
+// What a launch hands over beside ScoreArgs: constants of the score in units of log 2, and the shape of the grid.
+struct ScoreCall {
+  ScoreArgs a;
+  float sl2;                     // scale * log2 e
+  float raw;                     // 1 / scale: a bias in units of the plain product
+  // cap: of the product x itself, s = c2 tanh(x scale / cap), c2 = cap log2 e
+  float c2, ic2, kx, small;      // kx = 2 log2 e scale / cap; |x| <= small: tanh by its polynomial
+  float poly[5];                 // s = x (poly[0] + x^2 (poly[1] + ...)) there
+  int tiles;                     // tiles of a sequence (equal sequences)
+  int fold, nsplit;
+  float* part;                   // [nsplit][rows][2 * hkv * hd] fp32
+};
+
+// ---- where a workgroup works ------------------------------------------------------------------------------------------------
+struct Work { int lo, len, prefix, t; };       // rows of its sequence, its prefix, its tile; len = 0: nothing to do
+
+// QUERIES: tiles are taken from the last on (causal: the heaviest first), keys from the first on.
+template <int BQ, bool QUERIES>
+__device__ __forceinline__ Work find_work(const ScoreCall& c, int rank, int lane) {
+  const ScoreArgs& a = c.a;
+  int i, t;
+  if (!a.seq_start) {
+    i = rank % a.n_seq;
+    t = QUERIES ? tile_of_rank(rank / a.n_seq, c.tiles, c.fold) : key_tile_of_rank(rank / a.n_seq, c.tiles, c.fold);
+  } else {
+    const int u = QUERIES ? a.rows / BQ + a.n_seq - 1 - rank : rank;
+    i = 0;
+    for (int n = a.n_seq; n > 1;) {            // sequences i .. i + n - 1 are left; 64 of them are looked at
+      const int step = (n + 63) >> 6, at = lane * step;
+      const bool before = at < n && min(max(a.seq_start[i + min(at, n - 1)], 0), a.rows) / BQ + i + at <= u;
+      const int k = max(__popcll(__ballot(before)) - 1, 0) * step;
+      i += k;
+      n = min(step, n - k);
+    }
+    i = __builtin_amdgcn_readfirstlane(i);
+    t = u - (min(max(a.seq_start[i], 0), a.rows) / BQ + i);
+  }
+  const SeqSpan s = seq_span(a, i);
+  Work w;
+  w.lo = __builtin_amdgcn_readfirstlane(s.lo);
+  w.t = __builtin_amdgcn_readfirstlane(t);
+  const int len = __builtin_amdgcn_readfirstlane(s.hi - s.lo);
+  w.prefix = __builtin_amdgcn_readfirstlane(s.prefix);
+  w.len = w.t >= 0 && w.t * BQ < len ? len : 0;
+  return w;
+}
+
+// ---- tiles ------------------------------------------------------------------------------------------------------------------
+// Rows row0 .. row0 + ROWS - 1 of one head of a sequence -> LDS.  Load j of a thread covers rows j * SWEEP + its own inside a sweep; the
+// swizzle repeats every 16 rows, so one offset per matrix is enough.  The descriptor starts at the tile's first row and ends with the
+// sequence's last, so offsets stay small however long the buffer is.
+template <int HD, int NTHR, int ROWS>
+struct Loader {
+  using G = Geo<HD>;
+  static constexpr int SWEEP = NTHR / G::PPR, NLD = ROWS / SWEEP;
+  static_assert(SWEEP % 16 == 0 && ROWS % SWEEP == 0, "swizzle period");
+  const bf16* base;
+  int64_t ld;
+  unsigned off0, hop;
+  __device__ __forceinline__ void init(const bf16* p, int64_t stride, int wave, int lane) {
+    const int sl = wave * 64 + lane, r = sl / G::PPR, c = (sl % G::PPR) ^ G::swz(r);
+    base = p; ld = stride;
+    off0 = (unsigned)((r * ld + c * 8) * 2);
+    hop = (unsigned)(SWEEP * ld * 2);
+  }
+  __device__ __forceinline__ void fetch(lds_char* tile, int row0, int len, int wave) const {
+    const int rem = min(len - row0, ROWS);
+    const rsrc_words rs = raw_rsrc(base + (int64_t)row0 * ld, rem > 0 ? (unsigned)(((rem - 1) * ld + HD) * 2) : 0u);
+#pragma unroll
+    for (int j = 0; j < NLD; ++j) load_to_lds_b128(rs, (unsigned)(size_t)(tile + (j * (NTHR / 64) + wave) * 1024), off0 + j * hop);
+  }
+};
+
+// ---- scores -----------------------------------------------------------------------------------------------------------------
+// 16 products x -> capped scores in units of log 2.  tanh(y) / y is a polynomial in y^2 up to |y| = 0.6 (fitted by least squares of the
+// relative error, 7e-8 at most), which is where scores lie that are not pressed against the cap; a block with any larger one takes
+// 1 - 2 / (exp(2 y) + 1), whose two transcendental instructions each cost as much as four others.
+__device__ __forceinline__ void cap_block(f32x16& x, const ScoreCall& c) {
+  float mx = 0.f;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) mx = fmaxf(mx, fabsf(x[e]));
+  if (__any(mx > c.small)) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = fmaf(__builtin_amdgcn_rcpf(fast_exp2(x[e] * c.kx) + 1.f), -2.f * c.c2, c.c2);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float y = x[e] * x[e];
+      x[e] *= fmaf(y, fmaf(y, fmaf(y, fmaf(y, c.poly[4], c.poly[3]), c.poly[2]), c.poly[1]), c.poly[0]);
+    }
+  }
+}
+
+// ---- forward ----------------------------------------------------------------------------------------------------------------
+struct Row { int q, last; };           // a lane's query and the last key that it sees, both inside the sequence
+
+template <int HD, int BUF, int NC, bool CAP>
+__device__ __forceinline__ void fwd_tile(lds_char* lds, const FragOff<HD>& fo, const ScoreCall& c, const bf16x8 (&qf)[HD / 16], f32x16 (&o)[HD / 32],
+                                         float& m, float& l, int kv0, Row row, int hf, float slope2, bool online, bool need_mask, bool ahead) {
+  using G = Geo<HD>;
+  constexpr int KT = BUF, VT = BUF + G::TILEB, AHEAD = 3, NPV = G::NHB * 2 * NC, VA = 4;
+  bf16x8 kf[AHEAD + 1][NC];
+#pragma unroll
+  for (int kk = 0; kk < AHEAD; ++kk)
+#pragma unroll
+    for (int n = 0; n < NC; ++n) kf[kk][n] = frag_rows<HD>(lds, fo, KT, n * 32, kk);
+  f32x16 s[NC];
+#pragma unroll
+  for (int kk = 0; kk < G::NKK; ++kk) {
+    if (kk + AHEAD < G::NKK) {
+#pragma unroll
+      for (int n = 0; n < NC; ++n) kf[(kk + AHEAD) % (AHEAD + 1)][n] = frag_rows<HD>(lds, fo, KT, n * 32, kk + AHEAD);
+    }
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+      if (kk == 0) s[n] = mfma0(kf[0][n], qf[0]);
+      else s[n] = MFMA(kf[kk % (AHEAD + 1)][n], qf[kk], s[n]);
+    }
+    SCHED_FENCE;
+  }
+  bf16x8 vf[VA];
+#pragma unroll
+  for (int i = 0; i < VA; ++i) vf[i] = frag_cols_tr<HD>(lds, fo, VT, (i / G::NHB) * 16, i % G::NHB);
+  SCHED_FENCE;
+  if (CAP) {
+#pragma unroll
+    for (int n = 0; n < NC; ++n) cap_block(s[n], c);
+  }
+  // bias: slope (key - query), which is off[n] + slope * row inside the block; keys ahead of the query get twice theirs back
+  const bool bias = c.a.slope != nullptr;
+  float off[NC];
+#pragma unroll
+  for (int n = 0; n < NC; ++n) off[n] = bias ? slope2 * (float)(kv0 + n * 32 + hf * 4 - row.q) : 0.f;
+  if (bias) {
+    const float sb = CAP ? slope2 : slope2 * c.raw * LN2;
+#pragma unroll
+    for (int n = 0; n < NC; ++n)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[n][e] += sb * (float)acc_row(e, 0);
+    if (ahead) {
+#pragma unroll
+      for (int n = 0; n < NC; ++n) {
+        const float first = (float)(kv0 + n * 32 + hf * 4 - row.q);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[n][e] -= 2.f * sb * fmaxf(first + (float)acc_row(e, 0), 0.f);
+      }
+    }
+  }
+  if (need_mask) {
+    const int bound = row.last - kv0 - hf * 4;
+#pragma unroll
+    for (int n = 0; n < NC; ++n)
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (n * 32 + acc_row(e, 0) > bound) s[n][e] = -INFINITY;
+  }
+  const float sl = CAP ? 1.f : c.sl2;
+  if (!CAP || online) {
+    float top = -INFINITY;                       // the two lanes that hold a row differ in `off`, so they compare finished scores
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[n][e]);
+      top = fmaxf(top, fmaf(mx, sl, off[n]));
+    }
+    const float mn = fmaxf(m, half_max(top, hf));
+#pragma unroll
+    for (int n = 0; n < NC; ++n)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[n][e] = fast_exp2(fmaf(s[n][e], sl, off[n] - mn));
+    if (__any(mn != m)) {                        // the running max moved for some query of the wavefront
+      const float alpha = fast_exp2(m - mn);
+      l *= alpha;
+#pragma unroll
+      for (int hb = 0; hb < G::NHB; ++hb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[hb][e] *= alpha;
+    }
+    m = mn;
+  } else {
+#pragma unroll
+    for (int n = 0; n < NC; ++n)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[n][e] = fast_exp2(bias ? s[n][e] + off[n] : s[n][e]);
+  }
+  // P is rounded to bf16 for its product; the row's sum is of what it was before
+  bf16x8 pf[NC][2];
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int n = 0; n < NC; ++n)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) { sum[e & 3] += s[n][e]; pf[n][e >> 3][e & 7] = (bf16)s[n][e]; }
+  l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  SCHED_FENCE;
+#pragma unroll
+  for (int i = 0; i < NPV; ++i) {
+    const bf16x8 v = vf[i % VA];
+    if (i + VA < NPV) {
+      const int n = i + VA;
+      vf[i % VA] = frag_cols_tr<HD>(lds, fo, VT, (n / G::NHB) * 16, n % G::NHB);
+    }
+    o[i % G::NHB] = MFMA(v, pf[(i / G::NHB) >> 1][(i / G::NHB) & 1], o[i % G::NHB]);
+    SCHED_FENCE;
+  }
+}
+
+// Workgroup shapes as in attn_mfma.hip: KS wavefronts share 32 queries, each taking its part of a step's keys.
+template <int NT, int KS> constexpr int block_q() { return (NT / 64) * 32 / KS; }
+constexpr int WIDE = 512, NARROW = 256;
+
+template <int HD, int NT, int KS, bool CAP>
+__global__ __launch_bounds__(NT, KS == 4 && HD == 64 ? 4 : 2) void score_fwd_kernel(ScoreCall c) {
+  using G = Geo<HD>;
+  constexpr int SUB = KS == 4 ? 2 : 1, TS = TK * SUB;
+  constexpr int KT = 0, VT = G::TILEB, BUFB = SUB * 2 * G::TILEB;
+  extern __shared__ __attribute__((aligned(1024))) char smem_raw[];
+  lds_char* lds = (lds_char*)smem_raw;
+  const ScoreArgs& a = c.a;
+  const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  constexpr int BQ = block_q<NT, KS>(), KW = KS == 1 ? 64 : 32;
+  const int qb = wave / KS, kh = wave % KS;
+  const int j = blockIdx.x % a.h, g = j / (a.h / a.hkv);
+  const Work w = find_work<BQ, true>(c, blockIdx.x / a.h, lane);
+  if (w.len == 0) return;
+  const int q0b = w.t * BQ, q0w = q0b + qb * 32, vis = a.causal ? w.prefix : w.len;       // the first `vis` keys are seen by all
+  const Row row{q0w + (lane & 31), min(max(a.causal ? q0w + (lane & 31) : 0, vis - 1), w.len - 1)};
+  const float slope2 = a.slope ? a.slope[j] * LOG2E : 0.f;
+  const int end = max(min(q0b + BQ, w.len), vis), end_w = max(min(q0w + 32, w.len), vis);   // keys that the workgroup, the wavefront sees
+  const int nstep = (end + TS - 1) / TS;
+  Loader<HD, NT, TK> K, V;
+  K.init((const bf16*)a.k + (int64_t)w.lo * a.ldk + g * HD, a.ldk, wave, lane);
+  V.init((const bf16*)a.v + (int64_t)w.lo * a.ldv + g * HD, a.ldv, wave, lane);
+  auto fetch = [&](int buf, int row0) {
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) {
+      K.fetch(lds + buf + u * 2 * G::TILEB + KT, row0 + u * TK, w.len, wave);
+      V.fetch(lds + buf + u * 2 * G::TILEB + VT, row0 + u * TK, w.len, wave);
+    }
+  };
+  fetch(0, 0);
+  if (nstep > 1) fetch(BUFB, TS);
+
+  const bf16* qp = (const bf16*)a.q + (int64_t)w.lo * a.ldq + j * HD;
+  bf16x8 qf[G::NKK];
+#pragma unroll
+  for (int kk = 0; kk < G::NKK; ++kk) qf[kk] = frag_rows_global(qp, a.ldq, q0w, w.len, kk * 16, lane);
+  f32x16 o[G::NHB];
+#pragma unroll
+  for (int hb = 0; hb < G::NHB; ++hb) zero(o[hb]);
+  // Capped scores lie within c2 of zero and a bias only lowers them: up to c2 = 80 exp2 of them and its sums stay well inside fp32, so
+  // the running maximum (and the rescaling that comes with it) is not needed.
+  const bool online = !CAP || c.c2 > 80.f || slope2 < 0.f;
+  float m = online ? -1e30f : 0.f, l = 0.f;
+  FragOff<HD> fo;
+  fo.init(lane, lds);
+  if (KS > 1) fo.hop((kh >> 1) * 2 * G::TILEB + (kh & 1) * 32 * G::ROWB);
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+
+  auto step = [&](int t, auto buf) {
+    constexpr int BUF = decltype(buf)::value;
+    const int kv0 = t * TS, kvw = kv0 + kh * 32;
+    if (kvw < end_w && q0w < w.len) {
+      const bool need_mask = (a.causal && kvw + KW > max(q0w + 1, vis)) || kvw + KW > w.len;
+      fwd_tile<HD, BUF, KW / 32, CAP>(lds, fo, c, qf, o, m, l, kvw, row, hf, slope2, online, need_mask, kvw + KW > q0w + 1);
+    }
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if (t + 2 < nstep) fetch(BUF, kv0 + 2 * TS);
+  };
+  for (int t = 0; t < nstep; t += 2) {
+    step(t, std::integral_constant<int, 0>{});
+    if (t + 1 < nstep) step(t + 1, std::integral_constant<int, BUFB>{});
+  }
+
+  l = half_sum(l, hf);
+  if constexpr (KS > 1) {
+    constexpr int OB = G::NHB * 4 * 1024, NQB = BQ / 32;
+    static_assert((KS - 1) * NQB * (OB + 512) <= 2 * BUFB, "the merge area fits the tile buffers");
+    auto area = [&](int part) { return lds + ((part - 1) * NQB + qb) * (OB + 512); };
+    if (kh > 0) {
+      lds_char* mo = area(kh) + lane * 16;
+#pragma unroll
+      for (int hb = 0; hb < G::NHB; ++hb)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4)
+          *(__attribute__((address_space(3))) f32x4*)(mo + (hb * 4 + q4) * 1024) =
+              f32x4{o[hb][q4 * 4], o[hb][q4 * 4 + 1], o[hb][q4 * 4 + 2], o[hb][q4 * 4 + 3]};
+      *(__attribute__((address_space(3))) f32x2*)(area(kh) + OB + lane * 8) = f32x2{m, l};
+    }
+    __syncthreads();
+    if (kh > 0) return;
+#pragma unroll
+    for (int part = 1; part < KS; ++part) {
+      lds_char* mo = area(part) + lane * 16;
+      const f32x2 other = *(__attribute__((address_space(3))) const f32x2*)(area(part) + OB + lane * 8);
+      const float mn = fmaxf(m, other.x);
+      const float a0 = fast_exp2(m - mn), a1 = fast_exp2(other.x - mn);
+      l = l * a0 + other.y * a1;
+#pragma unroll
+      for (int hb = 0; hb < G::NHB; ++hb)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          const f32x4 v = *(__attribute__((address_space(3))) const f32x4*)(mo + (hb * 4 + q4) * 1024);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[hb][q4 * 4 + e] = o[hb][q4 * 4 + e] * a0 + v[e] * a1;
+        }
+      m = mn;
+    }
+  }
+  if (row.q < w.len) {
+    const float inv = 1.f / l;
+    bf16* orow = (bf16*)a.o + (int64_t)(w.lo + row.q) * a.ldo + j * HD;
+#pragma unroll
+    for (int hb = 0; hb < G::NHB; ++hb)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) {
+        bf16x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (bf16)(o[hb][q4 * 4 + e] * inv);
+        *reinterpret_cast<bf16x4*>(orow + hb * 32 + q4 * 8 + hf * 4) = v;
+      }
+    if (hf == 0 && a.lse) a.lse[(int64_t)j * a.rows + w.lo + row.q] = (m + log2f(l)) * LN2;
+  }
+}
+
+// ---- dQ ---------------------------------------------------------------------------------------------------------------------
+template <int HD, int BUF, bool CAP>
+__device__ __forceinline__ void dq_block(lds_char* lds, const FragOff<HD>& fo, const ScoreCall& c, const bf16x8 (&qf)[HD / 16], const bf16x8 (&dof)[HD / 16],
+                                         f32x16 (&dq)[HD / 32], int n, int kv0, Row row, int hf, float slope2, float lse2, const f32x16& ndl,
+                                         bool need_mask, bool ahead) {
+  using G = Geo<HD>;
+  constexpr int KT = BUF, VT = BUF + G::TILEB, AHEAD = 3, NDQ = G::NHB * 2, VA = 4;
+  bf16x8 kf[AHEAD + 1][2];
+#pragma unroll
+  for (int kk = 0; kk < AHEAD; ++kk) { kf[kk][0] = frag_rows<HD>(lds, fo, KT, n * 32, kk); kf[kk][1] = frag_rows<HD>(lds, fo, VT, n * 32, kk); }
+  f32x16 s, dp;
+#pragma unroll
+  for (int kk = 0; kk < G::NKK; ++kk) {
+    if (kk + AHEAD < G::NKK) {
+      kf[(kk + AHEAD) % (AHEAD + 1)][0] = frag_rows<HD>(lds, fo, KT, n * 32, kk + AHEAD);
+      kf[(kk + AHEAD) % (AHEAD + 1)][1] = frag_rows<HD>(lds, fo, VT, n * 32, kk + AHEAD);
+    }
+    if (kk == 0) { s = mfma0(kf[0][0], qf[0]); dp = MFMA(kf[0][1], dof[0], ndl); }
+    else {
+      s = MFMA(kf[kk % (AHEAD + 1)][0], qf[kk], s);
+      dp = MFMA(kf[kk % (AHEAD + 1)][1], dof[kk], dp);
+    }
+    SCHED_FENCE;
+  }
+  bf16x8 tf[VA];
+#pragma unroll
+  for (int i = 0; i < VA; ++i) tf[i] = frag_cols_tr<HD>(lds, fo, KT, n * 32 + (i / G::NHB) * 16, i % G::NHB);
+  SCHED_FENCE;
+  if (CAP) {
+    cap_block(s, c);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {               // dP - delta times the cap's derivative 1 - t^2
+      const float t = s[e] * c.ic2;
+      dp[e] *= fmaf(-t, t, 1.f);
+    }
+  }
+  const float first = (float)(kv0 + n * 32 + hf * 4 - row.q), off = (c.a.slope ? slope2 * first : 0.f) - lse2;
+  const float sl = CAP ? 1.f : c.sl2;
+  if (c.a.slope) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = fmaf(s[e], sl, off) + slope2 * (float)acc_row(e, 0);
+    if (ahead) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] -= 2.f * slope2 * fmaxf(first + (float)acc_row(e, 0), 0.f);
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = fast_exp2(s[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = fast_exp2(fmaf(s[e], sl, off));
+  }
+  if (need_mask) {
+    const int bound = row.last - kv0 - hf * 4 - n * 32;
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (acc_row(e, 0) > bound) s[e] = 0.f;
+  }
+  bf16x8 dsf[2];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) dsf[e >> 3][e & 7] = (bf16)(s[e] * dp[e]);
+  SCHED_FENCE;
+#pragma unroll
+  for (int i = 0; i < NDQ; ++i) {
+    const bf16x8 v = tf[i % VA];
+    if (i + VA < NDQ) {
+      const int x = i + VA;
+      tf[i % VA] = frag_cols_tr<HD>(lds, fo, KT, n * 32 + (x / G::NHB) * 16, x % G::NHB);
+    }
+    dq[i % G::NHB] = MFMA(v, dsf[i / G::NHB], dq[i % G::NHB]);
+    SCHED_FENCE;
+  }
+}
+
+template <int HD, int NT, int KS, bool CAP>
+__device__ __forceinline__ void dq_workgroup(const ScoreCall& c, lds_char* lds, int j, int rank) {
+  using G = Geo<HD>;
+  constexpr int SUB = KS == 4 ? 2 : 1, TS = TK * SUB;
+  constexpr int KT = 0, VT = G::TILEB, BUFB = SUB * 2 * G::TILEB;
+  const ScoreArgs& a = c.a;
+  const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  constexpr int BQ = block_q<NT, KS>();
+  const int qb = wave / KS, kh = wave % KS, g = j / (a.h / a.hkv);
+  const Work w = find_work<BQ, true>(c, rank, lane);
+  if (w.len == 0) return;
+  const int q0b = w.t * BQ, q0w = q0b + qb * 32, vis = a.causal ? w.prefix : w.len;
+  const Row row{q0w + (lane & 31), min(max(a.causal ? q0w + (lane & 31) : 0, vis - 1), w.len - 1)};
+  const float slope2 = a.slope ? a.slope[j] * LOG2E : 0.f;
+  const int end = max(min(q0b + BQ, w.len), vis), end_w = max(min(q0w + 32, w.len), vis);
+  const int nstep = (end + TS - 1) / TS;
+  Loader<HD, NT, TK> K, V;
+  K.init((const bf16*)a.k + (int64_t)w.lo * a.ldk + g * HD, a.ldk, wave, lane);
+  V.init((const bf16*)a.v + (int64_t)w.lo * a.ldv + g * HD, a.ldv, wave, lane);
+  auto fetch = [&](int buf, int row0) {
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) {
+      K.fetch(lds + buf + u * 2 * G::TILEB + KT, row0 + u * TK, w.len, wave);
+      V.fetch(lds + buf + u * 2 * G::TILEB + VT, row0 + u * TK, w.len, wave);
+    }
+  };
+  fetch(0, 0);
+  if (nstep > 1) fetch(BUFB, TS);
+
+  const bf16* qp = (const bf16*)a.q + (int64_t)w.lo * a.ldq + j * HD;
+  const bf16* dop = (const bf16*)a.dout + (int64_t)w.lo * a.lddo + j * HD;
+  const bf16* op = (const bf16*)a.o + (int64_t)w.lo * a.ldo + j * HD;
+  bf16x8 qf[G::NKK], dof[G::NKK];
+#pragma unroll
+  for (int kk = 0; kk < G::NKK; ++kk) {
+    qf[kk] = frag_rows_global(qp, a.ldq, q0w, w.len, kk * 16, lane);
+    dof[kk] = frag_rows_global(dop, a.lddo, q0w, w.len, kk * 16, lane);
+  }
+  // delta = rowsum(dO * O) of the lane's query, from the dO fragments in registers; written out for the dK/dV pass
+  float part = 0.f;
+#pragma unroll
+  for (int kk = 0; kk < G::NKK; ++kk) {
+    const bf16x8 of = frag_rows_global(op, a.ldo, q0w, w.len, kk * 16, lane);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) part = fmaf((float)dof[kk][e], (float)of[e], part);
+  }
+  const float dl = half_sum(part, hf);
+  float lse2 = 1e30f;                                  // rows past the end: P = 0
+  if (row.q < w.len) {
+    const int64_t at = (int64_t)j * a.rows + w.lo + row.q;
+    lse2 = a.lse[at] * LOG2E;
+    if (hf == 0 && kh == 0) a.delta[at] = dl;
+  }
+  f32x16 dq[G::NHB], ndl;
+#pragma unroll
+  for (int hb = 0; hb < G::NHB; ++hb) zero(dq[hb]);
+#pragma unroll
+  for (int e = 0; e < 16; ++e) ndl[e] = -dl;
+  FragOff<HD> fo;
+  fo.init(lane, lds);
+  if (KS > 1) fo.hop((kh >> 1) * 2 * G::TILEB + (kh & 1) * 32 * G::ROWB);
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+
+  auto step = [&](int t, auto buf) {
+    constexpr int BUF = decltype(buf)::value;
+    const int kv0 = t * TS, kvw = kv0 + kh * 32;
+    if (kvw < end_w && q0w < w.len) {
+#pragma unroll
+      for (int n = 0; n < (KS > 1 ? 1 : 2); ++n) {
+        const int k0 = kvw + n * 32;
+        if (n > 0 && k0 >= end_w) continue;            // no query of the wavefront sees this block
+        const bool need_mask = (a.causal && k0 + 32 > max(q0w + 1, vis)) || k0 + 32 > w.len;
+        dq_block<HD, BUF, CAP>(lds, fo, c, qf, dof, dq, n, kvw, row, hf, slope2, lse2, ndl, need_mask, k0 + 32 > q0w + 1);
+      }
+    }
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if (t + 2 < nstep) fetch(BUF, kv0 + 2 * TS);
+  };
+  for (int t = 0; t < nstep; t += 2) {
+    step(t, std::integral_constant<int, 0>{});
+    if (t + 1 < nstep) step(t + 1, std::integral_constant<int, BUFB>{});
+  }
+
+  if constexpr (KS > 1) {      // add the other key parts' dQ to the first's, in order, through LDS
+    constexpr int OB = G::NHB * 4 * 1024, NQB = BQ / 32;
+    static_assert((KS - 1) * NQB * OB <= 2 * BUFB, "the merge area fits the tile buffers");
+    if (kh > 0) {
+      lds_char* mo = lds + ((kh - 1) * NQB + qb) * OB + lane * 16;
+#pragma unroll
+      for (int hb = 0; hb < G::NHB; ++hb)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4)
+          *(__attribute__((address_space(3))) f32x4*)(mo + (hb * 4 + q4) * 1024) =
+              f32x4{dq[hb][q4 * 4], dq[hb][q4 * 4 + 1], dq[hb][q4 * 4 + 2], dq[hb][q4 * 4 + 3]};
+    }
+    __syncthreads();
+    if (kh > 0) return;
+#pragma unroll
+    for (int p = 1; p < KS; ++p) {
+      lds_char* mo = lds + ((p - 1) * NQB + qb) * OB + lane * 16;
+#pragma unroll
+      for (int hb = 0; hb < G::NHB; ++hb)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          const f32x4 v = *(__attribute__((address_space(3))) const f32x4*)(mo + (hb * 4 + q4) * 1024);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) dq[hb][q4 * 4 + e] += v[e];
+        }
+    }
+  }
+  if (row.q < w.len) {
+    bf16* out = (bf16*)a.dq + (int64_t)(w.lo + row.q) * a.lddq + j * HD;
+#pragma unroll
+    for (int hb = 0; hb < G::NHB; ++hb)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) {
+        bf16x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (bf16)(dq[hb][q4 * 4 + e] * a.scale);
+        *reinterpret_cast<bf16x4*>(out + hb * 32 + q4 * 8 + hf * 4) = v;
+      }
+  }
+}
+template <int HD, int NT, int KS, bool CAP>
+__global__ __launch_bounds__(NT, 2) void score_dq_kernel(ScoreCall c) {
+  extern __shared__ __attribute__((aligned(1024))) char smem_raw[];
+  dq_workgroup<HD, NT, KS, CAP>(c, (lds_char*)smem_raw, blockIdx.x % c.a.h, blockIdx.x / c.a.h);
+}
+
+// ---- dK/dV ------------------------------------------------------------------------------------------------------------------
+// One workgroup = TQ keys of one (sequence, KV head): per 32 keys two wavefronts on a SIMD, one for dV, which makes P, one for dK, which
+// takes it (times the cap's derivative) from a 4 KiB slot in LDS; QS = 2: two such pairs, on every second 32 queries each.
+constexpr int KEYS = 128, KEYS_SMALL = 64;
+
+template <int HD, int TQ, int QS, bool CAP, bool OWN_DELTA>
+__device__ __forceinline__ void dkv_workgroup(const ScoreCall& c, lds_char* lds, int bx, int rank) {
+  using G = Geo<HD>;
+  constexpr int NTHR = TQ * 4 * QS, NB = TQ / 32 / QS, NKW = TQ / 32, TILEB = TQ * G::ROWB;
+  constexpr int QT = 0, OT = TILEB, LT = 2 * TILEB, DT = LT + TQ * 4, BUFB = DT + TQ * 4;
+  const ScoreArgs& a = c.a;
+  const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int role = wave / (NKW * QS), kw = wave % NKW, qs = QS == 2 ? (wave / NKW) % 2 : 0;
+  const int g = bx / c.nsplit, sp = bx % c.nsplit;
+  const int dkv = a.hkv * HD, grp = a.h / a.hkv / c.nsplit, j0 = g * (a.h / a.hkv) + sp * grp;
+  const Work w = find_work<TQ, false>(c, rank, lane);
+  if (w.len == 0) return;
+  const int kt = w.t, nkt = (w.len + TQ - 1) / TQ;
+  const bf16* qbase = (const bf16*)a.q + (int64_t)w.lo * a.ldq;
+  const bf16* dobase = (const bf16*)a.dout + (int64_t)w.lo * a.lddo;
+  const bf16* kp = (const bf16*)a.k + (int64_t)w.lo * a.ldk + g * HD;
+  const bf16* vp = (const bf16*)a.v + (int64_t)w.lo * a.ldv + g * HD;
+  const int k0b = kt * TQ, k0w = k0b + kw * 32;
+  const int key = k0w + (lane & 31);
+  const bool bias = a.slope != nullptr;
+
+  const int t_first = a.causal && k0b >= w.prefix ? kt : 0;     // a key of the prefix is seen by every query
+  const int per_head = nkt - t_first;
+  const int niter = per_head * grp;
+  Loader<HD, NTHR, TQ> Q, D;
+  Q.init(qbase, a.ldq, wave, lane);
+  D.init(dobase, a.lddo, wave, lane);
+  constexpr int NLD = Loader<HD, NTHR, TQ>::NLD, SWEEP = Loader<HD, NTHR, TQ>::SWEEP;
+  float stat_l = 0.f, stat_d = 0.f;
+  bf16x8 of[OWN_DELTA ? NLD : 1];
+  auto fetch = [&](int it, lds_char* buf) {
+    const int j = j0 + it / per_head, q0 = (t_first + it % per_head) * TQ;
+    Q.base = qbase + j * HD;
+    D.base = dobase + j * HD;
+    Q.fetch(buf + QT, q0, w.len, wave);
+    D.fetch(buf + OT, q0, w.len, wave);
+    if (wave < TQ / 64) {                // one query per lane; those past the end get P = 0
+      const int qi = q0 + wave * 64 + lane;
+      const int64_t at = (int64_t)j * a.rows + w.lo + qi;
+      const float slope2 = bias ? a.slope[j] * LOG2E : 0.f;
+      stat_l = qi < w.len ? -LOG2E * a.lse[at] - (bias ? slope2 * (float)(qi - k0b) : 0.f) : -1e30f;
+      if (!OWN_DELTA) stat_d = qi < w.len ? a.delta[at] : 0.f;
+    }
+    if constexpr (OWN_DELTA) {           // the pieces of O that go with the pieces of dO this thread has just asked for
+      const bf16* oh = (const bf16*)a.o + (int64_t)w.lo * a.ldo + j * HD;
+      const int sl = wave * 64 + lane, cc = (sl % G::PPR) ^ G::swz(sl / G::PPR);
+#pragma unroll
+      for (int n = 0; n < NLD; ++n) of[n] = *reinterpret_cast<const bf16x8*>(oh + (int64_t)min(q0 + n * SWEEP + sl / G::PPR, w.len - 1) * a.ldo + cc * 8);
+    }
+  };
+  // the statistics of the tile fetched last: the exponents' share of the query (-lse, and the bias up to the workgroup's first key), and -delta
+  auto put_stats = [&](lds_char* buf, int q_of) {
+    if (wave < TQ / 64) {
+      *(__attribute__((address_space(3))) float*)(buf + LT + (wave * 64 + lane) * 4) = stat_l;
+      if (!OWN_DELTA) *(__attribute__((address_space(3))) float*)(buf + DT + (wave * 64 + lane) * 4) = -stat_d;
+    }
+    if constexpr (OWN_DELTA) {
+      __builtin_amdgcn_s_waitcnt(0);     // own loads only, so no barrier: thread and piece correspond as in the fetch, PPR lanes hold a row
+      float part[NLD];
+#pragma unroll
+      for (int n = 0; n < NLD; ++n) {
+        const bf16x8 dv = *(__attribute__((address_space(3))) const bf16x8*)(buf + OT + (n * (NTHR / 64) + wave) * 1024 + lane * 16);
+        part[n] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) part[n] = fmaf((float)dv[e], (float)of[n][e], part[n]);
+      }
+#pragma unroll
+      for (int x = 1; x < G::PPR; x <<= 1)
+#pragma unroll
+        for (int n = 0; n < NLD; ++n) part[n] += __shfl_xor(part[n], x);
+      if (lane % G::PPR == 0) {
+#pragma unroll
+        for (int n = 0; n < NLD; ++n) {
+          const int r = n * SWEEP + (wave * 64 + lane) / G::PPR;
+          *(__attribute__((address_space(3))) float*)(buf + DT + r * 4) = q_of + r < w.len ? -part[n] : 0.f;
+        }
+      }
+    }
+  };
+  fetch(0, lds);
+  put_stats(lds, t_first * TQ);
+  if (niter > 1) fetch(1, lds + BUFB);
+
+  FragOff<HD> fo;
+  fo.init(lane, lds);
+  if (QS == 2) fo.hop(qs * 32 * G::ROWB);
+  lds_char* cur = lds;
+  lds_char* ldp = lds + LT + hf * 16 + qs * 128;
+  int hopb = BUFB;
+  typedef __attribute__((address_space(3))) const f32x4* lds_f4;
+  // the pair's slot and its counts: produced = blocks written, consumed = blocks read; the waits are bounded
+  lds_char* pslot = lds + 2 * BUFB + (qs * NKW + kw) * 4096 + lane * 16;
+  volatile __attribute__((address_space(3))) int* produced = (volatile __attribute__((address_space(3))) int*)(lds + 2 * BUFB + QS * NKW * 4096) + qs * NKW + kw;
+  volatile __attribute__((address_space(3))) int* consumed = produced + QS * NKW;
+  if (tid < 2 * QS * NKW) ((volatile __attribute__((address_space(3))) int*)(lds + 2 * BUFB + QS * NKW * 4096))[tid] = 0;
+  auto wait_for = [&](volatile __attribute__((address_space(3))) int* count, int value) {
+    for (int guard = 0; *count != value && guard < (1 << 20); ++guard) __builtin_amdgcn_s_sleep(1);
+    asm volatile("" ::: "memory");
+  };
+  int nblk = 0;
+  auto turn = [&](int it) {
+    if (it + 1 < niter) put_stats(cur + hopb, (t_first + (it + 1) % per_head) * TQ);
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if (it + 2 < niter) fetch(it + 2, cur);
+    fo.hop(hopb);
+    cur += hopb;
+    ldp += hopb;
+    hopb = -hopb;
+  };
+
+  bf16x8 kf[G::NKK];
+#pragma unroll
+  for (int kk = 0; kk < G::NKK; ++kk) kf[kk] = frag_rows_global(role ? vp : kp, role ? a.ldv : a.ldk, k0w, w.len, kk * 16, lane);
+  f32x16 acc[G::NHB];                                  // dV^T or dK^T of the wavefront's 32 keys
+#pragma unroll
+  for (int hb = 0; hb < G::NHB; ++hb) zero(acc[hb]);
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+
+  if (role == 0) {
+    for (int it = 0; it < niter; ++it) {
+      const int tq = t_first + it % per_head, q0 = tq * TQ;
+      const bool diag = a.causal && tq <= kt;          // some query of the tile is ahead of some key: masked unless the key is in the prefix
+      const int lim0 = key < w.prefix ? -(1 << 30) : key - q0 - hf * 4 - qs * 32;
+      const float slope2 = bias ? a.slope[j0 + it / per_head] * LOG2E : 0.f, kbias = slope2 * (float)(key - k0b);
+      const bool ahead = bias && tq <= kt;             // keys ahead of their query: twice the bias back
+#pragma unroll
+      for (int qc = 0; qc < NB; ++qc) {
+        f32x4 l4[4];
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) l4[e4] = *reinterpret_cast<lds_f4>(ldp + (qc * QS * 32 + e4 * 8) * 4);
+        f32x16 s;
+        dkv_rows_product<HD, QT>(lds, fo, qc * QS * 32, kf, s);
+        bf16x8 tf[4];
+        dkv_tr_read<HD, OT>(lds, fo, qc * QS * 32, tf);
+        SCHED_FENCE;
+        float wc[CAP ? 16 : 1];
+        if (CAP) {
+          cap_block(s, c);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) { const float t = s[e] * c.ic2; wc[e] = fmaf(-t, t, 1.f); }
+        }
+        if (bias) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[e] = (CAP ? s[e] + l4[e >> 2][e & 3] : fmaf(s[e], c.sl2, l4[e >> 2][e & 3])) + kbias;
+          if (ahead) {
+            const float first = (float)(q0 + (qc * QS + qs) * 32 + hf * 4 - key);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] += 2.f * slope2 * fminf(first + (float)acc_row(e, 0), 0.f);
+          }
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[e] = fast_exp2(s[e]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[e] = fast_exp2(CAP ? s[e] + l4[e >> 2][e & 3] : fmaf(s[e], c.sl2, l4[e >> 2][e & 3]));
+        }
+        if (diag) {
+          asm volatile("" ::: "memory");               // keep this a (wave-uniform) branch: it is rarely taken
+          const int lim = lim0 - qc * QS * 32;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[e] = acc_row(e, 0) < lim ? 0.f : s[e];
+        }
+        wait_for(consumed, nblk);                      // the slot is free
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) {
+          f32x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = CAP ? s[e4 * 4 + e] * wc[CAP ? e4 * 4 + e : 0] : s[e4 * 4 + e];
+          *(__attribute__((address_space(3))) f32x4*)(pslot + e4 * 1024) = v;
+        }
+        asm volatile("" ::: "memory");                 // the LDS executes a wavefront's instructions in order: the count
+        *produced = ++nblk;                            // is written after the block
+        asm volatile("" ::: "memory");
+        bf16x8 pf[2];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) pf[e >> 3][e & 7] = (bf16)s[e];
+        SCHED_FENCE;
+        dkv_tr_product<HD, OT>(lds, fo, qc * QS * 32, tf, pf, acc);          // dV^T += dO^T . P
+      }
+      turn(it);
+    }
+  } else {
+    for (int it = 0; it < niter; ++it) {
+#pragma unroll
+      for (int qc = 0; qc < NB; ++qc) {
+        f32x16 dp;                                      // starts at -delta of the block's queries
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) {
+          const f32x4 d4 = *reinterpret_cast<lds_f4>(ldp + (DT - LT) + (qc * QS * 32 + e4 * 8) * 4);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) dp[e4 * 4 + e] = d4[e];
+        }
+        dkv_rows_product<HD, OT, true>(lds, fo, qc * QS * 32, kf, dp);               // dP - delta
+        bf16x8 tf[4];
+        dkv_tr_read<HD, QT>(lds, fo, qc * QS * 32, tf);
+        SCHED_FENCE;
+        wait_for(produced, nblk + 1);
+        f32x4 pv[4];
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) pv[e4] = *(__attribute__((address_space(3))) const f32x4*)(pslot + e4 * 1024);
+        asm volatile("" ::: "memory");
+        *consumed = ++nblk;
+        asm volatile("" ::: "memory");
+        bf16x8 df[2];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) df[e >> 3][e & 7] = (bf16)(pv[e >> 2][e & 3] * dp[e]);
+        SCHED_FENCE;
+        dkv_tr_product<HD, QT>(lds, fo, qc * QS * 32, tf, df, acc);          // dK^T += Q^T . dS
+      }
+      turn(it);
+    }
+  }
+
+  if constexpr (QS == 2) {       // add the second pair's sums to the first's, through LDS
+    static_assert(2 * NKW * G::NHB * 4 * 1024 <= 2 * BUFB, "the merge area fits the tile buffers");
+    lds_char* mo = lds + (role * NKW + kw) * (G::NHB * 4 * 1024) + lane * 16;
+    if (qs == 1) {
+#pragma unroll
+      for (int hb = 0; hb < G::NHB; ++hb)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4)
+          *(__attribute__((address_space(3))) f32x4*)(mo + (hb * 4 + q4) * 1024) =
+              f32x4{acc[hb][q4 * 4], acc[hb][q4 * 4 + 1], acc[hb][q4 * 4 + 2], acc[hb][q4 * 4 + 3]};
+    }
+    __syncthreads();
+    if (qs == 1) return;
+#pragma unroll
+    for (int hb = 0; hb < G::NHB; ++hb)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) {
+        const f32x4 v = *(__attribute__((address_space(3))) const f32x4*)(mo + (hb * 4 + q4) * 1024);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[hb][q4 * 4 + e] += v[e];
+      }
+  }
+
+  if (key < w.len) {             // role 0 holds dV, role 1 dK (still to be scaled)
+    const float osc = role ? a.scale : 1.f;
+    if (c.nsplit == 1) {
+      bf16* out = role ? (bf16*)a.dk + (int64_t)(w.lo + key) * a.lddk + g * HD : (bf16*)a.dv + (int64_t)(w.lo + key) * a.lddv + g * HD;
+#pragma unroll
+      for (int hb = 0; hb < G::NHB; ++hb)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          bf16x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = (bf16)(acc[hb][q4 * 4 + e] * osc);
+          *reinterpret_cast<bf16x4*>(out + hb * 32 + q4 * 8 + hf * 4) = v;
+        }
+    } else {                     // this split's share, fp32; score_dkv_reduce_kernel adds them up in a fixed order
+      float* out = c.part + ((int64_t)sp * a.rows + w.lo + key) * (2 * dkv) + g * HD + (role ? 0 : dkv);
+#pragma unroll
+      for (int hb = 0; hb < G::NHB; ++hb)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          f32x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = acc[hb][q4 * 4 + e] * osc;
+          *reinterpret_cast<f32x4*>(out + hb * 32 + q4 * 8 + hf * 4) = v;
+        }
+    }
+  }
+}
+template <int HD, int TQ, int QS, bool CAP>
+__global__ __launch_bounds__(TQ * 4 * QS, 2) void score_dkv_kernel(ScoreCall c) {
+  extern __shared__ __attribute__((aligned(1024))) char smem_raw[];
+  const int nx = c.a.hkv * c.nsplit;
+  dkv_workgroup<HD, TQ, QS, CAP, false>(c, (lds_char*)smem_raw, blockIdx.x % nx, blockIdx.x / nx);
+}
+
+// dQ and dK/dV of a small problem in one launch, which neither fills by itself; the dK/dV workgroups, the longer ones, come first
+template <int HD, int KS, int QS, bool CAP>
+__global__ __launch_bounds__(256 * QS, 2) void score_bwd_kernel(ScoreCall c, int n_dkv) {
+  static_assert(KS == 2 * QS, "one workgroup size");
+  extern __shared__ __attribute__((aligned(1024))) char smem_raw[];
+  const int id = blockIdx.x, nx = c.a.hkv * c.nsplit;
+  if (id < n_dkv) dkv_workgroup<HD, KEYS_SMALL, QS, CAP, true>(c, (lds_char*)smem_raw, id % nx, id / nx);
+  else dq_workgroup<HD, 256 * QS, KS, CAP>(c, (lds_char*)smem_raw, (id - n_dkv) % c.a.h, (id - n_dkv) / c.a.h);
+}
+
+// dK | dV = sum over splits, in split order, rounded once; rows of no sequence are left alone
+__global__ __launch_bounds__(256) void score_dkv_reduce_kernel(ScoreCall c) {
+  const ScoreArgs& a = c.a;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int dkv = a.hkv * a.hd, per_row = 2 * dkv / 4;
+  if (i >= (int64_t)a.rows * per_row) return;
+  const int row = (int)(i / per_row), col = (int)(i % per_row) * 4;
+  SeqSpan s;
+  if (!seq_of_row(a, row, s)) return;
+  f32x4 acc = *reinterpret_cast<const f32x4*>(c.part + (int64_t)row * (2 * dkv) + col);
+  for (int sp = 1; sp < c.nsplit; ++sp) acc += *reinterpret_cast<const f32x4*>(c.part + ((int64_t)sp * a.rows + row) * (2 * dkv) + col);
+  bf16x4 o;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] = (bf16)acc[e];
+  bf16* out = col < dkv ? (bf16*)a.dk + (int64_t)row * a.lddk + col : (bf16*)a.dv + (int64_t)row * a.lddv + col - dkv;
+  *reinterpret_cast<bf16x4*>(out) = o;
+}
+
+// ---- host -------------------------------------------------------------------------------------------------------------------
+template <int HD, int KS> constexpr size_t fwd_lds() { return (size_t)(KS == 4 ? 8 : 4) * Geo<HD>::TILEB; }
+template <int HD, int TQ, int QS> constexpr size_t dkv_lds() { return (size_t)2 * (2 * TQ * Geo<HD>::ROWB + 2 * TQ * 4) + QS * (TQ / 32) * 4096 + 64; }
+
+template <typename K>
+hipError_t allow_lds(K kern, size_t bytes) {
+  return hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+
+constexpr int64_t RESIDENT = 2 * 256;  // workgroups of 4 wavefronts that a 256-CU chip holds (the scratch size depends on it, so it is a constant)
+
+// grid slots of bq rows each (times heads: workgroups), and what of them there is to do at least
+int64_t slots(const ScoreArgs& a, int bq) {
+  return a.seq_start ? a.rows / bq + a.n_seq : (int64_t)a.n_seq * ((a.rows / a.n_seq + bq - 1) / bq);
+}
+
+enum Shape { SHAPE_WIDE = 1, SHAPE_NARROW = 2, SHAPE_SPLIT = 3, SHAPE_SPLIT4 = 4 };
+// as for plain attention: 8 wavefronts x 32 queries when that gives two workgroups per CU, else 4, else 64 queries with the keys split
+Shape fwd_shape(const ScoreArgs& a, int width) {
+  if (width >= 1 && width <= 4) return (Shape)width;
+  if (slots(a, 256) * a.h >= RESIDENT) return SHAPE_WIDE;
+  if (slots(a, 128) * a.h >= RESIDENT) return SHAPE_NARROW;
+  return slots(a, 64) * a.h <= (a.hd == 64 ? RESIDENT : RESIDENT / 2) && a.rows / a.n_seq >= 1000 ? SHAPE_SPLIT4 : SHAPE_SPLIT;
+}
+int dkv_splits(const ScoreArgs& a, int tq) {
+  const int grp = a.h / a.hkv;
+  const int64_t wgs = slots(a, tq) * a.hkv;
+  int ns = 1;
+  while (ns < grp && wgs * ns < RESIDENT) {
+    int nx = ns + 1;
+    while (grp % nx) ++nx;
+    ns = nx;
+  }
+  return ns;
+}
+bool dkv_small(const ScoreArgs& a, int width) {
+  if (width >= 1 && width <= 4) return width >= 3;
+  return slots(a, KEYS) * a.hkv * dkv_splits(a, KEYS) < RESIDENT;
+}
+
+ScoreCall score_call(const ScoreArgs& a) {
+  ScoreCall c{};
+  c.a = a;
+  c.sl2 = a.scale * LOG2E;
+  c.raw = 1.f / a.scale;
+  c.nsplit = 1;
+  if (a.cap > 0.f) {
+    static const double p[5] = {0.999999926868628, -0.3333230997148176, 0.13310173617653454, -0.052101478331093104, 0.015475425016233654};
+    const double r = (double)a.scale / a.cap, c2 = (double)a.cap * 1.4426950408889634;
+    c.c2 = (float)c2;
+    c.ic2 = (float)(1.0 / c2);
+    c.kx = (float)(2.0 * 1.4426950408889634 * r);
+    c.small = (float)(0.6 / r);
+    double f = c2 * r;
+    for (int i = 0; i < 5; ++i, f *= r * r) c.poly[i] = (float)(p[i] * f);
+  }
+  return c;
+}
+
+template <int HD, int NT, int KS, bool CAP>
+hipError_t fwd_launch(ScoreCall c, hipStream_t s) {
+  constexpr size_t lds_bytes = fwd_lds<HD, KS>();
+  static const hipError_t ready = allow_lds(score_fwd_kernel<HD, NT, KS, CAP>, lds_bytes);
+  if (ready != hipSuccess) return ready;
+  const int64_t n = slots(c.a, block_q<NT, KS>()), grid = n * c.a.h;
+  c.tiles = c.a.seq_start ? 0 : (int)(n / c.a.n_seq);
+  c.fold = (NT == NARROW || KS == 4 || HD == 64) && c.a.causal && grid <= RESIDENT;
+  hipLaunchKernelGGL((score_fwd_kernel<HD, NT, KS, CAP>), dim3((unsigned)grid), dim3(NT), lds_bytes, s, c);
+  return hipGetLastError();
+}
+template <int HD, bool CAP>
+hipError_t fwd_t(const ScoreCall& c, int width, hipStream_t s) {
+  switch (fwd_shape(c.a, width)) {
+    case SHAPE_WIDE: return fwd_launch<HD, WIDE, 1, CAP>(c, s);
+    case SHAPE_NARROW: return fwd_launch<HD, NARROW, 1, CAP>(c, s);
+    case SHAPE_SPLIT: return fwd_launch<HD, NARROW, 2, CAP>(c, s);
+    default: return fwd_launch<HD, WIDE, 4, CAP>(c, s);
+  }
+}
+
+template <int HD, int NT, int KS, bool CAP>
+hipError_t dq_launch(ScoreCall c, hipStream_t s) {
+  constexpr size_t lds_bytes = fwd_lds<HD, KS>();
+  static const hipError_t ready = allow_lds(score_dq_kernel<HD, NT, KS, CAP>, lds_bytes);
+  if (ready != hipSuccess) return ready;
+  const int64_t n = slots(c.a, block_q<NT, KS>()), grid = n * c.a.h;
+  c.tiles = c.a.seq_start ? 0 : (int)(n / c.a.n_seq);
+  c.fold = NT == NARROW && c.a.causal && grid <= RESIDENT;
+  hipLaunchKernelGGL((score_dq_kernel<HD, NT, KS, CAP>), dim3((unsigned)grid), dim3(NT), lds_bytes, s, c);
+  return hipGetLastError();
+}
+hipError_t reduce_launch(const ScoreCall& c, hipStream_t s) {
+  const int64_t pieces = (int64_t)c.a.rows * (2 * c.a.hkv * c.a.hd / 4);
+  hipLaunchKernelGGL(score_dkv_reduce_kernel, dim3((unsigned)((pieces + 255) / 256)), dim3(256), 0, s, c);
+  return hipGetLastError();
+}
+template <int HD, int TQ, int QS, bool CAP>
+hipError_t dkv_launch(ScoreCall c, hipStream_t s) {
+  constexpr size_t lds_bytes = dkv_lds<HD, TQ, QS>();
+  static const hipError_t ready = allow_lds(score_dkv_kernel<HD, TQ, QS, CAP>, lds_bytes);
+  if (ready != hipSuccess) return ready;
+  c.nsplit = dkv_splits(c.a, TQ);
+  const int64_t n = slots(c.a, TQ), grid = n * c.a.hkv * c.nsplit;
+  c.tiles = c.a.seq_start ? 0 : (int)(n / c.a.n_seq);
+  c.fold = TQ == KEYS_SMALL && c.a.causal && grid <= RESIDENT;
+  hipLaunchKernelGGL((score_dkv_kernel<HD, TQ, QS, CAP>), dim3((unsigned)grid), dim3(TQ * 4 * QS), lds_bytes, s, c);
+  return c.nsplit > 1 ? reduce_launch(c, s) : hipGetLastError();
+}
+template <int HD, int KS, int QS, bool CAP>
+hipError_t bwd_fused_launch(ScoreCall c, hipStream_t s) {
+  constexpr size_t dq_bytes = fwd_lds<HD, KS>(), dkv_bytes = dkv_lds<HD, KEYS_SMALL, QS>(), lds_bytes = dq_bytes > dkv_bytes ? dq_bytes : dkv_bytes;
+  static const hipError_t ready = allow_lds(score_bwd_kernel<HD, KS, QS, CAP>, lds_bytes);
+  if (ready != hipSuccess) return ready;
+  c.nsplit = dkv_splits(c.a, KEYS_SMALL);
+  const int64_t n = slots(c.a, 64), n_dkv = n * c.a.hkv * c.nsplit, grid = n_dkv + n * c.a.h;
+  c.tiles = c.a.seq_start ? 0 : (int)(n / c.a.n_seq);
+  hipLaunchKernelGGL((score_bwd_kernel<HD, KS, QS, CAP>), dim3((unsigned)grid), dim3(256 * QS), lds_bytes, s, c, (int)n_dkv);
+  return c.nsplit > 1 ? reduce_launch(c, s) : hipGetLastError();
+}
+template <int HD, bool CAP>
+hipError_t bwd_t(const ScoreCall& c, int width, hipStream_t s) {
+  const ScoreArgs& a = c.a;
+  const int64_t n64 = slots(a, 64), n_dkv = n64 * a.hkv * dkv_splits(a, KEYS_SMALL), total = n64 * a.h + n_dkv;
+  const int len = a.rows / a.n_seq;
+  if (width == 6 || (width == 0 && (2 * total <= RESIDENT || (a.causal && total <= RESIDENT && len > 320)))) return bwd_fused_launch<HD, 4, 2, CAP>(c, s);
+  if (width == 5 || (width == 0 && (HD == 128 ? a.causal && len <= 320 && total <= RESIDENT : total <= (len > 128 ? 960 : 768)))) return bwd_fused_launch<HD, 2, 1, CAP>(c, s);
+  hipError_t e;      // dQ first: it also leaves delta in the scratch for the dK/dV pass
+  switch (fwd_shape(a, width)) {
+    case SHAPE_WIDE: e = dq_launch<HD, WIDE, 1, CAP>(c, s); break;
+    case SHAPE_NARROW: e = dq_launch<HD, NARROW, 1, CAP>(c, s); break;
+    default: e = dq_launch<HD, NARROW, 2, CAP>(c, s); break;
+  }
+  if (e != hipSuccess) return e;
+  if (!dkv_small(a, width)) return dkv_launch<HD, KEYS, 1, CAP>(c, s);
+  const bool two = width ? width == 4 : len > 320 && n_dkv <= (HD == 64 ? RESIDENT : RESIDENT / 2);
+  return two ? dkv_launch<HD, KEYS_SMALL, 2, CAP>(c, s) : dkv_launch<HD, KEYS_SMALL, 1, CAP>(c, s);
+}
+
+bool rows_ok(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && ld < (1 << 23); }
+
+}  // namespace
+
+// the backward's fp32 shares of dK | dV, behind delta in the scratch; sized for either tile of the dK/dV kernel
+size_t score_part_bytes(const ScoreArgs& a) {
+  const int n128 = dkv_splits(a, KEYS), n64 = dkv_splits(a, KEYS_SMALL), ns = n128 > n64 ? n128 : n64;
+  return ns > 1 ? (size_t)ns * a.rows * 2 * a.hkv * a.hd * sizeof(float) : 0;
+}
+
+// (strides below 2^23: a tile of 128 rows has to lie within the 2 GiB that a load's offset reaches)
+bool score_mfma_supported(const ScoreArgs& a) {
+  if (!rows_ok(a.q, a.ldq) || !rows_ok(a.k, a.ldk) || !rows_ok(a.v, a.ldv) || !rows_ok(a.o, a.ldo)) return false;
+  if (a.dout && (!rows_ok(a.dout, a.lddo) || !rows_ok(a.dq, a.lddq) || !rows_ok(a.dk, a.lddk) || !rows_ok(a.dv, a.lddv))) return false;
+  return slots(a, 64) * 2 * a.h * 512 < ((int64_t)1 << 32);         // threads of a grid
+}
+hipError_t score_fwd_mfma(const ScoreArgs& a, int width, hipStream_t s) {
+  const ScoreCall c = score_call(a);
+  if (a.cap > 0.f) return a.hd == 128 ? fwd_t<128, true>(c, width, s) : fwd_t<64, true>(c, width, s);
+  return a.hd == 128 ? fwd_t<128, false>(c, width, s) : fwd_t<64, false>(c, width, s);
+}
+hipError_t score_bwd_mfma(const ScoreArgs& a, float* part, int width, hipStream_t s) {
+  ScoreCall c = score_call(a);
+  c.part = part;
+  if (a.cap > 0.f) return a.hd == 128 ? bwd_t<128, true>(c, width, s) : bwd_t<64, true>(c, width, s);
+  return a.hd == 128 ? bwd_t<128, false>(c, width, s) : bwd_t<64, false>(c, width, s);
+}
+
+}  // namespace stg

@@ -1200,12 +1200,17 @@ int stage_kernel_score_attention_fwd(const stage_score_attention_t* p, const voi
   const int64_t d = (int64_t)a.h * a.hd, dkv = (int64_t)a.hkv * a.hd;
   if (ldq < d || ldk < dkv || ldv < dkv || ldo < d) return STAGE_E_INVAL;
   a.q = q; a.ldq = ldq; a.k = k; a.ldk = ldk; a.v = v; a.ldv = ldv; a.o = o; a.ldo = ldo; a.lse = lse;
+  const int width = kernel_set >= 2 && kernel_set <= 7 ? kernel_set - 1 : 0;
+  if (kernel_set != 1 && p->dtype == STAGE_DTYPE_BF16 && score_mfma_supported(a)) return hip_rc(score_fwd_mfma(a, width, (hipStream_t)hip_stream));
   return hip_rc(score_fwd_ref((DType)p->dtype, a, (hipStream_t)hip_stream));
 }
 
+// delta, then the tuned kernels' shares of dK and dV
+static size_t score_delta_bytes(const ScoreArgs& a) { return ((size_t)a.h * a.rows * sizeof(float) + 15) / 16 * 16; }
 size_t stage_kernel_score_attention_bwd_scratch_bytes(const stage_score_attention_t* p) {
   ScoreArgs a;
-  return score_args(p, &a) ? ((size_t)a.h * a.rows * sizeof(float) + 15) / 16 * 16 : 0;
+  if (!score_args(p, &a)) return 0;
+  return score_delta_bytes(a) + (p->dtype == STAGE_DTYPE_BF16 ? score_part_bytes(a) : 0);
 }
 
 int stage_kernel_score_attention_bwd(const stage_score_attention_t* p, const void* q, int64_t ldq, const void* k, int64_t ldk,
@@ -1220,6 +1225,9 @@ int stage_kernel_score_attention_bwd(const stage_score_attention_t* p, const voi
   if (ldq < d || ldk < dkv || ldv < dkv || ldo < d || lddo < d || lddq < d || lddk < dkv || lddv < dkv) return STAGE_E_INVAL;
   a.q = q; a.ldq = ldq; a.k = k; a.ldk = ldk; a.v = v; a.ldv = ldv; a.o = (void*)o; a.ldo = ldo; a.lse = (float*)lse;
   a.dout = dout; a.lddo = lddo; a.dq = dq; a.lddq = lddq; a.dk = dk; a.lddk = lddk; a.dv = dv; a.lddv = lddv; a.delta = (float*)scratch;
+  const int width = kernel_set >= 2 && kernel_set <= 7 ? kernel_set - 1 : 0;
+  if (kernel_set != 1 && p->dtype == STAGE_DTYPE_BF16 && score_mfma_supported(a))
+    return hip_rc(score_bwd_mfma(a, (float*)((char*)scratch + score_delta_bytes(a)), width, (hipStream_t)hip_stream));
   return hip_rc(score_bwd_ref((DType)p->dtype, a, (hipStream_t)hip_stream));
 }
 

@@ -22,7 +22,8 @@ def slopes(h):
 # lengths of the packed sequences, rows before the first and behind the last
 PACKED = {"one": ([1], 0, 0), "ones": ([1, 1, 1, 1, 1], 0, 2), "empty": ([0, 5, 0, 0, 70, 0], 3, 0), "tiles": ([64, 128, 32, 256], 0, 0),
           "odd": ([63, 65, 129, 1, 31, 33], 2, 5), "long": ([3, 610], 0, 1)}
-KERNELS = [("fp32", 1), ("bf16", 1)]
+# 0: by the shape, 1: the plain kernels; the others fix the workgroup shapes, 2 .. 5 of forward, dQ and dK/dV, 6 and 7 of the one-launch backward
+KERNELS = [("fp32", 0), ("fp32", 1)] + [("bf16", n) for n in range(8)]
 
 
 @pytest.mark.parametrize("dtype,kernel_set", KERNELS)
