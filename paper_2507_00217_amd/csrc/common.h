@@ -184,6 +184,9 @@ hipError_t score_bwd_ref(DType dt, const ScoreArgs& a, hipStream_t s);
 bool score_mfma_supported(const ScoreArgs& a);
 size_t score_part_bytes(const ScoreArgs& a);
 hipError_t score_fwd_mfma(const ScoreArgs& a, int width, hipStream_t s);
+bool score32_supported(const ScoreArgs& a);          // fp32
+hipError_t score32_fwd(const ScoreArgs& a, hipStream_t s);
+hipError_t score32_bwd(const ScoreArgs& a, hipStream_t s);
 hipError_t score_bwd_mfma(const ScoreArgs& a, float* part, int width, hipStream_t s);
 
 // tuned gfx950 kernels (bf16 MFMA)

@@ -1202,6 +1202,7 @@ int stage_kernel_score_attention_fwd(const stage_score_attention_t* p, const voi
   a.q = q; a.ldq = ldq; a.k = k; a.ldk = ldk; a.v = v; a.ldv = ldv; a.o = o; a.ldo = ldo; a.lse = lse;
   const int width = kernel_set >= 2 && kernel_set <= 7 ? kernel_set - 1 : 0;
   if (kernel_set != 1 && p->dtype == STAGE_DTYPE_BF16 && score_mfma_supported(a)) return hip_rc(score_fwd_mfma(a, width, (hipStream_t)hip_stream));
+  if (kernel_set != 1 && p->dtype == STAGE_DTYPE_FP32 && score32_supported(a)) return hip_rc(score32_fwd(a, (hipStream_t)hip_stream));
   return hip_rc(score_fwd_ref((DType)p->dtype, a, (hipStream_t)hip_stream));
 }
 
@@ -1228,6 +1229,7 @@ int stage_kernel_score_attention_bwd(const stage_score_attention_t* p, const voi
   const int width = kernel_set >= 2 && kernel_set <= 7 ? kernel_set - 1 : 0;
   if (kernel_set != 1 && p->dtype == STAGE_DTYPE_BF16 && score_mfma_supported(a))
     return hip_rc(score_bwd_mfma(a, (float*)((char*)scratch + score_delta_bytes(a)), width, (hipStream_t)hip_stream));
+  if (kernel_set != 1 && p->dtype == STAGE_DTYPE_FP32 && score32_supported(a)) return hip_rc(score32_bwd(a, (hipStream_t)hip_stream));
   return hip_rc(score_bwd_ref((DType)p->dtype, a, (hipStream_t)hip_stream));
 }
 
