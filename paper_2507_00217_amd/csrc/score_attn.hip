@@ -24,8 +24,9 @@ struct ScoreCall {
   float sl2;                     // scale * log2 e
   float raw;                     // 1 / scale: a bias in units of the plain product
   // cap: of the product x itself, s = c2 tanh(x scale / cap), c2 = cap log2 e
-  float c2, ic2, kx, small;      // kx = 2 log2 e scale / cap; |x| <= small: tanh by its polynomial
-  float poly[5];                 // s = x (poly[0] + x^2 (poly[1] + ...)) there
+  float c2, ic2, kx;             // kx = 2 log2 e scale / cap
+  float small, middling;         // |x| up to which the polynomials hold: s = x (sl2 + x^2 (p[0] + x^2 ...))
+  float p3[2], p5[4];
   int tiles;                     // tiles of a sequence (equal sequences)
   int fold, nsplit;
   float* part;                   // [nsplit][rows][2 * hkv * hd] fp32
@@ -34,18 +35,60 @@ struct ScoreCall {
 // ---- where a workgroup works ------------------------------------------------------------------------------------------------
 struct Work { int lo, len, prefix, t; };       // rows of its sequence, its prefix, its tile; len = 0: nothing to do
 
-// QUERIES: tiles are taken from the last on (causal: the heaviest first), keys from the first on.
+// Sums over the lanes up to this one, by moves between lanes inside the instruction: rows of 16, then their ends into the rows behind.
+template <int CTRL, int ROWS> __device__ __forceinline__ int dpp_add(int v) {
+  return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int scan_add(int v) {
+  v = dpp_add<0x111, 0xf>(v);
+  v = dpp_add<0x112, 0xf>(v);
+  v = dpp_add<0x114, 0xf>(v);
+  v = dpp_add<0x118, 0xf>(v);
+  v = dpp_add<0x142, 0xa>(v);
+  return dpp_add<0x143, 0xc>(v);
+}
+
+// The workgroup of rank `rank`: equal sequences and up to 64 packed ones get theirs heaviest tiles first (QUERIES: the more keys, the
+// heavier; else tiles of keys: the more queries).  Heaviness is counted in tiles.  Of a packed sequence of nt tiles, tiles of queries
+// weigh their number, but those within the prefix as much as its last; tiles of keys nt - 1 minus their number, but those of the prefix
+// nt - 1; without a causal mask all weigh the same.  The level that the rank falls into is searched for with the count of
+// tiles of at least a weight, one sequence to a lane.
 template <int BQ, bool QUERIES>
 __device__ __forceinline__ Work find_work(const ScoreCall& c, int rank, int lane) {
   const ScoreArgs& a = c.a;
+  Work w;
+  if (a.seq_start && a.n_seq <= 64) {
+    const SeqSpan s = seq_span(a, min(lane, a.n_seq - 1));
+    const int len = lane < a.n_seq ? s.hi - s.lo : 0, nt = (len + BQ - 1) / BQ;
+    // tiles 0 .. flat - 1 weigh `top`; QUERIES: tile t >= flat weighs t (more), else nt - 1 - t (less)
+    const int inside = (s.prefix + BQ - 1) / BQ;
+    const int flat = a.causal ? max(min(inside, nt), min(nt, 1)) : nt, top = QUERIES ? flat - 1 : nt - 1;
+    auto heavier = [&](int x) { return QUERIES ? (x <= top ? nt : max(nt - x, 0)) : (x <= top ? flat + max(nt - flat - x, 0) : 0); };   // tiles of weight >= x
+    auto total = [&](int x) { return __builtin_amdgcn_readlane(scan_add(heavier(x)), 63); };
+    if (rank >= total(0)) { w.lo = w.len = w.prefix = w.t = 0; return w; }
+    int lo = 0, hi = 1 + a.rows / BQ;                  // total(lo) > rank >= total(hi)
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (total(mid) > rank) lo = mid;
+      else hi = mid;
+    }
+    const int k = rank - total(lo + 1), n = heavier(lo) - heavier(lo + 1), upto = scan_add(n);
+    const int i = __builtin_ctzll(__ballot(upto > k));
+    w.lo = __builtin_amdgcn_readlane(s.lo, i);
+    w.len = __builtin_amdgcn_readlane(len, i);
+    w.prefix = __builtin_amdgcn_readlane(s.prefix, i);
+    const int nth = k - __builtin_amdgcn_readlane(upto - n, i);
+    w.t = lo == __builtin_amdgcn_readlane(top, i) ? nth : QUERIES ? lo : __builtin_amdgcn_readlane(nt, i) - 1 - lo;
+    return w;
+  }
   int i, t;
   if (!a.seq_start) {
     i = rank % a.n_seq;
     t = QUERIES ? tile_of_rank(rank / a.n_seq, c.tiles, c.fold) : key_tile_of_rank(rank / a.n_seq, c.tiles, c.fold);
-  } else {
+  } else {                                             // more sequences: the slots, last rows first for queries
     const int u = QUERIES ? a.rows / BQ + a.n_seq - 1 - rank : rank;
     i = 0;
-    for (int n = a.n_seq; n > 1;) {            // sequences i .. i + n - 1 are left; 64 of them are looked at
+    for (int n = a.n_seq; n > 1;) {                    // sequences i .. i + n - 1 are left; 64 of them are looked at
       const int step = (n + 63) >> 6, at = lane * step;
       const bool before = at < n && min(max(a.seq_start[i + min(at, n - 1)], 0), a.rows) / BQ + i + at <= u;
       const int k = max(__popcll(__ballot(before)) - 1, 0) * step;
@@ -56,7 +99,6 @@ __device__ __forceinline__ Work find_work(const ScoreCall& c, int rank, int lane
     t = u - (min(max(a.seq_start[i], 0), a.rows) / BQ + i);
   }
   const SeqSpan s = seq_span(a, i);
-  Work w;
   w.lo = __builtin_amdgcn_readfirstlane(s.lo);
   w.t = __builtin_amdgcn_readfirstlane(t);
   const int len = __builtin_amdgcn_readfirstlane(s.hi - s.lo);
@@ -92,22 +134,29 @@ struct Loader {
 };
 
 // ---- scores -----------------------------------------------------------------------------------------------------------------
-// 16 products x -> capped scores in units of log 2.  tanh(y) / y is a polynomial in y^2 up to |y| = 0.6 (fitted by least squares of the
-// relative error, 7e-8 at most), which is where scores lie that are not pressed against the cap; a block with any larger one takes
-// 1 - 2 / (exp(2 y) + 1), whose two transcendental instructions each cost as much as four others.
+// 16 products x -> capped scores in units of log 2.  Scores that are not pressed against the cap, |y| <= 0.25 or 0.6 with y = x scale / cap, take
+// tanh(y) = y (1 + y^2 (a1 + ...)) with two or four coefficients (fitted by least squares; tanh is off by 8e-8 and 3e-8 at most, less
+// than the rounding of a score of 10), a block with any larger one 1 - 2 / (exp(2 y) + 1), whose two transcendental instructions each
+// cost as much as four others.
 __device__ __forceinline__ void cap_block(f32x16& x, const ScoreCall& c) {
   float mx = 0.f;
 #pragma unroll
   for (int e = 0; e < 16; ++e) mx = fmaxf(mx, fabsf(x[e]));
-  if (__any(mx > c.small)) {
-#pragma unroll
-    for (int e = 0; e < 16; ++e) x[e] = fmaf(__builtin_amdgcn_rcpf(fast_exp2(x[e] * c.kx) + 1.f), -2.f * c.c2, c.c2);
-  } else {
+  if (!__any(mx > c.small)) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       const float y = x[e] * x[e];
-      x[e] *= fmaf(y, fmaf(y, fmaf(y, fmaf(y, c.poly[4], c.poly[3]), c.poly[2]), c.poly[1]), c.poly[0]);
+      x[e] *= fmaf(y, fmaf(y, c.p3[1], c.p3[0]), c.sl2);
     }
+  } else if (!__any(mx > c.middling)) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float y = x[e] * x[e];
+      x[e] *= fmaf(y, fmaf(y, fmaf(y, fmaf(y, c.p5[3], c.p5[2]), c.p5[1]), c.p5[0]), c.sl2);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = fmaf(__builtin_amdgcn_rcpf(fast_exp2(x[e] * c.kx) + 1.f), -2.f * c.c2, c.c2);
   }
 }
 
@@ -903,14 +952,19 @@ ScoreCall score_call(const ScoreArgs& a) {
   c.raw = 1.f / a.scale;
   c.nsplit = 1;
   if (a.cap > 0.f) {
-    static const double p[5] = {0.999999926868628, -0.3333230997148176, 0.13310173617653454, -0.052101478331093104, 0.015475425016233654};
+    static const double p3[2] = {-0.33322914994946595, 0.12846042911412406};
+    static const double p5[4] = {-0.33332247985930596, 0.13308098290393836, -0.05199433652233533, 0.015319205699263892};
     const double r = (double)a.scale / a.cap, c2 = (double)a.cap * 1.4426950408889634;
     c.c2 = (float)c2;
     c.ic2 = (float)(1.0 / c2);
     c.kx = (float)(2.0 * 1.4426950408889634 * r);
-    c.small = (float)(0.6 / r);
-    double f = c2 * r;
-    for (int i = 0; i < 5; ++i, f *= r * r) c.poly[i] = (float)(p[i] * f);
+    c.small = (float)(0.25 / r);
+    c.middling = (float)(0.6 / r);
+    double f = c2 * r * r * r;
+    for (int i = 0; i < 4; ++i, f *= r * r) {
+      if (i < 2) c.p3[i] = (float)(p3[i] * f);
+      c.p5[i] = (float)(p5[i] * f);
+    }
   }
   return c;
 }
