@@ -83,7 +83,7 @@ struct ScoreArgs {
 constexpr int ROPE_MAX_PAIRS = 64;
 struct RotateArgs {
   double turn[ROPE_MAX_PAIRS];   // frequency of every pair, in turns per position
-  int axis[ROPE_MAX_PAIRS];      // its axis
+  unsigned char axis[ROPE_MAX_PAIRS];      // its axis
   int halves;                    // pairs (p, p + hd / 2) instead of (2p, 2p + 1)
   const int* pos; int64_t pos_stride;      // [axes][pos_stride], or null: no rotation
 };
@@ -96,7 +96,7 @@ struct HeadNormArgs {
   float* rstd;                   // [rows, h + hkv] (forward: or null)
   const void* dy; int64_t lddy;  // backward only
   float* dgq; float* dgk;        // fp32, added to
-  float* partial;                // [HEAD_NORM_PARTS][2][hd]
+  float* partial;                // head_norm_partial_bytes(hd) bytes
 };
 
 struct NormArgs {

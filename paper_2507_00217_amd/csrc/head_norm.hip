@@ -17,7 +17,7 @@ namespace stg {
 namespace {
 
 constexpr int WAVES = 4, NT = WAVES * 64;
-constexpr int PARTS = 512;             // workgroups of the backward, each of which leaves one row of partial sums
+constexpr int PARTS = 1024;            // workgroups of the backward, each of which leaves one row of partial sums
 
 template <typename T> constexpr int vec() { return 16 / (int)sizeof(T); }
 
@@ -88,8 +88,7 @@ __device__ __forceinline__ void lane_turns(const RotateArgs& r, int c, double (&
 
 // Forward, or (without the norm) the rotation alone.  A wavefront's share is U steps of 64 / LPH heads of one row, all of whose
 // loads are in flight together.
-constexpr int U = 4;
-template <typename T, int HD, bool HALVES, bool NORM>
+template <typename T, int HD, bool HALVES, bool NORM, int U>
 __global__ __launch_bounds__(NT) void head_rotate_kernel(HeadNormArgs n, RotateArgs r, int chunks) {
   using P = Pairs<T, HD, HALVES>;
   constexpr int N = P::N, LPH = HD / vec<T>(), HPW = 64 / LPH;
@@ -101,7 +100,8 @@ __global__ __launch_bounds__(NT) void head_rotate_kernel(HeadNormArgs n, RotateA
   T* y = (T*)n.y + (int64_t)row * n.ldy;
   P v[U];
 #pragma unroll
-  for (int u = 0; u < U; ++u) v[u].load(x + (int64_t)min(h0 + u * HPW, heads - 1) * HD, c);
+  for (int u = 0; u < U; ++u)
+    v[u].load(x + (int64_t)min(h0 + u * HPW, heads - 1) * HD, c);
   float cs[N], sn[N];
   if (r.pos) {
     double turn[N];
@@ -224,13 +224,37 @@ __global__ __launch_bounds__(NT) void head_norm_bwd_kernel(HeadNormArgs n, Rotat
   }
 }
 
+// Of the share sizes that there are, the one with the fewest steps to no purpose, of those the largest (sine and cosine are computed
+// once for a share), but none that leaves fewer than 16 wavefronts to a compute unit.
+int steps_of_share(int steps, int rows) {
+  int best = 1;
+  for (const int u : {2, 3, 4, 5, 8}) {
+    const int chunks = (steps + u - 1) / u, was = (steps + best - 1) / best * best;
+    if ((int64_t)rows * chunks >= 4096 && chunks * u <= was) best = u;
+  }
+  return best;
+}
+
 template <typename T, int HD, bool HALVES, bool NORM>
 hipError_t rotate_launch(const HeadNormArgs& n, const RotateArgs& r, hipStream_t s) {
   constexpr int HPW = 64 * vec<T>() / HD;
-  const int chunks = (n.h + n.hkv + U * HPW - 1) / (U * HPW);
-  const int64_t units = (int64_t)n.rows * chunks;
-  hipLaunchKernelGGL((head_rotate_kernel<T, HD, HALVES, NORM>), dim3((unsigned)((units + WAVES - 1) / WAVES)), dim3(NT), 0, s, n, r, chunks);
-  return hipGetLastError();
+  const int steps = (n.h + n.hkv + HPW - 1) / HPW;
+  auto launch = [&](auto u) {
+    constexpr int U = decltype(u)::value;
+    const int chunks = (steps + U - 1) / U;
+    const int64_t units = (int64_t)n.rows * chunks;
+    hipLaunchKernelGGL((head_rotate_kernel<T, HD, HALVES, NORM, U>), dim3((unsigned)((units + WAVES - 1) / WAVES)), dim3(NT), 0, s, n, r, chunks);
+    return hipGetLastError();
+  };
+  using std::integral_constant;
+  switch (steps_of_share(steps, n.rows)) {
+    case 1: return launch(integral_constant<int, 1>{});
+    case 2: return launch(integral_constant<int, 2>{});
+    case 3: return launch(integral_constant<int, 3>{});
+    case 5: return launch(integral_constant<int, 5>{});
+    case 8: return launch(integral_constant<int, 8>{});
+    default: return launch(integral_constant<int, 4>{});
+  }
 }
 template <typename T, int HD, bool HALVES>
 hipError_t bwd_launch(const HeadNormArgs& n, const RotateArgs& r, hipStream_t s) {

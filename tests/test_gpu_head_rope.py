@@ -145,3 +145,42 @@ def test_qk_norm_rope(dtype, hd, halves, n_axes, rows, h, hkv):
     assert fwd(xd, False) == 0
     torch.cuda.synchronize()
     assert torch.equal(xd[:, :n], y[:, :n]) and bool(torch.isnan(xd[:, n:].float()).all())
+
+
+@pytest.mark.parametrize("dtype,hd,per_step", [("fp32", 128, 2), ("fp32", 64, 4), ("bf16", 128, 4), ("bf16", 64, 8)])
+@pytest.mark.parametrize("steps", [1, 2, 3, 4, 5, 6, 7, 8, 9, 11])
+def test_shares_of_a_row_agree_bitwise(dtype, hd, per_step, steps):
+    """With rows enough to fill the chip a wavefront takes several steps of a row's heads (a row is `steps` of them, the last one cut short), with a
+    hundred rows one: the same bits either way, forward and (whose shares do not depend on the rows) backward."""
+    import torch
+    from paper_2507_00217_amd import stage as S
+    L, rows, few = S.lib(), 4103, 100
+    heads = steps * per_step - (1 if steps > 1 else 0)
+    h, hkv = max(1, heads - 1 - steps // 3), heads - max(1, heads - 1 - steps // 3)
+    n, g = heads * hd, torch.Generator(device="cuda:0").manual_seed(7)
+    td = torch.float32 if dtype == "fp32" else torch.bfloat16
+    x, dy = (torch.randn(rows, n, generator=g, device="cuda:0").to(td) for _ in range(2))
+    gam = (1 + 0.1 * torch.randn(2, hd, generator=g, device="cuda:0")).to(td)
+    axes, keep, _ = axes_of(2, hd, rows, 1e4, steps % 2, 0)
+    part = torch.empty(L.stage_kernel_qk_norm_rope_partial_bytes(hd), dtype=torch.uint8, device="cuda:0")
+
+    def run(r):
+        y, z, dx = (torch.full((r, n), float("nan"), device="cuda:0").to(td) for _ in range(3))
+        rstd, dg = torch.full((r, heads), float("nan"), device="cuda:0"), torch.zeros(2, hd, device="cuda:0")
+        assert L.stage_kernel_qk_norm_rope_fwd(DT[dtype], r, h, hkv, hd, 1e-5, C.byref(axes), ptr(x), n, ptr(gam[0]), ptr(gam[1]), ptr(y), n, ptr(rstd), None) == 0
+        assert L.stage_kernel_rope_axes(DT[dtype], r, heads, hd, C.byref(axes), 1, ptr(x), n, ptr(z), n, None) == 0
+        assert L.stage_kernel_qk_norm_rope_bwd(DT[dtype], r, h, hkv, hd, C.byref(axes), ptr(x), n, ptr(rstd), ptr(gam[0]), ptr(gam[1]), ptr(dy), n, ptr(dx), n,
+                                               ptr(dg[0]), ptr(dg[1]), ptr(part), None) == 0
+        torch.cuda.synchronize()
+        return y, z, rstd, dx, dg
+    many, short = run(rows), run(few)
+    for a, b in zip(many[:4], short[:4]):
+        assert bool(torch.isfinite(a.float()).all()) and torch.equal(a[:few], b)
+    # the weights' gradients of all rows, from the kernel's own rstd, in 64 bits
+    f = lambda t: t.double().cpu().numpy()
+    ang = sc.rope_angles(keep.cpu().numpy()[:, :rows], SECTIONS[(2, hd)], hd, np.float32(1e4), 0)
+    gr = sc.rotate(f(dy), ang, hd, steps % 2, True)
+    _, dgq, dgk = sc.qk_norm_backward(f(x), f(many[2]), f(gam[0]), f(gam[1]), h, hkv, gr)
+    terms = (pair_length(gr, hd, steps % 2).reshape(rows, heads, hd) * (np.abs(f(x)).reshape(rows, heads, hd) * f(many[2])[..., None])).sum(0)
+    close("dgq", to_np(many[4][0]), dgq, F[dtype] * terms[:h].sum(0))
+    close("dgk", to_np(many[4][1]), dgk, F[dtype] * terms[h:].sum(0))
