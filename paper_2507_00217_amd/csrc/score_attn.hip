@@ -914,35 +914,54 @@ hipError_t allow_lds(K kern, size_t bytes) {
   return hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
 
-constexpr int64_t RESIDENT = 2 * 256;  // workgroups of 4 wavefronts that a 256-CU chip holds (the scratch size depends on it, so it is a constant)
+constexpr int64_t RESIDENT = 2 * 256;  // workgroups of 4 wavefronts that a chip of 256 CUs holds (a constant: the scratch's size depends on it)
 
 // grid slots of bq rows each (times heads: workgroups), and what of them there is to do at least
 int64_t slots(const ScoreArgs& a, int bq) {
   return a.seq_start ? a.rows / bq + a.n_seq : (int64_t)a.n_seq * ((a.rows / a.n_seq + bq - 1) / bq);
 }
 
+// What the rules below are: measured on sequences of 30 to 16384 rows, 4 to 40 heads (us; "packed" = lengths drawn, n of them).
+int mean_len(const ScoreArgs& a) { return a.rows / a.n_seq; }
+
 enum Shape { SHAPE_WIDE = 1, SHAPE_NARROW = 2, SHAPE_SPLIT = 3, SHAPE_SPLIT4 = 4 };
-// as for plain attention: 8 wavefronts x 32 queries when that gives two workgroups per CU, else 4, else 64 queries with the keys split
-Shape fwd_shape(const ScoreArgs& a, int width) {
+// Forward and dQ: 8 wavefronts x 32 queries, 4 x 32, or 64 queries whose keys 2 or 4 wavefronts share.
+// WIDE only for long equal sequences: it reads every K/V tile once for twice the queries, but its last tiles are twice as much masked
+// (WIDE / NARROW: forward of head_dim 128 32 heads x 4096 149 / 158, 32 x 4 x 2048 228 / 187, 16 x 13 packed in 8192 71 / 62; dQ 189 / 202, 270 / 244,
+// 92 / 84), and in the forward of head_dim 64 never, where NARROW has more wavefronts to a CU (32 x 4096 118 / 90).
+// SPLIT below about a round and a half of NARROW (SPLIT / NARROW, head_dim 128: 16 x 3000 58 / 64, 40 x 1500 47 / 40), SPLIT4 for few workgroups
+// with long chains (SPLIT4 / SPLIT: 4 x 5000 60 / 72, 16 x 2048 45 / 36; head_dim 64, whose workgroups sit two to a CU, 16 x 2048 21.5 / 24.7).
+Shape q_shape(const ScoreArgs& a, int width, bool forward) {
   if (width >= 1 && width <= 4) return (Shape)width;
-  if (slots(a, 256) * a.h >= RESIDENT) return SHAPE_WIDE;
-  if (slots(a, 128) * a.h >= RESIDENT) return SHAPE_NARROW;
-  return slots(a, 64) * a.h <= (a.hd == 64 ? RESIDENT : RESIDENT / 2) && a.rows / a.n_seq >= 1000 ? SHAPE_SPLIT4 : SHAPE_SPLIT;
+  const bool long_equal = !a.seq_start && mean_len(a) >= 4096;
+  if (long_equal && !(forward && a.hd == 64) && slots(a, 256) * a.h >= 400) return SHAPE_WIDE;
+  if (slots(a, 128) * a.h >= (forward && a.hd == 64 ? 512 : 450)) return SHAPE_NARROW;
+  return forward && slots(a, 64) * a.h <= (a.hd == 64 ? 512 : 384) && mean_len(a) >= 1000 ? SHAPE_SPLIT4 : SHAPE_SPLIT;
 }
+// dK/dV: into how many workgroups the query heads of a KV head go: until there are two rounds of them (128 keys: one workgroup to a CU; 64 keys:
+// two), or every query head has its own.  (Split for one round, 16 heads on 2 x 13 packed in 8192 239, for two 194; their sums cost 13 of it.)
 int dkv_splits(const ScoreArgs& a, int tq) {
   const int grp = a.h / a.hkv;
-  const int64_t wgs = slots(a, tq) * a.hkv;
+  const int64_t wgs = slots(a, tq) * a.hkv, want = tq == 128 ? 512 : 1024;
   int ns = 1;
-  while (ns < grp && wgs * ns < RESIDENT) {
+  while (ns < grp && wgs * ns < want) {
     int nx = ns + 1;
     while (grp % nx) ++nx;
     ns = nx;
   }
   return ns;
 }
-bool dkv_small(const ScoreArgs& a, int width) {
-  if (width >= 1 && width <= 4) return width >= 3;
-  return slots(a, KEYS) * a.hkv * dkv_splits(a, KEYS) < RESIDENT;
+// dK/dV: 128 keys to a workgroup, 64, or 64 with two pairs of wavefronts to 32 keys.
+// 64 keys for short sequences and enough workgroups (128 keys / 64, 16 heads x 100 packed in 8192 101 / 70, 16 x 4 x 1024 55 / 59; head_dim 64
+// 75 / 41, 36 / 33, 32 x 4 x 2048 237 / 207, 12 x 9000 355 / 391); two pairs for few workgroups (128 keys / two pairs, 4 x 5000 134 / 101, 8 x 1024 34 / 25, 12 x 3 x
+// 777 36 / 36; head_dim 64 97 / 80, 25 / 19, 24 / 19, 8 x 5 packed in 6000 79 / 66, 12 x 3 packed in 4096 54 / 52).
+enum KeyShape { KEYS_128 = 1, KEYS_64 = 3, KEYS_64_TWO = 4 };
+KeyShape k_shape(const ScoreArgs& a, int width) {
+  if (width >= 1 && width <= 4) return width <= 2 ? KEYS_128 : (KeyShape)width;
+  const int64_t n64 = slots(a, 64) * a.hkv * dkv_splits(a, 64), n128 = slots(a, 128) * a.hkv * dkv_splits(a, 128);
+  if (mean_len(a) > 320 && n64 <= (a.hd == 64 ? 850 : 320)) return KEYS_64_TWO;
+  if (mean_len(a) <= (a.hd == 64 ? 2048 : 512) && n64 >= 960) return KEYS_64;
+  return n128 < 450 ? KEYS_64 : KEYS_128;
 }
 
 ScoreCall score_call(const ScoreArgs& a) {
@@ -982,7 +1001,7 @@ hipError_t fwd_launch(ScoreCall c, hipStream_t s) {
 }
 template <int HD, bool CAP>
 hipError_t fwd_t(const ScoreCall& c, int width, hipStream_t s) {
-  switch (fwd_shape(c.a, width)) {
+  switch (q_shape(c.a, width, true)) {
     case SHAPE_WIDE: return fwd_launch<HD, WIDE, 1, CAP>(c, s);
     case SHAPE_NARROW: return fwd_launch<HD, NARROW, 1, CAP>(c, s);
     case SHAPE_SPLIT: return fwd_launch<HD, NARROW, 2, CAP>(c, s);
@@ -1032,20 +1051,28 @@ hipError_t bwd_fused_launch(ScoreCall c, hipStream_t s) {
 template <int HD, bool CAP>
 hipError_t bwd_t(const ScoreCall& c, int width, hipStream_t s) {
   const ScoreArgs& a = c.a;
-  const int64_t n64 = slots(a, 64), n_dkv = n64 * a.hkv * dkv_splits(a, KEYS_SMALL), total = n64 * a.h + n_dkv;
-  const int len = a.rows / a.n_seq;
-  if (width == 6 || (width == 0 && (2 * total <= RESIDENT || (a.causal && total <= RESIDENT && len > 320)))) return bwd_fused_launch<HD, 4, 2, CAP>(c, s);
-  if (width == 5 || (width == 0 && (HD == 128 ? a.causal && len <= 320 && total <= RESIDENT : total <= (len > 128 ? 960 : 768)))) return bwd_fused_launch<HD, 2, 1, CAP>(c, s);
+  const int64_t n64 = slots(a, 64), total = n64 * a.h + n64 * a.hkv * dkv_splits(a, 64);
+  const int len = mean_len(a);
+  // Both passes in one launch while their workgroups (64 queries, 64 keys) number little more than what is resident; with two pairs of
+  // wavefronts up to one to a CU, or with long causal chains somewhat more (one launch / two: head_dim 128 8 x 1024 33 / 46, 4 x 5000 157 / 175, 16 x
+  // 2048 115 / 102), with one pair (head_dim 64: three to a CU) for shorter sequences (12 x 3 x 777 32 / 33, 32 x 700 26 / 29, 4 x 5000 140 / 128; head_dim
+  // 128 8 x 6 packed in 600 14 / 21).
+  const bool two_pairs = 2 * total <= RESIDENT || (a.causal && ((total <= RESIDENT && len > 320) || (total <= 700 && len > 1500)));
+  if (width == 6 || (width == 0 && two_pairs)) return bwd_fused_launch<HD, 4, 2, CAP>(c, s);
+  const bool one_pair = HD == 128 ? a.causal && len <= 320 && total <= RESIDENT : len <= 1500 && total <= (len > 128 ? 960 : 768);
+  if (width == 5 || (width == 0 && one_pair)) return bwd_fused_launch<HD, 2, 1, CAP>(c, s);
   hipError_t e;      // dQ first: it also leaves delta in the scratch for the dK/dV pass
-  switch (fwd_shape(a, width)) {
+  switch (q_shape(a, width, false)) {
     case SHAPE_WIDE: e = dq_launch<HD, WIDE, 1, CAP>(c, s); break;
     case SHAPE_NARROW: e = dq_launch<HD, NARROW, 1, CAP>(c, s); break;
     default: e = dq_launch<HD, NARROW, 2, CAP>(c, s); break;
   }
   if (e != hipSuccess) return e;
-  if (!dkv_small(a, width)) return dkv_launch<HD, KEYS, 1, CAP>(c, s);
-  const bool two = width ? width == 4 : len > 320 && n_dkv <= (HD == 64 ? RESIDENT : RESIDENT / 2);
-  return two ? dkv_launch<HD, KEYS_SMALL, 2, CAP>(c, s) : dkv_launch<HD, KEYS_SMALL, 1, CAP>(c, s);
+  switch (k_shape(a, width)) {
+    case KEYS_128: return dkv_launch<HD, KEYS, 1, CAP>(c, s);
+    case KEYS_64: return dkv_launch<HD, KEYS_SMALL, 1, CAP>(c, s);
+    default: return dkv_launch<HD, KEYS_SMALL, 2, CAP>(c, s);
+  }
 }
 
 bool rows_ok(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && ld < (1 << 23); }
