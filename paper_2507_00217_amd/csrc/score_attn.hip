@@ -398,7 +398,7 @@ __global__ __launch_bounds__(NT, KS == 4 && HD == 64 ? 4 : 2) void score_fwd_ker
 // ---- dQ ---------------------------------------------------------------------------------------------------------------------
 template <int HD, int BUF, bool CAP>
 __device__ __forceinline__ void dq_block(lds_char* lds, const FragOff<HD>& fo, const ScoreCall& c, const bf16x8 (&qf)[HD / 16], const bf16x8 (&dof)[HD / 16],
-                                         f32x16 (&dq)[HD / 32], int n, int kv0, Row row, int hf, float slope2, float lse2, const f32x16& ndl,
+                                         f32x16 (&dq)[HD / 32], int n, int kv0, Row row, int hf, float slope2, float lse2, float dl, const f32x16& ndl,
                                          bool need_mask, bool ahead) {
   using G = Geo<HD>;
   constexpr int KT = BUF, VT = BUF + G::TILEB, AHEAD = 3, NDQ = G::NHB * 2, VA = 4;
@@ -412,7 +412,7 @@ __device__ __forceinline__ void dq_block(lds_char* lds, const FragOff<HD>& fo, c
       kf[(kk + AHEAD) % (AHEAD + 1)][0] = frag_rows<HD>(lds, fo, KT, n * 32, kk + AHEAD);
       kf[(kk + AHEAD) % (AHEAD + 1)][1] = frag_rows<HD>(lds, fo, VT, n * 32, kk + AHEAD);
     }
-    if (kk == 0) { s = mfma0(kf[0][0], qf[0]); dp = MFMA(kf[0][1], dof[0], ndl); }
+    if (kk == 0) { s = mfma0(kf[0][0], qf[0]); dp = CAP ? mfma0(kf[0][1], dof[0]) : MFMA(kf[0][1], dof[0], ndl); }
     else {
       s = MFMA(kf[kk % (AHEAD + 1)][0], qf[kk], s);
       dp = MFMA(kf[kk % (AHEAD + 1)][1], dof[kk], dp);
@@ -428,7 +428,7 @@ __device__ __forceinline__ void dq_block(lds_char* lds, const FragOff<HD>& fo, c
 #pragma unroll
     for (int e = 0; e < 16; ++e) {               // dP - delta times the cap's derivative 1 - t^2
       const float t = s[e] * c.ic2;
-      dp[e] *= fmaf(-t, t, 1.f);
+      dp[e] = (dp[e] - dl) * fmaf(-t, t, 1.f);
     }
   }
   const float first = (float)(kv0 + n * 32 + hf * 4 - row.q), off = (c.a.slope ? slope2 * first : 0.f) - lse2;
@@ -526,7 +526,7 @@ __device__ __forceinline__ void dq_workgroup(const ScoreCall& c, lds_char* lds, 
 #pragma unroll
   for (int hb = 0; hb < G::NHB; ++hb) zero(dq[hb]);
 #pragma unroll
-  for (int e = 0; e < 16; ++e) ndl[e] = -dl;
+  for (int e = 0; e < 16; ++e) ndl[e] = -dl;           // what the dP products start at; capped, delta is subtracted behind them, for want of registers
   FragOff<HD> fo;
   fo.init(lane, lds);
   if (KS > 1) fo.hop((kh >> 1) * 2 * G::TILEB + (kh & 1) * 32 * G::ROWB);
@@ -542,7 +542,7 @@ __device__ __forceinline__ void dq_workgroup(const ScoreCall& c, lds_char* lds, 
         const int k0 = kvw + n * 32;
         if (n > 0 && k0 >= end_w) continue;            // no query of the wavefront sees this block
         const bool need_mask = (a.causal && k0 + 32 > max(q0w + 1, vis)) || k0 + 32 > w.len;
-        dq_block<HD, BUF, CAP>(lds, fo, c, qf, dof, dq, n, kvw, row, hf, slope2, lse2, ndl, need_mask, k0 + 32 > q0w + 1);
+        dq_block<HD, BUF, CAP>(lds, fo, c, qf, dof, dq, n, kvw, row, hf, slope2, lse2, dl, ndl, need_mask, k0 + 32 > q0w + 1);
       }
     }
     __builtin_amdgcn_s_waitcnt(0);
@@ -1002,7 +1002,9 @@ hipError_t fwd_launch(ScoreCall c, hipStream_t s) {
 template <int HD, bool CAP>
 hipError_t fwd_t(const ScoreCall& c, int width, hipStream_t s) {
   switch (q_shape(c.a, width, true)) {
-    case SHAPE_WIDE: return fwd_launch<HD, WIDE, 1, CAP>(c, s);
+    case SHAPE_WIDE:
+      if constexpr (HD == 128) return fwd_launch<HD, WIDE, 1, CAP>(c, s);
+      // fall through
     case SHAPE_NARROW: return fwd_launch<HD, NARROW, 1, CAP>(c, s);
     case SHAPE_SPLIT: return fwd_launch<HD, NARROW, 2, CAP>(c, s);
     default: return fwd_launch<HD, WIDE, 4, CAP>(c, s);
