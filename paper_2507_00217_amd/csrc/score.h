@@ -43,4 +43,16 @@ __device__ __forceinline__ int keys_end(const ScoreArgs& a, const SeqSpan& s, in
 // The queries that see key `row` are [queries_begin, s.hi).
 __device__ __forceinline__ int queries_begin(const ScoreArgs& a, const SeqSpan& s, int row) { return a.causal && row >= s.lo + s.prefix ? row : s.lo; }
 
+// Score of a product x, exact to a few roundings (the bf16 kernels have faster forms), and the cap's derivative there.
+__device__ __forceinline__ float shaped(float x, const ScoreArgs& a, float slope, int dist, float& dcap) {
+  float s = x * a.scale;
+  dcap = 1.f;
+  if (a.cap > 0.f) {
+    const float t = tanhf(s / a.cap);
+    s = a.cap * t;
+    dcap = fmaf(-t, t, 1.f);
+  }
+  return a.slope ? s - slope * (float)abs(dist) : s;
+}
+
 }  // namespace stg

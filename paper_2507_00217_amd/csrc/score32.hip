@@ -11,18 +11,6 @@
 namespace stg {
 namespace {
 
-// Score of a product x: cap and bias, exact to a few roundings (tanhf, not the approximation of the bf16 kernels); d: the cap's derivative.
-__device__ __forceinline__ float shaped(float x, const ScoreArgs& a, float slope, int dist, float& d) {
-  float s = x * a.scale;
-  d = 1.f;
-  if (a.cap > 0.f) {
-    const float t = tanhf(s / a.cap);
-    s = a.cap * t;
-    d = fmaf(-t, t, 1.f);
-  }
-  return a.slope ? s - slope * (float)abs(dist) : s;
-}
-
 struct Block { int lo, len, prefix, r0; };     // rows of the sequence, its prefix, first row of the block in it; len = 0: nothing to do
 __device__ __forceinline__ Block find_block(const ScoreArgs& a, int slot, int lane) {
   int i, t;

@@ -160,6 +160,165 @@ __device__ __forceinline__ void cap_block(f32x16& x, const ScoreCall& c) {
   }
 }
 
+// ---- infinities and NaN behind the mask ----------------------------------------------------------------------------------------
+// The products of a tile take all of its rows, those that a query does not see with weight zero, which is right as long as they are finite:
+// zero times an infinity or NaN is NaN.  The loops carry no branch for it.  A row that comes out not finite is computed again, by its
+// wavefront alone and from the pairs that count only: a lane takes one key (query) of 64 at a time, then every 64th column of the sum.
+__device__ __forceinline__ float wave_max(float v) {
+  for (int x = 1; x < 64; x <<= 1) v = fmaxf(v, __shfl_xor(v, x));
+  return v;
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  for (int x = 1; x < 64; x <<= 1) v += __shfl_xor(v, x);
+  return v;
+}
+template <int HD> __device__ __forceinline__ float dot_rows(const bf16* x, const bf16* y) {
+  float s = 0.f;
+#pragma unroll 1
+  for (int t = 0; t < HD; t += 8) {
+    const bf16x8 u = *reinterpret_cast<const bf16x8*>(x + t), v = *reinterpret_cast<const bf16x8*>(y + t);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s = fmaf((float)u[e], (float)v[e], s);
+  }
+  return s;
+}
+// acc (columns lane, lane + 64) += sum over the n rows from p on of weight (lane x: row x's) times the row
+template <int HD> __device__ __forceinline__ void add_rows(float (&acc)[HD / 64], float weight, const bf16* p, int64_t ld, int n, int lane) {
+#pragma unroll 1
+  for (int x = 0; x < n; ++x) {
+    const float f = __shfl(weight, x);
+#pragma unroll
+    for (int k = 0; k < HD / 64; ++k) acc[k] = fmaf(f, (float)p[x * ld + lane + 64 * k], acc[k]);
+  }
+}
+// the rows (of 32) of a wavefront's accumulators, one to a lane and its partner 32 further on, that hold an infinity or NaN
+template <int N> __device__ __forceinline__ unsigned odd_rows(const f32x16 (&acc)[N], bool live) {
+  float t = 0.f;
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) t = fmaf(acc[n][e], 0.f, t);            // 0, or NaN
+  const uint64_t odd = __ballot(live && t != 0.f);
+  return __builtin_amdgcn_readfirstlane((unsigned)(odd | odd >> 32));       // (said to be uniform, it leaves the loops' registers alone)
+}
+// The arguments once more, from where the launch put them (a kernel's ScoreCall is its first argument): what is computed again is found
+// again too, from them, the rank and the lane's number; kept to the end it would take registers that the loops lack.
+__device__ __forceinline__ ScoreCall call_again() {
+  typedef const __attribute__((address_space(4))) uint64_t* words;
+  words p = (words)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  static_assert(sizeof(ScoreCall) % 8 == 0, "whole words");
+  union { ScoreCall c; uint64_t w[sizeof(ScoreCall) / 8]; } u;
+#pragma unroll
+  for (unsigned i = 0; i < sizeof(ScoreCall) / 8; ++i) u.w[i] = p[i];
+  return u.c;
+}
+__device__ __forceinline__ int lane_again() { return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)); }
+// forward, queries: block qb of 32 of the tile of BQ that `rank` is, head j
+template <int HD, int BQ> __device__ __forceinline__ void again_fwd(int j, int rank, int qb, unsigned rows) {
+  const ScoreCall c = call_again();
+  const ScoreArgs& a = c.a;
+  const int lane = lane_again(), g = j / (a.h / a.hkv);
+  const Work w = find_work<BQ, true>(c, rank, lane);
+  const int q0 = w.t * BQ + qb * 32;
+  const bf16* kp = (const bf16*)a.k + (int64_t)w.lo * a.ldk + g * HD;
+  const bf16* vp = (const bf16*)a.v + (int64_t)w.lo * a.ldv + g * HD;
+  const float slope = a.slope ? a.slope[j] : 0.f;
+#pragma unroll 1
+  for (; rows; rows &= rows - 1) {
+    const int q = q0 + __builtin_ctz(rows), end = a.causal ? max(q + 1, w.prefix) : w.len;
+    const bf16* qp = (const bf16*)a.q + (int64_t)(w.lo + q) * a.ldq + j * HD;
+    float m = -INFINITY, l = 0.f, acc[HD / 64] = {}, d;
+#pragma unroll 1
+    for (int u0 = 0; u0 < end; u0 += 64) {
+      const int u = u0 + lane;
+      const float s = u < end ? shaped(dot_rows<HD>(qp, kp + (int64_t)u * a.ldk), a, slope, q - u, d) : -INFINITY;
+      const float mn = fmaxf(m, wave_max(s)), sub = mn == -INFINITY ? 0.f : mn;
+      const float p = u < end ? expf(s - sub) : 0.f, alpha = expf(m - sub);
+      l = l * alpha + wave_sum(p);
+      m = mn;
+#pragma unroll
+      for (int k = 0; k < HD / 64; ++k) acc[k] *= alpha;
+      add_rows<HD>(acc, p, vp + (int64_t)u0 * a.ldv, a.ldv, min(64, end - u0), lane);
+    }
+#pragma unroll
+    for (int k = 0; k < HD / 64; ++k) ((bf16*)a.o)[(int64_t)(w.lo + q) * a.ldo + j * HD + lane + 64 * k] = (bf16)(acc[k] / l);
+    if (lane == 0 && a.lse) a.lse[(int64_t)j * a.rows + w.lo + q] = m + logf(l);
+  }
+}
+template <int HD, int BQ> __device__ __forceinline__ void again_dq(int j, int rank, int qb, unsigned rows) {
+  const ScoreCall c = call_again();
+  const ScoreArgs& a = c.a;
+  const int lane = lane_again(), g = j / (a.h / a.hkv);
+  const Work w = find_work<BQ, true>(c, rank, lane);
+  const int q0 = w.t * BQ + qb * 32;
+  const bf16* kp = (const bf16*)a.k + (int64_t)w.lo * a.ldk + g * HD;
+  const bf16* vp = (const bf16*)a.v + (int64_t)w.lo * a.ldv + g * HD;
+  const float slope = a.slope ? a.slope[j] : 0.f;
+#pragma unroll 1
+  for (; rows; rows &= rows - 1) {
+    const int q = q0 + __builtin_ctz(rows), end = a.causal ? max(q + 1, w.prefix) : w.len;
+    const bf16* qp = (const bf16*)a.q + (int64_t)(w.lo + q) * a.ldq + j * HD;
+    const bf16* dp = (const bf16*)a.dout + (int64_t)(w.lo + q) * a.lddo + j * HD;
+    const float lse = a.lse[(int64_t)j * a.rows + w.lo + q], delta = dot_rows<HD>(dp, (const bf16*)a.o + (int64_t)(w.lo + q) * a.ldo + j * HD);
+    float acc[HD / 64] = {};
+#pragma unroll 1
+    for (int u0 = 0; u0 < end; u0 += 64) {
+      const int u = u0 + lane;
+      float ds = 0.f, d;
+      if (u < end) {
+        const float s = shaped(dot_rows<HD>(qp, kp + (int64_t)u * a.ldk), a, slope, q - u, d);
+        ds = expf(s - lse) * (dot_rows<HD>(dp, vp + (int64_t)u * a.ldv) - delta) * d;
+      }
+      add_rows<HD>(acc, ds, kp + (int64_t)u0 * a.ldk, a.ldk, min(64, end - u0), lane);
+    }
+#pragma unroll
+    for (int k = 0; k < HD / 64; ++k) ((bf16*)a.dq)[(int64_t)(w.lo + q) * a.lddq + j * HD + lane + 64 * k] = (bf16)(acc[k] * a.scale);
+  }
+}
+// dV (dk = false) or dK: block kw of 32 keys of the tile of TQ that `rank` is, of the KV head and split bx
+template <int HD, int TQ> __device__ __forceinline__ void again_dkv(int bx, int rank, int kw, bool dk, unsigned rows) {
+  const ScoreCall c = call_again();
+  const ScoreArgs& a = c.a;
+  const int lane = lane_again(), g = bx / c.nsplit, sp = bx % c.nsplit, grp = a.h / a.hkv / c.nsplit, j0 = g * (a.h / a.hkv) + sp * grp;
+  const Work w = find_work<TQ, false>(c, rank, lane);
+  const int k0 = w.t * TQ + kw * 32, dkv = a.hkv * HD;
+  const int64_t ldout = dk ? a.lddk : a.lddv, ldpart = 2 * dkv;
+  bf16* out = (bf16*)(dk ? a.dk : a.dv) + (int64_t)w.lo * ldout + g * HD;
+  float* part = c.nsplit > 1 ? c.part + ((int64_t)sp * a.rows + w.lo) * ldpart + g * HD + (dk ? 0 : dkv) : nullptr;
+#pragma unroll 1
+  for (; rows; rows &= rows - 1) {
+    const int u = k0 + __builtin_ctz(rows), begin = a.causal && u >= w.prefix ? u : 0;
+    const bf16* kp = (const bf16*)a.k + (int64_t)(w.lo + u) * a.ldk + g * HD;
+    const bf16* vp = (const bf16*)a.v + (int64_t)(w.lo + u) * a.ldv + g * HD;
+    float acc[HD / 64] = {};
+#pragma unroll 1
+    for (int j = j0; j < j0 + grp; ++j) {
+      const float slope = a.slope ? a.slope[j] : 0.f;
+      const bf16* qp = (const bf16*)a.q + (int64_t)w.lo * a.ldq + j * HD;
+      const bf16* dp = (const bf16*)a.dout + (int64_t)w.lo * a.lddo + j * HD;
+      const bf16* op = (const bf16*)a.o + (int64_t)w.lo * a.ldo + j * HD;
+#pragma unroll 1
+      for (int i0 = begin; i0 < w.len; i0 += 64) {
+        const int i = i0 + lane;
+        float f = 0.f, d;
+        if (i < w.len) {
+          const bf16* di = dp + (int64_t)i * a.lddo;
+          f = expf(shaped(dot_rows<HD>(qp + (int64_t)i * a.ldq, kp), a, slope, i - u, d) - a.lse[(int64_t)j * a.rows + w.lo + i]);
+          if (dk) f *= (dot_rows<HD>(di, vp) - dot_rows<HD>(di, op + (int64_t)i * a.ldo)) * d;
+        }
+        add_rows<HD>(acc, f, dk ? qp + (int64_t)i0 * a.ldq : dp + (int64_t)i0 * a.lddo, dk ? a.ldq : a.lddo, min(64, w.len - i0), lane);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < HD / 64; ++k) {
+      const float v = dk ? acc[k] * a.scale : acc[k];
+      if (part) part[u * ldpart + lane + 64 * k] = v;
+      else out[u * ldout + lane + 64 * k] = (bf16)v;
+    }
+  }
+}
+
 // ---- forward ----------------------------------------------------------------------------------------------------------------
 struct Row { int q, last; };           // a lane's query and the last key that it sees, both inside the sequence
 
@@ -379,7 +538,8 @@ __global__ __launch_bounds__(NT, KS == 4 && HD == 64 ? 4 : 2) void score_fwd_ker
       m = mn;
     }
   }
-  if (row.q < w.len) {
+  const unsigned odd = odd_rows(o, row.q < w.len);
+  if (row.q < w.len && !(odd >> (lane & 31) & 1)) {
     const float inv = 1.f / l;
     bf16* orow = (bf16*)a.o + (int64_t)(w.lo + row.q) * a.ldo + j * HD;
 #pragma unroll
@@ -393,6 +553,7 @@ __global__ __launch_bounds__(NT, KS == 4 && HD == 64 ? 4 : 2) void score_fwd_ker
       }
     if (hf == 0 && a.lse) a.lse[(int64_t)j * a.rows + w.lo + row.q] = (m + log2f(l)) * LN2;
   }
+  if (__builtin_expect(odd != 0, 0)) again_fwd<HD, BQ>(j, blockIdx.x / a.h, qb, odd);
 }
 
 // ---- dQ ---------------------------------------------------------------------------------------------------------------------
@@ -581,7 +742,8 @@ __device__ __forceinline__ void dq_workgroup(const ScoreCall& c, lds_char* lds, 
         }
     }
   }
-  if (row.q < w.len) {
+  const unsigned odd = odd_rows(dq, row.q < w.len);
+  if (row.q < w.len && !(odd >> (lane & 31) & 1)) {
     bf16* out = (bf16*)a.dq + (int64_t)(w.lo + row.q) * a.lddq + j * HD;
 #pragma unroll
     for (int hb = 0; hb < G::NHB; ++hb)
@@ -593,6 +755,7 @@ __device__ __forceinline__ void dq_workgroup(const ScoreCall& c, lds_char* lds, 
         *reinterpret_cast<bf16x4*>(out + hb * 32 + q4 * 8 + hf * 4) = v;
       }
   }
+  if (__builtin_expect(odd != 0, 0)) again_dq<HD, BQ>(j, rank, qb, odd);
 }
 template <int HD, int NT, int KS, bool CAP>
 __global__ __launch_bounds__(NT, 2) void score_dq_kernel(ScoreCall c) {
@@ -614,8 +777,8 @@ __device__ __forceinline__ void dkv_workgroup(const ScoreCall& c, lds_char* lds,
   const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int role = wave / (NKW * QS), kw = wave % NKW, qs = QS == 2 ? (wave / NKW) % 2 : 0;
-  const int g = bx / c.nsplit, sp = bx % c.nsplit;
-  const int dkv = a.hkv * HD, grp = a.h / a.hkv / c.nsplit, j0 = g * (a.h / a.hkv) + sp * grp;
+  const int g = __builtin_amdgcn_readfirstlane(bx / c.nsplit), sp = bx - g * c.nsplit;
+  const int dkv = a.hkv * HD, per_kv = __builtin_amdgcn_readfirstlane(a.h / a.hkv), grp = __builtin_amdgcn_readfirstlane(per_kv / c.nsplit), j0 = g * per_kv + sp * grp;
   const Work w = find_work<TQ, false>(c, rank, lane);
   if (w.len == 0) return;
   const int kt = w.t, nkt = (w.len + TQ - 1) / TQ;
@@ -843,7 +1006,8 @@ __device__ __forceinline__ void dkv_workgroup(const ScoreCall& c, lds_char* lds,
       }
   }
 
-  if (key < w.len) {             // role 0 holds dV, role 1 dK (still to be scaled)
+  const unsigned odd = odd_rows(acc, key < w.len);
+  if (key < w.len && !(odd >> (lane & 31) & 1)) {             // role 0 holds dV, role 1 dK (still to be scaled)
     const float osc = role ? a.scale : 1.f;
     if (c.nsplit == 1) {
       bf16* out = role ? (bf16*)a.dk + (int64_t)(w.lo + key) * a.lddk + g * HD : (bf16*)a.dv + (int64_t)(w.lo + key) * a.lddv + g * HD;
@@ -869,12 +1033,13 @@ __device__ __forceinline__ void dkv_workgroup(const ScoreCall& c, lds_char* lds,
         }
     }
   }
+  if (__builtin_expect(odd != 0, 0)) again_dkv<HD, TQ>(bx, rank, kw, role != 0, odd);
 }
 template <int HD, int TQ, int QS, bool CAP>
 __global__ __launch_bounds__(TQ * 4 * QS, 2) void score_dkv_kernel(ScoreCall c) {
   extern __shared__ __attribute__((aligned(1024))) char smem_raw[];
-  const int nx = c.a.hkv * c.nsplit;
-  dkv_workgroup<HD, TQ, QS, CAP, false>(c, (lds_char*)smem_raw, blockIdx.x % nx, blockIdx.x / nx);
+  const int nx = c.a.hkv * c.nsplit, rank = __builtin_amdgcn_readfirstlane(blockIdx.x / nx);
+  dkv_workgroup<HD, TQ, QS, CAP, false>(c, (lds_char*)smem_raw, blockIdx.x - rank * nx, rank);
 }
 
 // dQ and dK/dV of a small problem in one launch, which neither fills by itself; the dK/dV workgroups, the longer ones, come first

@@ -23,18 +23,6 @@ __device__ __forceinline__ float wg_reduce(float v, bool is_max, float* red) {
   return r;
 }
 
-// the score of one pair, and the derivative of the cap there
-__device__ __forceinline__ float shaped(float dot, const ScoreArgs& a, float slope, int dist, float& dcap) {
-  float s = dot * a.scale;
-  dcap = 1.f;
-  if (a.cap > 0.f) {
-    const float t = tanhf(s / a.cap);
-    s = a.cap * t;
-    dcap = 1.f - t * t;
-  }
-  return a.slope ? s - slope * (float)(dist < 0 ? -dist : dist) : s;
-}
-
 template <typename T>
 __global__ __launch_bounds__(NT) void score_fwd_ref_kernel(ScoreArgs a) {
   __shared__ float p[NT], qs[128], red[NT / 64];

@@ -1,6 +1,7 @@
 """Attention of shaped scores and per-head norms as programs use them: many sequences, long ones, wide buffers, other streams, captured
 graphs, non-finite neighbours, and the operators one behind the other in a layer."""
 import ctypes as C
+import math
 
 import numpy as np
 import pytest
@@ -9,7 +10,7 @@ from oracle import score_oracle as sc
 from oracle import stage_oracle as so
 from paper_2507_00217_amd import synth
 from tests.gpu_util import TOL, launches, rnd, to_np
-from tests.score_util import DT, Attention, int_tensor, ptr
+from tests.score_util import DT, F32, U, Attention, close, int_tensor, ptr
 from tests.test_gpu_score_attention import KERNELS, inputs, slopes
 
 pytestmark = pytest.mark.gpu
@@ -283,3 +284,38 @@ def test_the_rules_reach_every_kernel():
             want |= {f"dkv Li{hd}ELi{f}ELb{cap}" for f in ("128ELi1", "64ELi1", "64ELi2")}
             want |= {f"bwd Li{hd}ELi{f}ELb{cap}" for f in ("4ELi2", "2ELi1")}
     assert forms == want, (sorted(want - forms), sorted(forms - want))
+
+
+@pytest.mark.parametrize("dtype,kernel_set", KERNELS)
+@pytest.mark.parametrize("hd,cap,h,hkv", [(64, 0.0, 2, 2), (128, 20.0, 4, 1)])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("where", ["keys", "queries"])
+def test_nothing_behind_the_mask_reaches_a_row(dtype, kernel_set, hd, cap, h, hkv, value, where):
+    """An infinity or NaN in the keys and values of one row (or in its query and dO): what does not see it is what it is without.  Row 85 lies
+    inside a block of 32, so its tile is shared with rows on both sides; the prefix of 20 keys does not hold it."""
+    import torch
+    rows, r = 150, 85
+    q, k, v, do = inputs(dtype, rows, h, hkv, hd, 97)
+    bad = [a.copy() for a in (q, k, v, do)]
+    for a in (bad[1:3] if where == "keys" else (bad[0], bad[3])):
+        a[r, 1::5] = value
+    p = Attention(dtype, *bad, h, hkv, 1, cap=cap, prefixes=[20])
+    assert p.fwd(kernel_set) == 0 and p.bwd(kernel_set) == 0
+    torch.cuda.synchronize()
+    o, lse = to_np(p.o), to_np(p.lse)
+    rest = np.arange(rows) < r if where == "keys" else np.arange(rows) != r       # rows of o and dq that do not see it
+    after = np.arange(rows) > r                                                  # keys that no such query sees
+    opts = p.opts
+    ref, rlse, mag = sc.attention(q, k, v, **opts)
+    u = U[dtype]
+    lo = u if dtype == "bf16" else 0.0
+    close("o", o[rest], ref[rest], u * np.abs(ref[rest]) + (lo + F32) * mag[rest])
+    close("lse", lse[:, rest], rlse[:, rest], F32 * (1.0 + np.abs(rlse[:, rest])))
+    o, lse = np.where(rest[:, None], o, ref), np.where(rest[None], lse, rlse)
+    g = sc.attention_backward(q, k, v, o, lse, do, **opts)
+    for name in ("dq",) if where == "keys" else ("dq", "dk", "dv"):
+        part = rest if name == "dq" else after
+        val, rounded, apart = (t[part] for t in g[name])
+        close(name, to_np(getattr(p, name))[part], val, u * np.abs(val) + lo * rounded + F32 * apart)
+    seen = ~rest if where == "keys" else np.arange(rows) == r
+    assert np.isnan(to_np(p.o)[seen]).any(1).all() or not math.isnan(value)      # and what does see a NaN is NaN
