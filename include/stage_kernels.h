@@ -128,15 +128,16 @@ int stage_kernel_attention_bwd_ws(int dtype, int b, int s, int h, int hkv, int h
  *   s = scale * q.k,  with softcap c > 0 c * tanh(s / c),  with slopes minus slope[head] * |query row - key row|;
  *   a query sees the keys of its own sequence: all of them, or (causal) those up to itself and the sequence's prefix.
  * Sequence i is rows seq_start[i] .. seq_start[i+1] - 1; empty ones are allowed.  Rows before the first or behind the last are not read,
- * and what belongs to them in the outputs is left as it was. */
+ * and what belongs to them in the outputs is left as it was.  What a query does not see reaches none of its results, infinities and NaN
+ * included (rows that hold them take a slow way). */
 typedef struct {
   int32_t dtype;
   int32_t rows;              /* >= 1, at most 2^23 */
   int32_t n_seq;             /* >= 1, at most 2^20 */
   int32_t h, hkv, hd;        /* h a multiple of hkv; hd 64 or 128 */
   int32_t causal;            /* 0 or 1 */
-  float scale;               /* > 0, or 0 for hd^(-1/2) */
-  float softcap;             /* > 0, or 0 for none */
+  float scale;               /* 1e-30 or more, or 0 for hd^(-1/2) */
+  float softcap;             /* scale / 10^4 or more, or 0 for none */
   const float* slope;        /* device, [h], finite; or NULL for no distance bias (the slopes are constants: they get no gradient) */
   const int32_t* seq_start;  /* device, [n_seq + 1], ascending, within [0, rows] (what leaves that order gives undefined results, but touches
                                 nothing outside the rows); or NULL for n_seq sequences of rows / n_seq rows each, without remainder */
@@ -145,8 +146,8 @@ typedef struct {
 } stage_score_attention_t;
 
 /* q, o: [rows, h*hd]; k, v: [rows, hkv*hd], each with a row stride of its own (elements), so that they may be columns of one buffer.
- * lse: [h, rows] fp32, or NULL when there is no backward.  The tuned bf16 kernels want 16-byte aligned pointers and strides; what they do
- * not take, the plain kernels do. */
+ * lse: [h, rows] fp32, or NULL when there is no backward.  The tuned kernels want 16-byte aligned pointers and strides; what they do
+ * not take, the plain kernels do.  kernel_set as for the attention entries above (in fp32: 0 and 1). */
 int stage_kernel_score_attention_fwd(const stage_score_attention_t* p, const void* q, int64_t ldq, const void* k, int64_t ldk,
                                      const void* v, int64_t ldv, void* o, int64_t ldo, float* lse, int kernel_set, void* hip_stream);
 /* dq, dk, dv overlap no input and not each other.  scratch: stage_kernel_score_attention_bwd_scratch_bytes(p) bytes, 16-byte aligned, not

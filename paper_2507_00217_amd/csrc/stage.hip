@@ -1191,9 +1191,12 @@ static bool score_args(const stage_score_attention_t* p, ScoreArgs* a) {
       p->h % p->hkv || (p->hd != 64 && p->hd != 128) || (p->causal != 0 && p->causal != 1) || !(p->scale >= 0.f) || !std::isfinite(p->scale) ||
       !(p->softcap >= 0.f) || !std::isfinite(p->softcap) || (!p->seq_start && p->rows % p->n_seq) || (p->prefix && !p->causal))
     return false;
+  // (1 / scale and the fifth power of (scale / softcap)^2, the kernels' constants, have to be fp32 numbers)
+  const float scale = p->scale > 0.f ? p->scale : 1.f / sqrtf((float)p->hd);
+  if (scale < 1e-30f || (p->softcap > 0.f && scale > 1e4f * p->softcap)) return false;
   *a = ScoreArgs{};
   a->rows = p->rows; a->n_seq = p->n_seq; a->h = p->h; a->hkv = p->hkv; a->hd = p->hd; a->causal = p->causal;
-  a->scale = p->scale > 0.f ? p->scale : 1.f / sqrtf((float)p->hd);
+  a->scale = scale;
   a->cap = p->softcap; a->slope = p->slope; a->seq_start = p->seq_start; a->prefix = p->prefix;
   return true;
 }

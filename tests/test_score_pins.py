@@ -115,7 +115,8 @@ def score(**kw):
 
 BAD_SCORE = [dict(dtype=2), dict(rows=0), dict(rows=-1), dict(rows=(1 << 23) + 2), dict(n_seq=0), dict(n_seq=(1 << 20) + 1), dict(n_seq=3), dict(h=0), dict(hkv=0),
              dict(h=3), dict(hd=32), dict(hd=96), dict(causal=2), dict(scale=-1.0), dict(scale=float("inf")), dict(scale=float("nan")), dict(softcap=-1.0),
-             dict(softcap=float("nan")), dict(softcap=float("inf")), dict(causal=0, prefix=A())]
+             dict(softcap=float("nan")), dict(softcap=float("inf")), dict(causal=0, prefix=A()),
+             dict(scale=1e-31), dict(softcap=1e-5), dict(scale=1.0, softcap=9e-5)]
 
 
 @pytest.mark.parametrize("bad", BAD_SCORE)
