@@ -29,6 +29,7 @@ struct ScoreCall {
   float p3[2], p5[4];
   int tiles;                     // tiles of a sequence (equal sequences)
   int fold, nsplit;
+  int given;                     // backward: delta is in the scratch (score_delta_kernel)
   float* part;                   // [nsplit][rows][2 * hkv * hd] fp32
 };
 
@@ -260,7 +261,7 @@ template <int HD, int BQ> __device__ __forceinline__ void again_dq(int j, int ra
     const int q = q0 + __builtin_ctz(rows), end = a.causal ? max(q + 1, w.prefix) : w.len;
     const bf16* qp = (const bf16*)a.q + (int64_t)(w.lo + q) * a.ldq + j * HD;
     const bf16* dp = (const bf16*)a.dout + (int64_t)(w.lo + q) * a.lddo + j * HD;
-    const float lse = a.lse[(int64_t)j * a.rows + w.lo + q], delta = dot_rows<HD>(dp, (const bf16*)a.o + (int64_t)(w.lo + q) * a.ldo + j * HD);
+    const float lse = a.lse[(int64_t)j * a.rows + w.lo + q], delta = c.given ? a.delta[(int64_t)j * a.rows + w.lo + q] : dot_rows<HD>(dp, (const bf16*)a.o + (int64_t)(w.lo + q) * a.ldo + j * HD);
     float acc[HD / 64] = {};
 #pragma unroll 1
     for (int u0 = 0; u0 < end; u0 += 64) {
@@ -305,7 +306,7 @@ template <int HD, int TQ> __device__ __forceinline__ void again_dkv(int bx, int 
         if (i < w.len) {
           const bf16* di = dp + (int64_t)i * a.lddo;
           f = expf(shaped(dot_rows<HD>(qp + (int64_t)i * a.ldq, kp), a, slope, i - u, d) - a.lse[(int64_t)j * a.rows + w.lo + i]);
-          if (dk) f *= (dot_rows<HD>(di, vp) - dot_rows<HD>(di, op + (int64_t)i * a.ldo)) * d;
+          if (dk) f *= (dot_rows<HD>(di, vp) - (c.given ? a.delta[(int64_t)j * a.rows + w.lo + i] : dot_rows<HD>(di, op + (int64_t)i * a.ldo))) * d;
         }
         add_rows<HD>(acc, f, dk ? qp + (int64_t)i0 * a.ldq : dp + (int64_t)i0 * a.lddo, dk ? a.ldq : a.lddo, min(64, w.len - i0), lane);
       }
@@ -556,6 +557,94 @@ __global__ __launch_bounds__(NT, KS == 4 && HD == 64 ? 4 : 2) void score_fwd_ker
   if (__builtin_expect(odd != 0, 0)) again_fwd<HD, BQ>(j, blockIdx.x / a.h, qb, odd);
 }
 
+// ---- backward ---------------------------------------------------------------------------------------------------------------
+// 16 scores of a lane's query with keys from k0 on (capped: in units of log 2, else products) -> P = exp(s - lse), zero where masked
+template <bool CAP>
+__device__ __forceinline__ void probs_block(f32x16& s, const ScoreCall& c, int k0, Row row, int hf, float slope2, float lse2, bool need_mask, bool ahead) {
+  const float first = (float)(k0 + hf * 4 - row.q), off = (c.a.slope ? slope2 * first : 0.f) - lse2;
+  const float sl = CAP ? 1.f : c.sl2;
+  if (c.a.slope) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = fmaf(s[e], sl, off) + slope2 * (float)acc_row(e, 0);
+    if (ahead) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] -= 2.f * slope2 * fmaxf(first + (float)acc_row(e, 0), 0.f);
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = fast_exp2(s[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = fast_exp2(fmaf(s[e], sl, off));
+  }
+  if (need_mask) {
+    const int bound = row.last - k0 - hf * 4;
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (acc_row(e, 0) > bound) s[e] = 0.f;
+  }
+}
+
+// delta = rowsum(dO * O) is what dS = P (dP - delta) subtracts, and where a row's weight sits on few keys nearly all of dP: the rounding of O
+// to bf16 is then no longer small against what is left (dQ and dK of sequences of 8 rows, scores of 3 in the mean, off by 5.8e-3 of their
+// norm, of 4096 by 3.1e-3, where the roundings of dS and of the results alone are 2.4e-3).  So for short sequences delta is summed from the
+// probabilities, sum of P dP, ahead of the two passes: for rows of at most DELTA_KEYS keys, the others keep rowsum(dO * O).
+// One wavefront per 32 queries, operands straight from global memory.
+constexpr int DELTA_KEYS = 256;
+template <int HD, bool CAP>
+__global__ __launch_bounds__(256, 2) void score_delta_kernel(ScoreCall c) {
+  using G = Geo<HD>;
+  const ScoreArgs& a = c.a;
+  const int lane = threadIdx.x & 63, hf = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rank = __builtin_amdgcn_readfirstlane(blockIdx.x / a.h), j = blockIdx.x - rank * a.h, g = j / (a.h / a.hkv);
+  const Work w = find_work<128, true>(c, rank, lane);
+  const int q0 = w.t * 128 + wave * 32, vis = a.causal ? w.prefix : w.len;
+  if (q0 >= w.len) return;
+  const Row row{q0 + (lane & 31), min(max(a.causal ? q0 + (lane & 31) : 0, vis - 1), w.len - 1)};
+  const float slope2 = a.slope ? a.slope[j] * LOG2E : 0.f;
+  const int end = max(min(q0 + 32, w.len), vis);
+  const bf16* kp = (const bf16*)a.k + (int64_t)w.lo * a.ldk + g * HD;
+  const bf16* vp = (const bf16*)a.v + (int64_t)w.lo * a.ldv + g * HD;
+  const bf16* qp = (const bf16*)a.q + (int64_t)w.lo * a.ldq + j * HD;
+  const bf16* dop = (const bf16*)a.dout + (int64_t)w.lo * a.lddo + j * HD;
+  bf16x8 dof[G::NKK];
+#pragma unroll
+  for (int kk = 0; kk < G::NKK; ++kk) dof[kk] = frag_rows_global(dop, a.lddo, q0, w.len, kk * 16, lane);
+  float sum = 0.f;
+  const int64_t at = (int64_t)j * a.rows + w.lo + row.q;
+  if (end > DELTA_KEYS) {
+    const bf16* op = (const bf16*)a.o + (int64_t)w.lo * a.ldo + j * HD;
+#pragma unroll
+    for (int kk = 0; kk < G::NKK; ++kk) {
+      const bf16x8 of = frag_rows_global(op, a.ldo, q0, w.len, kk * 16, lane);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum = fmaf((float)dof[kk][e], (float)of[e], sum);
+    }
+  } else {
+    bf16x8 qf[G::NKK];
+#pragma unroll
+    for (int kk = 0; kk < G::NKK; ++kk) qf[kk] = frag_rows_global(qp, a.ldq, q0, w.len, kk * 16, lane);
+    const float lse2 = row.q < w.len ? a.lse[at] * LOG2E : 1e30f;
+    for (int k0 = 0; k0 < end; k0 += 32) {
+      f32x16 s, dp;
+#pragma unroll
+      for (int kk = 0; kk < G::NKK; ++kk) {
+        const bf16x8 kf = frag_rows_global(kp, a.ldk, k0, w.len, kk * 16, lane), vf = frag_rows_global(vp, a.ldv, k0, w.len, kk * 16, lane);
+        s = kk == 0 ? mfma0(kf, qf[kk]) : MFMA(kf, qf[kk], s);
+        dp = kk == 0 ? mfma0(vf, dof[kk]) : MFMA(vf, dof[kk], dp);
+      }
+      if (CAP) cap_block(s, c);
+      const bool need_mask = (a.causal && k0 + 32 > max(q0 + 1, vis)) || k0 + 32 > w.len;
+      probs_block<CAP>(s, c, k0, row, hf, slope2, lse2, need_mask, k0 + 32 > q0 + 1);
+      const int bound = need_mask ? row.last - k0 - hf * 4 : 32;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sum += acc_row(e, 0) > bound ? 0.f : s[e] * dp[e];      // (a masked dP may be anything)
+    }
+  }
+  sum = half_sum(sum, hf);
+  if (row.q < w.len && hf == 0) a.delta[at] = sum;
+}
+
 // ---- dQ ---------------------------------------------------------------------------------------------------------------------
 template <int HD, int BUF, bool CAP>
 __device__ __forceinline__ void dq_block(lds_char* lds, const FragOff<HD>& fo, const ScoreCall& c, const bf16x8 (&qf)[HD / 16], const bf16x8 (&dof)[HD / 16],
@@ -592,27 +681,7 @@ __device__ __forceinline__ void dq_block(lds_char* lds, const FragOff<HD>& fo, c
       dp[e] = (dp[e] - dl) * fmaf(-t, t, 1.f);
     }
   }
-  const float first = (float)(kv0 + n * 32 + hf * 4 - row.q), off = (c.a.slope ? slope2 * first : 0.f) - lse2;
-  const float sl = CAP ? 1.f : c.sl2;
-  if (c.a.slope) {
-#pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] = fmaf(s[e], sl, off) + slope2 * (float)acc_row(e, 0);
-    if (ahead) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] -= 2.f * slope2 * fmaxf(first + (float)acc_row(e, 0), 0.f);
-    }
-#pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] = fast_exp2(s[e]);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] = fast_exp2(fmaf(s[e], sl, off));
-  }
-  if (need_mask) {
-    const int bound = row.last - kv0 - hf * 4 - n * 32;
-#pragma unroll
-    for (int e = 0; e < 16; ++e)
-      if (acc_row(e, 0) > bound) s[e] = 0.f;
-  }
+  probs_block<CAP>(s, c, kv0 + n * 32, row, hf, slope2, lse2, need_mask, ahead);
   bf16x8 dsf[2];
 #pragma unroll
   for (int e = 0; e < 16; ++e) dsf[e >> 3][e & 7] = (bf16)(s[e] * dp[e]);
@@ -668,20 +737,22 @@ __device__ __forceinline__ void dq_workgroup(const ScoreCall& c, lds_char* lds, 
     qf[kk] = frag_rows_global(qp, a.ldq, q0w, w.len, kk * 16, lane);
     dof[kk] = frag_rows_global(dop, a.lddo, q0w, w.len, kk * 16, lane);
   }
-  // delta = rowsum(dO * O) of the lane's query, from the dO fragments in registers; written out for the dK/dV pass
-  float part = 0.f;
+  // delta of the lane's query: given, or rowsum(dO * O) from the dO fragments in registers, written out for the dK/dV pass
+  const int64_t at = (int64_t)j * a.rows + w.lo + row.q;
+  const float lse2 = row.q < w.len ? a.lse[at] * LOG2E : 1e30f;          // rows past the end: P = 0
+  float dl = 0.f;
+  if (c.given) {
+    if (row.q < w.len) dl = a.delta[at];
+  } else {
+    float part = 0.f;
 #pragma unroll
-  for (int kk = 0; kk < G::NKK; ++kk) {
-    const bf16x8 of = frag_rows_global(op, a.ldo, q0w, w.len, kk * 16, lane);
+    for (int kk = 0; kk < G::NKK; ++kk) {
+      const bf16x8 of = frag_rows_global(op, a.ldo, q0w, w.len, kk * 16, lane);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) part = fmaf((float)dof[kk][e], (float)of[e], part);
-  }
-  const float dl = half_sum(part, hf);
-  float lse2 = 1e30f;                                  // rows past the end: P = 0
-  if (row.q < w.len) {
-    const int64_t at = (int64_t)j * a.rows + w.lo + row.q;
-    lse2 = a.lse[at] * LOG2E;
-    if (hf == 0 && kh == 0) a.delta[at] = dl;
+      for (int e = 0; e < 8; ++e) part = fmaf((float)dof[kk][e], (float)of[e], part);
+    }
+    dl = half_sum(part, hf);
+    if (row.q < w.len && hf == 0 && kh == 0) a.delta[at] = dl;
   }
   f32x16 dq[G::NHB], ndl;
 #pragma unroll
@@ -1043,12 +1114,12 @@ __global__ __launch_bounds__(TQ * 4 * QS, 2) void score_dkv_kernel(ScoreCall c) 
 }
 
 // dQ and dK/dV of a small problem in one launch, which neither fills by itself; the dK/dV workgroups, the longer ones, come first
-template <int HD, int KS, int QS, bool CAP>
+template <int HD, int KS, int QS, bool CAP, bool OWN_DELTA>
 __global__ __launch_bounds__(256 * QS, 2) void score_bwd_kernel(ScoreCall c, int n_dkv) {
   static_assert(KS == 2 * QS, "one workgroup size");
   extern __shared__ __attribute__((aligned(1024))) char smem_raw[];
   const int id = blockIdx.x, nx = c.a.hkv * c.nsplit;
-  if (id < n_dkv) dkv_workgroup<HD, KEYS_SMALL, QS, CAP, true>(c, (lds_char*)smem_raw, id % nx, id / nx);
+  if (id < n_dkv) dkv_workgroup<HD, KEYS_SMALL, QS, CAP, OWN_DELTA>(c, (lds_char*)smem_raw, id % nx, id / nx);
   else dq_workgroup<HD, 256 * QS, KS, CAP>(c, (lds_char*)smem_raw, (id - n_dkv) % c.a.h, (id - n_dkv) / c.a.h);
 }
 
@@ -1204,20 +1275,28 @@ hipError_t dkv_launch(ScoreCall c, hipStream_t s) {
   hipLaunchKernelGGL((score_dkv_kernel<HD, TQ, QS, CAP>), dim3((unsigned)grid), dim3(TQ * 4 * QS), lds_bytes, s, c);
   return c.nsplit > 1 ? reduce_launch(c, s) : hipGetLastError();
 }
-template <int HD, int KS, int QS, bool CAP>
+template <int HD, int KS, int QS, bool CAP, bool OWN_DELTA>
 hipError_t bwd_fused_launch(ScoreCall c, hipStream_t s) {
   constexpr size_t dq_bytes = fwd_lds<HD, KS>(), dkv_bytes = dkv_lds<HD, KEYS_SMALL, QS>(), lds_bytes = dq_bytes > dkv_bytes ? dq_bytes : dkv_bytes;
-  static const hipError_t ready = allow_lds(score_bwd_kernel<HD, KS, QS, CAP>, lds_bytes);
+  static const hipError_t ready = allow_lds(score_bwd_kernel<HD, KS, QS, CAP, OWN_DELTA>, lds_bytes);
   if (ready != hipSuccess) return ready;
   c.nsplit = dkv_splits(c.a, KEYS_SMALL);
   const int64_t n = slots(c.a, 64), n_dkv = n * c.a.hkv * c.nsplit, grid = n_dkv + n * c.a.h;
   c.tiles = c.a.seq_start ? 0 : (int)(n / c.a.n_seq);
-  hipLaunchKernelGGL((score_bwd_kernel<HD, KS, QS, CAP>), dim3((unsigned)grid), dim3(256 * QS), lds_bytes, s, c, (int)n_dkv);
+  hipLaunchKernelGGL((score_bwd_kernel<HD, KS, QS, CAP, OWN_DELTA>), dim3((unsigned)grid), dim3(256 * QS), lds_bytes, s, c, (int)n_dkv);
   return c.nsplit > 1 ? reduce_launch(c, s) : hipGetLastError();
 }
 template <int HD, bool CAP>
-hipError_t bwd_t(const ScoreCall& c, int width, hipStream_t s) {
+hipError_t bwd_t(ScoreCall c, int width, hipStream_t s) {
   const ScoreArgs& a = c.a;
+  if (mean_len(a) <= DELTA_KEYS) {
+    c.given = 1;
+    const int64_t n = slots(a, 128);
+    c.tiles = a.seq_start ? 0 : (int)(n / a.n_seq);
+    hipLaunchKernelGGL((score_delta_kernel<HD, CAP>), dim3((unsigned)(n * a.h)), dim3(256), 0, s, c);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
   const int64_t n64 = slots(a, 64), total = n64 * a.h + n64 * a.hkv * dkv_splits(a, 64);
   const int len = mean_len(a);
   // Both passes in one launch while their workgroups (64 queries, 64 keys) number little more than what is resident; with two pairs of
@@ -1225,9 +1304,9 @@ hipError_t bwd_t(const ScoreCall& c, int width, hipStream_t s) {
   // 2048 115 / 102), with one pair (head_dim 64: three to a CU) for shorter sequences (12 x 3 x 777 32 / 33, 32 x 700 26 / 29, 4 x 5000 140 / 128; head_dim
   // 128 8 x 6 packed in 600 14 / 21).
   const bool two_pairs = 2 * total <= RESIDENT || (a.causal && ((total <= RESIDENT && len > 320) || (total <= 700 && len > 1500)));
-  if (width == 6 || (width == 0 && two_pairs)) return bwd_fused_launch<HD, 4, 2, CAP>(c, s);
+  if (width == 6 || (width == 0 && two_pairs)) return c.given ? bwd_fused_launch<HD, 4, 2, CAP, false>(c, s) : bwd_fused_launch<HD, 4, 2, CAP, true>(c, s);
   const bool one_pair = HD == 128 ? a.causal && len <= 320 && total <= RESIDENT : len <= 1500 && total <= (len > 128 ? 960 : 768);
-  if (width == 5 || (width == 0 && one_pair)) return bwd_fused_launch<HD, 2, 1, CAP>(c, s);
+  if (width == 5 || (width == 0 && one_pair)) return c.given ? bwd_fused_launch<HD, 2, 1, CAP, false>(c, s) : bwd_fused_launch<HD, 2, 1, CAP, true>(c, s);
   hipError_t e;      // dQ first: it also leaves delta in the scratch for the dK/dV pass
   switch (q_shape(a, width, false)) {
     case SHAPE_WIDE: e = dq_launch<HD, WIDE, 1, CAP>(c, s); break;

@@ -67,9 +67,20 @@ class Attention:
     def cols(self, t, n):
         return to_np(t[:, :n])
 
+    def delta_from_probabilities(self, kernel_set):
+        """The rows whose delta the bf16 kernels sum from the probabilities instead of taking it from the rounded o: those of at most 256 keys
+        where sequences have at most 256 rows in the mean, by blocks of 32 queries."""
+        out = np.zeros(self.rows, bool)
+        if self.dtype == "bf16" and kernel_set != 1 and self.rows // self.opts["n_seq"] <= 256 and all(t.stride(0) % 8 == 0 for t in (self.q, self.k, self.v, self.o)):
+            for at, n, pre in sc.sequences(self.rows, self.opts["starts"], self.opts["prefixes"], self.opts["n_seq"]):
+                for q0 in range(0, n, 32):
+                    end = max(min(q0 + 32, n), pre) if self.opts["causal"] else n
+                    out[at + q0:at + min(q0 + 32, n)] = end <= 256
+        return out
+
     def check(self, kernel_set=0, f32=F32):
-        """Runs both directions and compares with the oracle; the backward's oracle takes the kernel's own o and lse.  f32: for scores
-        beyond 100."""
+        """Runs both directions and compares with the oracle; the backward's oracle takes the kernel's own lse, and its o where delta comes from
+        that.  f32: for scores beyond 100."""
         import torch
         q, k, v, do = self.np
         assert self.fwd(kernel_set) == 0
@@ -81,6 +92,7 @@ class Attention:
         close("lse", lse, rlse, f32 * (1.0 + np.abs(rlse)))
         assert self.bwd(kernel_set) == 0
         torch.cuda.synchronize()
+        o = np.where(self.delta_from_probabilities(kernel_set)[:, None], ref, o)
         for name, (val, rounded, apart) in sc.attention_backward(q, k, v, o, lse, do, **self.opts).items():
             got = self.cols(getattr(self, name), val.shape[1])
             close(name, got, val, u * np.abs(val) + (u if self.dtype == "bf16" else 0) * rounded + f32 * apart)

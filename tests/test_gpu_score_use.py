@@ -265,7 +265,8 @@ def test_the_rules_reach_every_kernel():
             for rows, n_seq, h, hkv, packed in [      # (rows < 0: so many without a causal mask)
                                                 (8192, 1, 32, 32, 0), (4096, 2, 32, 8, 0), (8192, 13, 16, 2, 1), (2048, 1, 16, 16, 0), (5000, 1, 4, 4, 0), (2400, 3, 12, 12, 0),
                                                 (600, 6, 8, 8, 1), (8192, 100, 16, 16, 1), (1024, 1, 8, 8, 0), (9000, 1, 12, 12, 0), (6000, 5, 8, 8, 1), (700, 1, 40, 40, 0),
-                                                (3000, 1, 16, 16, 0), (6000, 1, 6, 6, 0), (1000, 5, 12, 12, 0), (-2048, 1, 8, 8, 0)]:
+                                                (3000, 1, 16, 16, 0), (6000, 1, 6, 6, 0), (1000, 5, 12, 12, 0), (-2048, 1, 8, 8, 0),
+                                                (900, 3, 8, 8, 0), (300, 1, 36, 36, 0)]:
                 a = S.ScoreAttention(dtype=1, rows=abs(rows), n_seq=n_seq, h=h, hkv=hkv, hd=hd, causal=int(rows > 0), softcap=cap, seq_start=starts.data_ptr() if packed else None)
                 p, d, dk = buf.data_ptr(), h * hd, hkv * hd
                 need = S.lib().stage_kernel_score_attention_bwd_scratch_bytes(C.byref(a))
@@ -282,7 +283,8 @@ def test_the_rules_reach_every_kernel():
             want |= {f"fwd Li{hd}ELi{f}ELb{cap}" for f in fwd}
             want |= {f"dq Li{hd}ELi{f}ELb{cap}" for f in ("512ELi1", "256ELi1", "256ELi2")}
             want |= {f"dkv Li{hd}ELi{f}ELb{cap}" for f in ("128ELi1", "64ELi1", "64ELi2")}
-            want |= {f"bwd Li{hd}ELi{f}ELb{cap}" for f in ("4ELi2", "2ELi1")}
+            want |= {f"bwd Li{hd}ELi{f}ELb{cap}ELb{own}" for f in ("4ELi2", "2ELi1") for own in (0, 1)}
+            want.add(f"delta Li{hd}ELb{cap}")
     assert forms == want, (sorted(want - forms), sorted(forms - want))
 
 
@@ -311,7 +313,8 @@ def test_nothing_behind_the_mask_reaches_a_row(dtype, kernel_set, hd, cap, h, hk
     lo = u if dtype == "bf16" else 0.0
     close("o", o[rest], ref[rest], u * np.abs(ref[rest]) + (lo + F32) * mag[rest])
     close("lse", lse[:, rest], rlse[:, rest], F32 * (1.0 + np.abs(rlse[:, rest])))
-    o, lse = np.where(rest[:, None], o, ref), np.where(rest[None], lse, rlse)
+    o = np.where(rest[:, None] & ~p.delta_from_probabilities(kernel_set)[:, None], o, ref)
+    lse = np.where(rest[None], lse, rlse)
     g = sc.attention_backward(q, k, v, o, lse, do, **opts)
     for name in ("dq",) if where == "keys" else ("dq", "dk", "dv"):
         part = rest if name == "dq" else after
