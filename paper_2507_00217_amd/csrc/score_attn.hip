@@ -29,7 +29,6 @@ struct ScoreCall {
   float p3[2], p5[4];
   int tiles;                     // tiles of a sequence (equal sequences)
   int fold, nsplit;
-  int given;                     // backward: delta is in the scratch (score_delta_kernel)
   float* part;                   // [nsplit][rows][2 * hkv * hd] fp32
 };
 
@@ -261,7 +260,7 @@ template <int HD, int BQ> __device__ __forceinline__ void again_dq(int j, int ra
     const int q = q0 + __builtin_ctz(rows), end = a.causal ? max(q + 1, w.prefix) : w.len;
     const bf16* qp = (const bf16*)a.q + (int64_t)(w.lo + q) * a.ldq + j * HD;
     const bf16* dp = (const bf16*)a.dout + (int64_t)(w.lo + q) * a.lddo + j * HD;
-    const float lse = a.lse[(int64_t)j * a.rows + w.lo + q], delta = c.given ? a.delta[(int64_t)j * a.rows + w.lo + q] : dot_rows<HD>(dp, (const bf16*)a.o + (int64_t)(w.lo + q) * a.ldo + j * HD);
+    const float lse = a.lse[(int64_t)j * a.rows + w.lo + q], delta = a.delta[(int64_t)j * a.rows + w.lo + q];
     float acc[HD / 64] = {};
 #pragma unroll 1
     for (int u0 = 0; u0 < end; u0 += 64) {
@@ -278,7 +277,7 @@ template <int HD, int BQ> __device__ __forceinline__ void again_dq(int j, int ra
   }
 }
 // dV (dk = false) or dK: block kw of 32 keys of the tile of TQ that `rank` is, of the KV head and split bx
-template <int HD, int TQ> __device__ __forceinline__ void again_dkv(int bx, int rank, int kw, bool dk, unsigned rows) {
+template <int HD, int TQ, bool OWN_DELTA> __device__ __forceinline__ void again_dkv(int bx, int rank, int kw, bool dk, unsigned rows) {
   const ScoreCall c = call_again();
   const ScoreArgs& a = c.a;
   const int lane = lane_again(), g = bx / c.nsplit, sp = bx % c.nsplit, grp = a.h / a.hkv / c.nsplit, j0 = g * (a.h / a.hkv) + sp * grp;
@@ -306,7 +305,7 @@ template <int HD, int TQ> __device__ __forceinline__ void again_dkv(int bx, int 
         if (i < w.len) {
           const bf16* di = dp + (int64_t)i * a.lddo;
           f = expf(shaped(dot_rows<HD>(qp + (int64_t)i * a.ldq, kp), a, slope, i - u, d) - a.lse[(int64_t)j * a.rows + w.lo + i]);
-          if (dk) f *= (dot_rows<HD>(di, vp) - (c.given ? a.delta[(int64_t)j * a.rows + w.lo + i] : dot_rows<HD>(di, op + (int64_t)i * a.ldo))) * d;
+          if (dk) f *= (dot_rows<HD>(di, vp) - (OWN_DELTA ? dot_rows<HD>(di, op + (int64_t)i * a.ldo) : a.delta[(int64_t)j * a.rows + w.lo + i])) * d;
         }
         add_rows<HD>(acc, f, dk ? qp + (int64_t)i0 * a.ldq : dp + (int64_t)i0 * a.lddo, dk ? a.ldq : a.lddo, min(64, w.len - i0), lane);
       }
@@ -584,65 +583,40 @@ __device__ __forceinline__ void probs_block(f32x16& s, const ScoreCall& c, int k
   }
 }
 
-// delta = rowsum(dO * O) is what dS = P (dP - delta) subtracts, and where a row's weight sits on few keys nearly all of dP: the rounding of O
-// to bf16 is then no longer small against what is left (dQ and dK of sequences of 8 rows, scores of 3 in the mean, off by 5.8e-3 of their
-// norm, of 4096 by 3.1e-3, where the roundings of dS and of the results alone are 2.4e-3).  So for short sequences delta is summed from the
-// probabilities, sum of P dP, ahead of the two passes: for rows of at most DELTA_KEYS keys, the others keep rowsum(dO * O).
-// One wavefront per 32 queries, operands straight from global memory.
-constexpr int DELTA_KEYS = 256;
-template <int HD, bool CAP>
-__global__ __launch_bounds__(256, 2) void score_delta_kernel(ScoreCall c) {
+// delta = rowsum(dO * O) is what dS = P (dP - delta) subtracts, and where a row's weight sits on few keys it is nearly all of dP: the rounding of
+// O to bf16 is then no longer small against what is left (dQ and dK of sequences of 8 rows, scores of 3 in the mean, off by 5.8e-3 of their norm,
+// of 4096 rows by 3.1e-3, where the roundings of dS and of the results alone are 2.4e-3).  So a block of 32 queries that sees no more than the
+// DELTA_KEYS keys that are in LDS before the loop starts gets delta as the sum of P dP, which costs it their two products once more.
+constexpr int DELTA_KEYS = 2 * TK;
+template <int HD, int BUF, bool CAP>
+__device__ __forceinline__ float delta_block(lds_char* lds, const FragOff<HD>& fo, const ScoreCall& c, const bf16x8 (&qf)[HD / 16], const bf16x8 (&dof)[HD / 16],
+                                             int n, int k0, Row row, int hf, float slope2, float lse2, bool need_mask, bool ahead) {
   using G = Geo<HD>;
-  const ScoreArgs& a = c.a;
-  const int lane = threadIdx.x & 63, hf = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int rank = __builtin_amdgcn_readfirstlane(blockIdx.x / a.h), j = blockIdx.x - rank * a.h, g = j / (a.h / a.hkv);
-  const Work w = find_work<128, true>(c, rank, lane);
-  const int q0 = w.t * 128 + wave * 32, vis = a.causal ? w.prefix : w.len;
-  if (q0 >= w.len) return;
-  const Row row{q0 + (lane & 31), min(max(a.causal ? q0 + (lane & 31) : 0, vis - 1), w.len - 1)};
-  const float slope2 = a.slope ? a.slope[j] * LOG2E : 0.f;
-  const int end = max(min(q0 + 32, w.len), vis);
-  const bf16* kp = (const bf16*)a.k + (int64_t)w.lo * a.ldk + g * HD;
-  const bf16* vp = (const bf16*)a.v + (int64_t)w.lo * a.ldv + g * HD;
-  const bf16* qp = (const bf16*)a.q + (int64_t)w.lo * a.ldq + j * HD;
-  const bf16* dop = (const bf16*)a.dout + (int64_t)w.lo * a.lddo + j * HD;
-  bf16x8 dof[G::NKK];
+  constexpr int KT = BUF, VT = BUF + G::TILEB, AHEAD = 3;
+  bf16x8 kf[AHEAD + 1][2];
+  f32x16 s, dp;
 #pragma unroll
-  for (int kk = 0; kk < G::NKK; ++kk) dof[kk] = frag_rows_global(dop, a.lddo, q0, w.len, kk * 16, lane);
-  float sum = 0.f;
-  const int64_t at = (int64_t)j * a.rows + w.lo + row.q;
-  if (end > DELTA_KEYS) {
-    const bf16* op = (const bf16*)a.o + (int64_t)w.lo * a.ldo + j * HD;
+  for (int kk = 0; kk < AHEAD; ++kk) { kf[kk][0] = frag_rows<HD>(lds, fo, KT, n * 32, kk); kf[kk][1] = frag_rows<HD>(lds, fo, VT, n * 32, kk); }
 #pragma unroll
-    for (int kk = 0; kk < G::NKK; ++kk) {
-      const bf16x8 of = frag_rows_global(op, a.ldo, q0, w.len, kk * 16, lane);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sum = fmaf((float)dof[kk][e], (float)of[e], sum);
+  for (int kk = 0; kk < G::NKK; ++kk) {
+    if (kk + AHEAD < G::NKK) {
+      kf[(kk + AHEAD) % (AHEAD + 1)][0] = frag_rows<HD>(lds, fo, KT, n * 32, kk + AHEAD);
+      kf[(kk + AHEAD) % (AHEAD + 1)][1] = frag_rows<HD>(lds, fo, VT, n * 32, kk + AHEAD);
     }
-  } else {
-    bf16x8 qf[G::NKK];
-#pragma unroll
-    for (int kk = 0; kk < G::NKK; ++kk) qf[kk] = frag_rows_global(qp, a.ldq, q0, w.len, kk * 16, lane);
-    const float lse2 = row.q < w.len ? a.lse[at] * LOG2E : 1e30f;
-    for (int k0 = 0; k0 < end; k0 += 32) {
-      f32x16 s, dp;
-#pragma unroll
-      for (int kk = 0; kk < G::NKK; ++kk) {
-        const bf16x8 kf = frag_rows_global(kp, a.ldk, k0, w.len, kk * 16, lane), vf = frag_rows_global(vp, a.ldv, k0, w.len, kk * 16, lane);
-        s = kk == 0 ? mfma0(kf, qf[kk]) : MFMA(kf, qf[kk], s);
-        dp = kk == 0 ? mfma0(vf, dof[kk]) : MFMA(vf, dof[kk], dp);
-      }
-      if (CAP) cap_block(s, c);
-      const bool need_mask = (a.causal && k0 + 32 > max(q0 + 1, vis)) || k0 + 32 > w.len;
-      probs_block<CAP>(s, c, k0, row, hf, slope2, lse2, need_mask, k0 + 32 > q0 + 1);
-      const int bound = need_mask ? row.last - k0 - hf * 4 : 32;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) sum += acc_row(e, 0) > bound ? 0.f : s[e] * dp[e];      // (a masked dP may be anything)
+    if (kk == 0) { s = mfma0(kf[0][0], qf[0]); dp = mfma0(kf[0][1], dof[0]); }
+    else {
+      s = MFMA(kf[kk % (AHEAD + 1)][0], qf[kk], s);
+      dp = MFMA(kf[kk % (AHEAD + 1)][1], dof[kk], dp);
     }
+    SCHED_FENCE;
   }
-  sum = half_sum(sum, hf);
-  if (row.q < w.len && hf == 0) a.delta[at] = sum;
+  if (CAP) cap_block(s, c);
+  probs_block<CAP>(s, c, k0, row, hf, slope2, lse2, need_mask, ahead);
+  const int bound = need_mask ? row.last - k0 - hf * 4 : 32;
+  float sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) sum += acc_row(e, 0) > bound ? 0.f : s[e] * dp[e];      // (a masked dP may be anything)
+  return sum;
 }
 
 // ---- dQ ---------------------------------------------------------------------------------------------------------------------
@@ -653,9 +627,9 @@ __device__ __forceinline__ void dq_block(lds_char* lds, const FragOff<HD>& fo, c
   using G = Geo<HD>;
   constexpr int KT = BUF, VT = BUF + G::TILEB, AHEAD = 3, NDQ = G::NHB * 2, VA = 4;
   bf16x8 kf[AHEAD + 1][2];
+  f32x16 s, dp;
 #pragma unroll
   for (int kk = 0; kk < AHEAD; ++kk) { kf[kk][0] = frag_rows<HD>(lds, fo, KT, n * 32, kk); kf[kk][1] = frag_rows<HD>(lds, fo, VT, n * 32, kk); }
-  f32x16 s, dp;
 #pragma unroll
   for (int kk = 0; kk < G::NKK; ++kk) {
     if (kk + AHEAD < G::NKK) {
@@ -737,33 +711,55 @@ __device__ __forceinline__ void dq_workgroup(const ScoreCall& c, lds_char* lds, 
     qf[kk] = frag_rows_global(qp, a.ldq, q0w, w.len, kk * 16, lane);
     dof[kk] = frag_rows_global(dop, a.lddo, q0w, w.len, kk * 16, lane);
   }
-  // delta of the lane's query: given, or rowsum(dO * O) from the dO fragments in registers, written out for the dK/dV pass
+  // delta of the lane's query, rowsum(dO * O) from the dO fragments in registers
   const int64_t at = (int64_t)j * a.rows + w.lo + row.q;
   const float lse2 = row.q < w.len ? a.lse[at] * LOG2E : 1e30f;          // rows past the end: P = 0
-  float dl = 0.f;
-  if (c.given) {
-    if (row.q < w.len) dl = a.delta[at];
-  } else {
-    float part = 0.f;
+  float part = 0.f;
 #pragma unroll
-    for (int kk = 0; kk < G::NKK; ++kk) {
-      const bf16x8 of = frag_rows_global(op, a.ldo, q0w, w.len, kk * 16, lane);
+  for (int kk = 0; kk < G::NKK; ++kk) {
+    const bf16x8 of = frag_rows_global(op, a.ldo, q0w, w.len, kk * 16, lane);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) part = fmaf((float)dof[kk][e], (float)of[e], part);
-    }
-    dl = half_sum(part, hf);
-    if (row.q < w.len && hf == 0 && kh == 0) a.delta[at] = dl;
+    for (int e = 0; e < 8; ++e) part = fmaf((float)dof[kk][e], (float)of[e], part);
   }
-  f32x16 dq[G::NHB], ndl;
-#pragma unroll
-  for (int hb = 0; hb < G::NHB; ++hb) zero(dq[hb]);
-#pragma unroll
-  for (int e = 0; e < 16; ++e) ndl[e] = -dl;           // what the dP products start at; capped, delta is subtracted behind them, for want of registers
   FragOff<HD> fo;
   fo.init(lane, lds);
   if (KS > 1) fo.hop((kh >> 1) * 2 * G::TILEB + (kh & 1) * 32 * G::ROWB);
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
+  if (end_w <= DELTA_KEYS && q0w < w.len) {            // or the sum of P dP (the keys of a wavefront with KS > 1: its parts of the steps)
+    part = 0.f;
+    Row row1 = row;                                    // copies that the compiler takes for others: what both places derive from them it would
+    int hf1 = hf;                                      // keep in registers through the loop
+    float slope1 = slope2, lse1 = lse2;
+    asm volatile("" : "+v"(row1.q), "+v"(row1.last), "+v"(hf1), "+v"(slope1), "+v"(lse1));
+    auto add = [&](int t, auto buf) {
+      constexpr int BUF = decltype(buf)::value;
+#pragma unroll
+      for (int n = 0; n < (KS > 1 ? 1 : 2); ++n) {
+        const int k0 = t * TS + kh * 32 + n * 32;
+        if (k0 >= end_w) break;
+        const bool need_mask = (a.causal && k0 + 32 > max(q0w + 1, vis)) || k0 + 32 > w.len;
+        part += delta_block<HD, BUF, CAP>(lds, fo, c, qf, dof, n, k0, row1, hf1, slope1, lse1, need_mask, k0 + 32 > q0w + 1);
+      }
+    };
+    add(0, std::integral_constant<int, 0>{});
+    if (KS < 4) add(1, std::integral_constant<int, BUFB>{});
+  } else if (kh > 0) part = 0.f;
+  float dl = half_sum(part, hf);
+  if constexpr (KS > 1) {                              // the other key parts' shares, in order
+    __attribute__((address_space(3))) float* shares = (__attribute__((address_space(3))) float*)(lds + 2 * BUFB) + (lane & 31);
+    if (hf == 0) shares[wave * 32] = dl;
+    __syncthreads();
+    dl = shares[qb * KS * 32];
+#pragma unroll
+    for (int p = 1; p < KS; ++p) dl += shares[(qb * KS + p) * 32];
+  }
+  if (row.q < w.len && hf == 0 && kh == 0) a.delta[at] = dl;         // for the dK/dV pass
+  f32x16 dq[G::NHB], ndl;
+#pragma unroll
+  for (int hb = 0; hb < G::NHB; ++hb) zero(dq[hb]);
+#pragma unroll
+  for (int e = 0; e < 16; ++e) ndl[e] = -dl;           // what the dP products start at; capped, delta is subtracted behind them, for want of registers
 
   auto step = [&](int t, auto buf) {
     constexpr int BUF = decltype(buf)::value;
@@ -1104,7 +1100,7 @@ __device__ __forceinline__ void dkv_workgroup(const ScoreCall& c, lds_char* lds,
         }
     }
   }
-  if (__builtin_expect(odd != 0, 0)) again_dkv<HD, TQ>(bx, rank, kw, role != 0, odd);
+  if (__builtin_expect(odd != 0, 0)) again_dkv<HD, TQ, OWN_DELTA>(bx, rank, kw, role != 0, odd);
 }
 template <int HD, int TQ, int QS, bool CAP>
 __global__ __launch_bounds__(TQ * 4 * QS, 2) void score_dkv_kernel(ScoreCall c) {
@@ -1114,12 +1110,12 @@ __global__ __launch_bounds__(TQ * 4 * QS, 2) void score_dkv_kernel(ScoreCall c) 
 }
 
 // dQ and dK/dV of a small problem in one launch, which neither fills by itself; the dK/dV workgroups, the longer ones, come first
-template <int HD, int KS, int QS, bool CAP, bool OWN_DELTA>
+template <int HD, int KS, int QS, bool CAP>
 __global__ __launch_bounds__(256 * QS, 2) void score_bwd_kernel(ScoreCall c, int n_dkv) {
   static_assert(KS == 2 * QS, "one workgroup size");
   extern __shared__ __attribute__((aligned(1024))) char smem_raw[];
   const int id = blockIdx.x, nx = c.a.hkv * c.nsplit;
-  if (id < n_dkv) dkv_workgroup<HD, KEYS_SMALL, QS, CAP, OWN_DELTA>(c, (lds_char*)smem_raw, id % nx, id / nx);
+  if (id < n_dkv) dkv_workgroup<HD, KEYS_SMALL, QS, CAP, true>(c, (lds_char*)smem_raw, id % nx, id / nx);
   else dq_workgroup<HD, 256 * QS, KS, CAP>(c, (lds_char*)smem_raw, (id - n_dkv) % c.a.h, (id - n_dkv) / c.a.h);
 }
 
@@ -1143,6 +1139,7 @@ __global__ __launch_bounds__(256) void score_dkv_reduce_kernel(ScoreCall c) {
 
 // ---- host -------------------------------------------------------------------------------------------------------------------
 template <int HD, int KS> constexpr size_t fwd_lds() { return (size_t)(KS == 4 ? 8 : 4) * Geo<HD>::TILEB; }
+template <int HD, int NT, int KS> constexpr size_t dq_lds() { return fwd_lds<HD, KS>() + (KS > 1 ? NT / 64 * 128 : 0); }      // + shares of delta
 template <int HD, int TQ, int QS> constexpr size_t dkv_lds() { return (size_t)2 * (2 * TQ * Geo<HD>::ROWB + 2 * TQ * 4) + QS * (TQ / 32) * 4096 + 64; }
 
 template <typename K>
@@ -1249,7 +1246,7 @@ hipError_t fwd_t(const ScoreCall& c, int width, hipStream_t s) {
 
 template <int HD, int NT, int KS, bool CAP>
 hipError_t dq_launch(ScoreCall c, hipStream_t s) {
-  constexpr size_t lds_bytes = fwd_lds<HD, KS>();
+  constexpr size_t lds_bytes = dq_lds<HD, NT, KS>();
   static const hipError_t ready = allow_lds(score_dq_kernel<HD, NT, KS, CAP>, lds_bytes);
   if (ready != hipSuccess) return ready;
   const int64_t n = slots(c.a, block_q<NT, KS>()), grid = n * c.a.h;
@@ -1275,38 +1272,31 @@ hipError_t dkv_launch(ScoreCall c, hipStream_t s) {
   hipLaunchKernelGGL((score_dkv_kernel<HD, TQ, QS, CAP>), dim3((unsigned)grid), dim3(TQ * 4 * QS), lds_bytes, s, c);
   return c.nsplit > 1 ? reduce_launch(c, s) : hipGetLastError();
 }
-template <int HD, int KS, int QS, bool CAP, bool OWN_DELTA>
+template <int HD, int KS, int QS, bool CAP>
 hipError_t bwd_fused_launch(ScoreCall c, hipStream_t s) {
-  constexpr size_t dq_bytes = fwd_lds<HD, KS>(), dkv_bytes = dkv_lds<HD, KEYS_SMALL, QS>(), lds_bytes = dq_bytes > dkv_bytes ? dq_bytes : dkv_bytes;
-  static const hipError_t ready = allow_lds(score_bwd_kernel<HD, KS, QS, CAP, OWN_DELTA>, lds_bytes);
+  constexpr size_t dq_bytes = dq_lds<HD, 256 * QS, KS>(), dkv_bytes = dkv_lds<HD, KEYS_SMALL, QS>(), lds_bytes = dq_bytes > dkv_bytes ? dq_bytes : dkv_bytes;
+  static const hipError_t ready = allow_lds(score_bwd_kernel<HD, KS, QS, CAP>, lds_bytes);
   if (ready != hipSuccess) return ready;
   c.nsplit = dkv_splits(c.a, KEYS_SMALL);
   const int64_t n = slots(c.a, 64), n_dkv = n * c.a.hkv * c.nsplit, grid = n_dkv + n * c.a.h;
   c.tiles = c.a.seq_start ? 0 : (int)(n / c.a.n_seq);
-  hipLaunchKernelGGL((score_bwd_kernel<HD, KS, QS, CAP, OWN_DELTA>), dim3((unsigned)grid), dim3(256 * QS), lds_bytes, s, c, (int)n_dkv);
+  hipLaunchKernelGGL((score_bwd_kernel<HD, KS, QS, CAP>), dim3((unsigned)grid), dim3(256 * QS), lds_bytes, s, c, (int)n_dkv);
   return c.nsplit > 1 ? reduce_launch(c, s) : hipGetLastError();
 }
 template <int HD, bool CAP>
-hipError_t bwd_t(ScoreCall c, int width, hipStream_t s) {
+hipError_t bwd_t(const ScoreCall& c, int width, hipStream_t s) {
   const ScoreArgs& a = c.a;
-  if (mean_len(a) <= DELTA_KEYS) {
-    c.given = 1;
-    const int64_t n = slots(a, 128);
-    c.tiles = a.seq_start ? 0 : (int)(n / a.n_seq);
-    hipLaunchKernelGGL((score_delta_kernel<HD, CAP>), dim3((unsigned)(n * a.h)), dim3(256), 0, s, c);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
   const int64_t n64 = slots(a, 64), total = n64 * a.h + n64 * a.hkv * dkv_splits(a, 64);
   const int len = mean_len(a);
   // Both passes in one launch while their workgroups (64 queries, 64 keys) number little more than what is resident; with two pairs of
   // wavefronts up to one to a CU, or with long causal chains somewhat more (one launch / two: head_dim 128 8 x 1024 33 / 46, 4 x 5000 157 / 175, 16 x
-  // 2048 115 / 102), with one pair (head_dim 64: three to a CU) for shorter sequences (12 x 3 x 777 32 / 33, 32 x 700 26 / 29, 4 x 5000 140 / 128; head_dim
-  // 128 8 x 6 packed in 600 14 / 21).
-  const bool two_pairs = 2 * total <= RESIDENT || (a.causal && ((total <= RESIDENT && len > 320) || (total <= 700 && len > 1500)));
-  if (width == 6 || (width == 0 && two_pairs)) return c.given ? bwd_fused_launch<HD, 4, 2, CAP, false>(c, s) : bwd_fused_launch<HD, 4, 2, CAP, true>(c, s);
-  const bool one_pair = HD == 128 ? a.causal && len <= 320 && total <= RESIDENT : len <= 1500 && total <= (len > 128 ? 960 : 768);
-  if (width == 5 || (width == 0 && one_pair)) return c.given ? bwd_fused_launch<HD, 2, 1, CAP, false>(c, s) : bwd_fused_launch<HD, 2, 1, CAP, true>(c, s);
+  // 2048 115 / 102), with one pair (head_dim 64: three to a CU) for shorter sequences (12 x 3 x 777 32 / 33, 32 x 700 26 / 29, 4 x 5000 140 / 128).
+  // Not for sequences of up to DELTA_KEYS rows in the mean: the dK/dV half cannot wait for the dQ half's delta and takes its own from the rounded O.
+  const bool longer = len > DELTA_KEYS;
+  const bool two_pairs = longer && (2 * total <= RESIDENT || (a.causal && ((total <= RESIDENT && len > 320) || (total <= 700 && len > 1500))));
+  if (width == 6 || (width == 0 && two_pairs)) return bwd_fused_launch<HD, 4, 2, CAP>(c, s);
+  const bool one_pair = longer && (HD == 128 ? a.causal && len <= 320 && total <= RESIDENT : len <= 1500 && total <= 960);
+  if (width == 5 || (width == 0 && one_pair)) return bwd_fused_launch<HD, 2, 1, CAP>(c, s);
   hipError_t e;      // dQ first: it also leaves delta in the scratch for the dK/dV pass
   switch (q_shape(a, width, false)) {
     case SHAPE_WIDE: e = dq_launch<HD, WIDE, 1, CAP>(c, s); break;

@@ -9,7 +9,7 @@ import ctypes as C
 import numpy as np
 
 from oracle import score_oracle as sc
-from tests.gpu_util import to_dev, to_np
+from tests.gpu_util import launches, to_dev, to_np
 
 U = {"fp32": 2.0 ** -24, "bf16": 2.0 ** -8}
 F32 = 2.0 ** -16
@@ -67,16 +67,25 @@ class Attention:
     def cols(self, t, n):
         return to_np(t[:, :n])
 
-    def delta_from_probabilities(self, kernel_set):
-        """The rows whose delta the bf16 kernels sum from the probabilities instead of taking it from the rounded o: those of at most 256 keys
-        where sequences have at most 256 rows in the mean, by blocks of 32 queries."""
-        out = np.zeros(self.rows, bool)
-        if self.dtype == "bf16" and kernel_set != 1 and self.rows // self.opts["n_seq"] <= 256 and all(t.stride(0) % 8 == 0 for t in (self.q, self.k, self.v, self.o)):
+    def o_for(self, kernel_set, o, ref):
+        """The o whose rowsum(dO * o) is the delta that dQ and that dK use: `ref` instead of the kernels' rounded `o` for the rows whose delta the bf16
+        kernels sum from the probabilities, blocks of 32 queries that see at most 128 keys; in dK only if it has a launch of its own."""
+        rows = np.zeros(self.rows, bool)
+        if self.dtype == "bf16" and kernel_set != 1 and all(t.stride(0) % 8 == 0 for t in (self.q, self.k, self.v, self.o)):
             for at, n, pre in sc.sequences(self.rows, self.opts["starts"], self.opts["prefixes"], self.opts["n_seq"]):
                 for q0 in range(0, n, 32):
                     end = max(min(q0 + 32, n), pre) if self.opts["causal"] else n
-                    out[at + q0:at + min(q0 + 32, n)] = end <= 256
-        return out
+                    rows[at + q0:at + min(q0 + 32, n)] = end <= 128
+        one_launch = any("score_bwd" in name for name, _, _ in launches(lambda st: self.bwd(kernel_set, st)))
+        dq = np.where(rows[:, None], ref, o)
+        return dq, o if one_launch else dq
+
+    def backward(self, kernel_set, o, ref, lse):
+        """The oracle's gradients with the delta of `o_for`"""
+        q, k, v, do = self.np
+        o_dq, o_dk = self.o_for(kernel_set, o, ref)
+        g = sc.attention_backward(q, k, v, o_dk, lse, do, **self.opts)
+        return {**g, "dq": sc.attention_backward(q, k, v, o_dq, lse, do, **self.opts)["dq"]}
 
     def check(self, kernel_set=0, f32=F32):
         """Runs both directions and compares with the oracle; the backward's oracle takes the kernel's own lse, and its o where delta comes from
@@ -92,8 +101,7 @@ class Attention:
         close("lse", lse, rlse, f32 * (1.0 + np.abs(rlse)))
         assert self.bwd(kernel_set) == 0
         torch.cuda.synchronize()
-        o = np.where(self.delta_from_probabilities(kernel_set)[:, None], ref, o)
-        for name, (val, rounded, apart) in sc.attention_backward(q, k, v, o, lse, do, **self.opts).items():
+        for name, (val, rounded, apart) in self.backward(kernel_set, o, ref, lse).items():
             got = self.cols(getattr(self, name), val.shape[1])
             close(name, got, val, u * np.abs(val) + (u if self.dtype == "bf16" else 0) * rounded + f32 * apart)
         for t, n in ((self.o, q.shape[1]), (self.dq, q.shape[1]), (self.dk, k.shape[1]), (self.dv, v.shape[1])):

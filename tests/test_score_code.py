@@ -6,12 +6,12 @@ from tests.test_kernel_code import code_objects, resources  # noqa: F401  (fixtu
 
 
 def test_registers_of_the_shaped_score_kernels(resources):  # noqa: F811
-    found = {re.sub(r".*?score_(\w+?)_kernelI(.*?)EEEvNS.*", r"\1 \2", n): r for n, r in resources.items() if re.search(r"score_(fwd|dq|dkv|bwd|delta)_kernelI", n)}
-    assert len(found) == 14 + 12 + 12 + 16 + 4, sorted(found)
+    found = {re.sub(r".*?score_(\w+?)_kernelI(.*?)EEEvNS.*", r"\1 \2", n): r for n, r in resources.items() if re.search(r"score_(fwd|dq|dkv|bwd)_kernelI", n)}
+    assert len(found) == 14 + 12 + 12 + 8, sorted(found)
     for n, r in found.items():
-        # dQ keeps one register in scratch across its loop, not in it, capped in the one launch with dK and dV three; the small forward of capped
+        # dQ keeps a register or two in scratch across its loop, not in it, capped in the one launch with dK and dV three; the small forward of capped
         # scores keeps two to have four wavefronts to a SIMD
-        allowed = 3 if n.startswith("bwd Li128ELi2ELi1ELb1") else 1 if n.startswith("dq ") else 2 if n == "fwd Li64ELi512ELi4ELb1" else 0
+        allowed = 3 if n.startswith("bwd Li128ELi2ELi1ELb1") else 2 if n.startswith("dq Li128") else 2 if n == "fwd Li64ELi512ELi4ELb1" else 0
         assert r["vgpr_spill_count"] <= allowed, (n, r)
     for n in ("fwd Li64ELi256ELi2ELb0", "fwd Li64ELi512ELi4ELb0", "dkv Li64ELi64ELi2ELb0"):
         assert found[n]["vgpr_count"] <= 128, (n, found[n])
