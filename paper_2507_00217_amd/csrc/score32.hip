@@ -22,7 +22,7 @@ __device__ __forceinline__ Block find_block(const ScoreArgs& a, int slot, int la
     for (int n = a.n_seq; n > 1;) {
       const int step = (n + 63) >> 6, at = lane * step;
       const bool before = at < n && min(max(a.seq_start[i + min(at, n - 1)], 0), a.rows) / 16 + i + at <= slot;
-      const int k = max(__popcll(__ballot(before)) - 1, 0) * step;
+      const int k = max((int)__popcll(__ballot(before)) - 1, 0) * step;
       i += k;
       n = min(step, n - k);
     }

@@ -91,7 +91,7 @@ __device__ __forceinline__ Work find_work(const ScoreCall& c, int rank, int lane
     for (int n = a.n_seq; n > 1;) {                    // sequences i .. i + n - 1 are left; 64 of them are looked at
       const int step = (n + 63) >> 6, at = lane * step;
       const bool before = at < n && min(max(a.seq_start[i + min(at, n - 1)], 0), a.rows) / BQ + i + at <= u;
-      const int k = max(__popcll(__ballot(before)) - 1, 0) * step;
+      const int k = max((int)__popcll(__ballot(before)) - 1, 0) * step;
       i += k;
       n = min(step, n - k);
     }

@@ -322,3 +322,45 @@ def test_nothing_behind_the_mask_reaches_a_row(dtype, kernel_set, hd, cap, h, hk
         close(name, to_np(getattr(p, name))[part], val, u * np.abs(val) + lo * rounded + F32 * apart)
     seen = ~rest if where == "keys" else np.arange(rows) == r
     assert np.isnan(to_np(p.o)[seen]).any(1).all() or not math.isnan(value)      # and what does see a NaN is NaN
+
+
+@pytest.mark.parametrize("dtype,kernel_set", KERNELS)
+@pytest.mark.parametrize("n_seq", [2, 70])
+@pytest.mark.parametrize("first", [20, 150, 330])
+def test_sequences_that_start_late(dtype, kernel_set, n_seq, first):
+    """Many rows before the first sequence: more than a workgroup's, and all but a few."""
+    rows, h, hkv, hd = 400, 2, 1, 64
+    q, k, v, do = inputs(dtype, rows, h, hkv, hd, 103)
+    starts = first + np.concatenate(([0], np.cumsum(drawn_lengths(n_seq, rows - first - 1, n_seq))))
+    Attention(dtype, q, k, v, do, h, hkv, 1, starts=starts, n_seq=n_seq, cap=20.0, slopes=[0.01, 0.1]).check(kernel_set)
+
+
+@pytest.mark.parametrize("dtype,kernel_set", KERNELS)
+@pytest.mark.parametrize("n_seq", [5, 90])
+def test_disordered_offsets_stay_inside_the_rows(dtype, kernel_set, n_seq):
+    """Offsets out of order, negative or beyond the rows, and prefixes likewise: nothing outside the rows is written, and the next call with good
+    ones is right.  (Every buffer lies between rows of its own, so that a stray access would find memory that belongs to the test.)"""
+    import torch
+    rows, h, hkv, hd, guard = 300, 2, 1, 64, 512
+    q, k, v, do = inputs(dtype, rows, h, hkv, hd, 101)
+    rng = np.random.default_rng(n_seq)
+    starts = rng.integers(-2 * rows, 3 * rows, n_seq + 1)
+    starts[:3] = (-2 ** 31, 2 ** 31 - 1, 40)
+    p = Attention(dtype, q, k, v, do, h, hkv, 1, starts=starts, prefixes=rng.integers(-2 * rows, 2 * rows, n_seq), n_seq=n_seq, cap=20.0, slopes=[0.01, 0.1])
+    around = {}
+    for n in ("q", "k", "v", "do", "o", "dq", "dk", "dv"):
+        t = getattr(p, n)
+        around[n] = torch.full((rows + 2 * guard, t.shape[1]), float("nan"), dtype=t.dtype, device="cuda:0")
+        around[n][guard:guard + rows] = t
+        setattr(p, n, around[n][guard:guard + rows])
+    flat = torch.full((h * rows + 2 * guard,), float("nan"), device="cuda:0")
+    p.lse = flat[guard:guard + h * rows].view(h, rows)
+    space = torch.full((p.scratch.numel() + 2 * guard,), 90, dtype=torch.uint8, device="cuda:0")
+    p.scratch = space[guard:guard + p.scratch.numel()]
+    assert p.fwd(kernel_set) == 0 and p.bwd(kernel_set) == 0
+    torch.cuda.synchronize()
+    for t in around.values():
+        assert bool(torch.isnan(t[:guard].float()).all()) and bool(torch.isnan(t[guard + rows:].float()).all())
+    assert bool(torch.isnan(flat[:guard]).all()) and bool(torch.isnan(flat[-guard:]).all())
+    assert bool((space[:guard] == 90).all()) and bool((space[-guard:] == 90).all())
+    Attention(dtype, q, k, v, do, h, hkv, 1, starts=[0, 100, rows], n_seq=2, cap=20.0, slopes=[0.01, 0.1]).check(kernel_set)
