@@ -17,7 +17,9 @@ namespace stg {
 namespace {
 
 constexpr int WAVES = 4, NT = WAVES * 64;
-constexpr int PARTS = 1024;            // workgroups of the backward, each of which leaves one row of partial sums
+// Workgroups of the backward, each of which leaves one row of partial sums, and their wavefronts: 16 to a compute unit in all.  (40 heads of
+// 128 x 4096 rows, forward and backward: 512 of 8 wavefronts 49.8 us, 256 of 16 49.9, 1024 of 4 52.5, 512 of 4 54.3; the sum over the rows is the difference.)
+constexpr int PARTS = 512, WB = 8, NTB = WB * 64;
 
 template <typename T> constexpr int vec() { return 16 / (int)sizeof(T); }
 
@@ -148,10 +150,10 @@ __global__ __launch_bounds__(NT) void head_rotate_kernel(HeadNormArgs n, RotateA
 // partial sums each; another launch adds those in a fixed order.
 constexpr int UB = 2;
 template <typename T, int HD, bool HALVES>
-__global__ __launch_bounds__(NT) void head_norm_bwd_kernel(HeadNormArgs n, RotateArgs r, int chunks) {
+__global__ __launch_bounds__(NTB) void head_norm_bwd_kernel(HeadNormArgs n, RotateArgs r, int chunks) {
   using P = Pairs<T, HD, HALVES>;
   constexpr int N = P::N, LPH = HD / vec<T>(), HPW = 64 / LPH;
-  __shared__ float red[WAVES * HPW][2][HD];
+  __shared__ float red[WB * HPW][2][HD];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane % LPH, heads = n.h + n.hkv;
   float gq[2][N], gk[2][N], dgq[2][N], dgk[2][N], cs[N], sn[N];
   {
@@ -167,7 +169,7 @@ __global__ __launch_bounds__(NT) void head_norm_bwd_kernel(HeadNormArgs n, Rotat
 #pragma unroll
   for (int q = 0; q < N; ++q) dgq[0][q] = dgq[1][q] = dgk[0][q] = dgk[1][q] = 0.f;
   const int64_t units = (int64_t)n.rows * chunks;
-  for (int64_t unit = (int64_t)blockIdx.x * WAVES + wave; unit < units; unit += (int64_t)gridDim.x * WAVES) {
+  for (int64_t unit = (int64_t)blockIdx.x * WB + wave; unit < units; unit += (int64_t)gridDim.x * WB) {
     const int row = (int)(unit / chunks), h0 = (int)(unit % chunks) * UB * HPW + lane / LPH;
     P xv[UB], dv[UB];
     float rstd[UB];
@@ -217,9 +219,9 @@ __global__ __launch_bounds__(NT) void head_norm_bwd_kernel(HeadNormArgs n, Rotat
       red[slot][1][col] = dgk[e][q];
     }
   __syncthreads();
-  for (int i = threadIdx.x; i < 2 * HD; i += NT) {
+  for (int i = threadIdx.x; i < 2 * HD; i += NTB) {
     float s = 0.f;
-    for (int k = 0; k < WAVES * HPW; ++k) s += (&red[k][0][0])[i];
+    for (int k = 0; k < WB * HPW; ++k) s += (&red[k][0][0])[i];
     n.partial[(int64_t)blockIdx.x * 2 * HD + i] = s;
   }
 }
@@ -259,9 +261,9 @@ template <typename T, int HD, bool HALVES>
 hipError_t bwd_launch(const HeadNormArgs& n, const RotateArgs& r, hipStream_t s) {
   constexpr int HPW = 64 * vec<T>() / HD;
   const int chunks = (n.h + n.hkv + UB * HPW - 1) / (UB * HPW);
-  const int64_t units = (int64_t)n.rows * chunks, want = (units + WAVES - 1) / WAVES;
+  const int64_t units = (int64_t)n.rows * chunks, want = (units + WB - 1) / WB;
   const int parts = (int)(want < PARTS ? want : PARTS);
-  hipLaunchKernelGGL((head_norm_bwd_kernel<T, HD, HALVES>), dim3(parts), dim3(NT), 0, s, n, r, chunks);
+  hipLaunchKernelGGL((head_norm_bwd_kernel<T, HD, HALVES>), dim3(parts), dim3(NTB), 0, s, n, r, chunks);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   ColSumList l{};
