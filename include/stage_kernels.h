@@ -146,7 +146,7 @@ typedef struct {
 } stage_score_attention_t;
 
 /* q, o: [rows, h*hd]; k, v: [rows, hkv*hd], each with a row stride of its own (elements), so that they may be columns of one buffer.
- * lse: [h, rows] fp32, or NULL when there is no backward.  The tuned kernels want 16-byte aligned pointers and strides; what they do
+ * o overlaps no input.  lse: [h, rows] fp32, or NULL when there is no backward.  The tuned kernels want 16-byte aligned pointers and strides; what they do
  * not take, the plain kernels do.  kernel_set as for the attention entries above (in fp32: 0 and 1). */
 int stage_kernel_score_attention_fwd(const stage_score_attention_t* p, const void* q, int64_t ldq, const void* k, int64_t ldk,
                                      const void* v, int64_t ldv, void* o, int64_t ldo, float* lse, int kernel_set, void* hip_stream);
