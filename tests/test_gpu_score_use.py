@@ -25,7 +25,7 @@ def drawn_lengths(n, rows, seed):
 
 
 @pytest.mark.parametrize("dtype,kernel_set", KERNELS)
-@pytest.mark.parametrize("n_seq", [64, 65, 200])
+@pytest.mark.parametrize("n_seq", [64, 65, 200, 5000])
 @pytest.mark.parametrize("causal,prefix", [(1, 1), (0, 0)])
 def test_many_sequences(dtype, kernel_set, n_seq, causal, prefix):
     """Up to 64 sequences and more than that are found in two ways; many of them are empty."""
