@@ -136,8 +136,8 @@ typedef struct {
   int32_t n_seq;             /* >= 1, at most 2^20 */
   int32_t h, hkv, hd;        /* h a multiple of hkv; hd 64 or 128 */
   int32_t causal;            /* 0 or 1 */
-  float scale;               /* 1e-30 or more, or 0 for hd^(-1/2) */
-  float softcap;             /* scale / 10^4 or more, or 0 for none */
+  float scale;               /* 1e-30 .. 1e30, or 0 for hd^(-1/2) */
+  float softcap;             /* 0 for none, or scale / 10^4 .. 1e38, with scale * (scale / softcap)^8 at most 1e38 (so it is wherever softcap >= scale) */
   const float* slope;        /* device, [h], finite; or NULL for no distance bias (the slopes are constants: they get no gradient) */
   const int32_t* seq_start;  /* device, [n_seq + 1], ascending, within [0, rows] (what leaves that order gives undefined results, but touches
                                 nothing outside the rows); or NULL for n_seq sequences of rows / n_seq rows each, without remainder */

@@ -1191,9 +1191,11 @@ static bool score_args(const stage_score_attention_t* p, ScoreArgs* a) {
       p->h % p->hkv || (p->hd != 64 && p->hd != 128) || (p->causal != 0 && p->causal != 1) || !(p->scale >= 0.f) || !std::isfinite(p->scale) ||
       !(p->softcap >= 0.f) || !std::isfinite(p->softcap) || (!p->seq_start && p->rows % p->n_seq) || (p->prefix && !p->causal))
     return false;
-  // (1 / scale and the fifth power of (scale / softcap)^2, the kernels' constants, have to be fp32 numbers)
+  // The kernels' constants have to be fp32 numbers: scale and softcap times log2 e, 1 / scale, and the coefficients of the tanh polynomial, of which the
+  // highest, 0.022 scale (scale / softcap)^8, is the largest where any is large.
   const float scale = p->scale > 0.f ? p->scale : 1.f / sqrtf((float)p->hd);
-  if (scale < 1e-30f || (p->softcap > 0.f && scale > 1e4f * p->softcap)) return false;
+  if (scale < 1e-30f || scale > 1e30f || p->softcap > 1e38f) return false;
+  if (p->softcap > 0.f && (scale > 1e4f * p->softcap || (double)scale * pow((double)scale / p->softcap, 8.0) > 1e38)) return false;
   *a = ScoreArgs{};
   a->rows = p->rows; a->n_seq = p->n_seq; a->h = p->h; a->hkv = p->hkv; a->hd = p->hd; a->causal = p->causal;
   a->scale = scale;
