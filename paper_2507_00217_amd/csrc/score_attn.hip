@@ -1291,8 +1291,10 @@ hipError_t bwd_t(const ScoreCall& c, int width, hipStream_t s) {
   // Both passes in one launch while their workgroups (64 queries, 64 keys) number little more than what is resident; with two pairs of
   // wavefronts up to one to a CU, or with long causal chains somewhat more (one launch / two: head_dim 128 8 x 1024 33 / 46, 4 x 5000 157 / 175, 16 x
   // 2048 115 / 102), with one pair (head_dim 64: three to a CU) for shorter sequences (12 x 3 x 777 32 / 33, 32 x 700 26 / 29, 4 x 5000 140 / 128).
-  // Not for sequences of up to DELTA_KEYS rows in the mean: the dK/dV half cannot wait for the dQ half's delta and takes its own from the rounded O.
-  const bool longer = len > DELTA_KEYS;
+  // Not for sequences of up to DELTA_KEYS rows: the dK/dV half cannot wait for the dQ half's delta and takes its own from the rounded O.  Nor for packed
+  // ones, whose lengths only the device knows: any of them may be that short, whatever their mean.  (That costs small packed batches time: one launch / two,
+  // head_dim 128 8 x 3 packed in 600 18 / 26, 4 x 4 in 2048 31 / 41, 4 x 3 in 4000 79 / 79; head_dim 64 8 x 3 in 600 13 / 19, 12 x 3 in 2331 45 / 50.)
+  const bool longer = !a.seq_start && len > DELTA_KEYS;
   const bool two_pairs = longer && (2 * total <= RESIDENT || (a.causal && ((total <= RESIDENT && len > 320) || (total <= 700 && len > 1500))));
   if (width == 6 || (width == 0 && two_pairs)) return bwd_fused_launch<HD, 4, 2, CAP>(c, s);
   const bool one_pair = longer && (HD == 128 ? a.causal && len <= 320 && total <= RESIDENT : len <= 1500 && total <= 960);

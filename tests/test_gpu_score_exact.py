@@ -1,0 +1,27 @@
+"""Attention of shaped scores against 64 bits from the inputs alone (tests/score_exact.py), at sizes and values where kernels differ in what they
+round."""
+import numpy as np
+import pytest
+
+from tests.score_exact import compare
+from tests.score_util import Attention
+from tests.test_gpu_score_attention import inputs, slopes
+
+pytestmark = pytest.mark.gpu
+
+# few rows among long ones: the mean is above 128 rows, so nothing but the offsets tells that some sequences are short
+MIXED = [[8, 700, 20, 12, 600, 33, 60, 480, 5, 120], [40, 9, 900, 3, 64, 128]]
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("lens", MIXED)
+@pytest.mark.parametrize("h,hkv,cap,causal", [(4, 4, 0.0, 1), (4, 2, 20.0, 1), (8, 8, 0.0, 0)])
+def test_short_sequences_packed_with_long_ones(hd, lens, h, hkv, cap, causal):
+    """Gradients of a short sequence do not lose what the rounding of O loses, whatever it is packed with."""
+    import torch
+    starts = np.concatenate(([0], np.cumsum(lens)))
+    q, k, v, do = inputs("bf16", int(starts[-1]), h, hkv, hd, 113, 2.0)
+    p = Attention("bf16", q, k, v, do, h, hkv, causal, cap=cap, starts=starts, n_seq=len(lens))
+    assert p.fwd() == 0 and p.bwd() == 0
+    torch.cuda.synchronize()
+    compare(p, only=lambda n: n <= 128)
