@@ -138,7 +138,8 @@ typedef struct {
   int32_t causal;            /* 0 or 1 */
   float scale;               /* 1e-30 .. 1e30, or 0 for hd^(-1/2) */
   float softcap;             /* 0 for none, or scale / 10^4 .. 1e38, with scale * (scale / softcap)^8 at most 1e38 (so it is wherever softcap >= scale) */
-  const float* slope;        /* device, [h], finite; or NULL for no distance bias (the slopes are constants: they get no gradient) */
+  const float* slope;        /* device, [h], of either sign, finite and at most 1e30 * scale in size; or NULL for no distance bias (the slopes are
+                                constants: they get no gradient) */
   const int32_t* seq_start;  /* device, [n_seq + 1], ascending, within [0, rows] (what leaves that order gives undefined results, but touches
                                 nothing outside the rows); or NULL for n_seq sequences of rows / n_seq rows each, without remainder */
   const int32_t* prefix;     /* device, [n_seq]: the leading keys of a sequence that all of its queries see (0: none; more than the sequence

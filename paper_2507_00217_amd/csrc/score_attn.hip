@@ -8,8 +8,10 @@
 // BQ rows each: that is never less than it needs, so rows / BQ + n_seq slots are enough for any lengths, a workgroup finds its
 // sequence by a search over the offsets (64 at a time), and no list of tiles has to be made beforehand.
 //
-// Exponents are in units of log 2 throughout.  The distance bias of a 32 x 32 block is a scalar per lane (its query or key against the
-// block's first row) plus a multiple of the row inside the block, which is the same for all lanes of a half: 16 scalar registers.
+// Exponents are in units of log 2 throughout.  The distance bias is slope times each pair's own distance, an exact whole number in fp32, so that it is off by
+// one rounding of itself and a query's own key has none, however steep the slope (taken against a block's first row, as a scalar per lane plus a
+// multiple of the row inside the block, one addition a score less, slopes of 1e4 left several percent in P, and it was no faster: forward and backward
+// of 8 heads of 128 x 16384 rows 551 + 1724 us, now 554 + 1711).
 #include "attn_tile.h"
 #include "score.h"
 
@@ -324,7 +326,7 @@ struct Row { int q, last; };           // a lane's query and the last key that i
 
 template <int HD, int BUF, int NC, bool CAP>
 __device__ __forceinline__ void fwd_tile(lds_char* lds, const FragOff<HD>& fo, const ScoreCall& c, const bf16x8 (&qf)[HD / 16], f32x16 (&o)[HD / 32],
-                                         float& m, float& l, int kv0, Row row, int hf, float slope2, bool online, bool need_mask, bool ahead) {
+                                         float& m, float& l, int kv0, Row row, int hf, float slope2, bool online, bool need_mask) {
   using G = Geo<HD>;
   constexpr int KT = BUF, VT = BUF + G::TILEB, AHEAD = 3, NPV = G::NHB * 2 * NC, VA = 4;
   bf16x8 kf[AHEAD + 1][NC];
@@ -354,24 +356,15 @@ __device__ __forceinline__ void fwd_tile(lds_char* lds, const FragOff<HD>& fo, c
 #pragma unroll
     for (int n = 0; n < NC; ++n) cap_block(s[n], c);
   }
-  // bias: slope (key - query), which is off[n] + slope * row inside the block; keys ahead of the query get twice theirs back
   const bool bias = c.a.slope != nullptr;
-  float off[NC];
-#pragma unroll
-  for (int n = 0; n < NC; ++n) off[n] = bias ? slope2 * (float)(kv0 + n * 32 + hf * 4 - row.q) : 0.f;
+  const float sl = CAP ? 1.f : c.sl2;
   if (bias) {
-    const float sb = CAP ? slope2 : slope2 * c.raw * LN2;
+    const float sb = CAP ? slope2 : slope2 * c.raw * LN2;                // in the units of s
 #pragma unroll
-    for (int n = 0; n < NC; ++n)
+    for (int n = 0; n < NC; ++n) {
+      const float first = (float)(kv0 + n * 32 + hf * 4 - row.q);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[n][e] += sb * (float)acc_row(e, 0);
-    if (ahead) {
-#pragma unroll
-      for (int n = 0; n < NC; ++n) {
-        const float first = (float)(kv0 + n * 32 + hf * 4 - row.q);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[n][e] -= 2.f * sb * fmaxf(first + (float)acc_row(e, 0), 0.f);
-      }
+      for (int e = 0; e < 16; ++e) s[n][e] = fmaf(-sb, fabsf(first + (float)acc_row(e, 0)), s[n][e]);
     }
   }
   if (need_mask) {
@@ -382,21 +375,17 @@ __device__ __forceinline__ void fwd_tile(lds_char* lds, const FragOff<HD>& fo, c
       for (int e = 0; e < 16; ++e)
         if (n * 32 + acc_row(e, 0) > bound) s[n][e] = -INFINITY;
   }
-  const float sl = CAP ? 1.f : c.sl2;
   if (!CAP || online) {
-    float top = -INFINITY;                       // the two lanes that hold a row differ in `off`, so they compare finished scores
-#pragma unroll
-    for (int n = 0; n < NC; ++n) {
-      float mx = -INFINITY;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[n][e]);
-      top = fmaxf(top, fmaf(mx, sl, off[n]));
-    }
-    const float mn = fmaxf(m, half_max(top, hf));
+    float top = -INFINITY;
 #pragma unroll
     for (int n = 0; n < NC; ++n)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[n][e] = fast_exp2(fmaf(s[n][e], sl, off[n] - mn));
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[n][e]);
+    const float mn = fmaxf(m, half_max(top, hf) * sl);
+#pragma unroll
+    for (int n = 0; n < NC; ++n)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[n][e] = fast_exp2(fmaf(s[n][e], sl, -mn));
     if (__any(mn != m)) {                        // the running max moved for some query of the wavefront
       const float alpha = fast_exp2(m - mn);
       l *= alpha;
@@ -410,7 +399,7 @@ __device__ __forceinline__ void fwd_tile(lds_char* lds, const FragOff<HD>& fo, c
 #pragma unroll
     for (int n = 0; n < NC; ++n)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[n][e] = fast_exp2(bias ? s[n][e] + off[n] : s[n][e]);
+      for (int e = 0; e < 16; ++e) s[n][e] = fast_exp2(s[n][e]);
   }
   // P is rounded to bf16 for its product; the row's sum is of what it was before
   bf16x8 pf[NC][2];
@@ -492,7 +481,7 @@ __global__ __launch_bounds__(NT, KS == 4 && HD == 64 ? 4 : 2) void score_fwd_ker
     const int kv0 = t * TS, kvw = kv0 + kh * 32;
     if (kvw < end_w && q0w < w.len) {
       const bool need_mask = (a.causal && kvw + KW > max(q0w + 1, vis)) || kvw + KW > w.len;
-      fwd_tile<HD, BUF, KW / 32, CAP>(lds, fo, c, qf, o, m, l, kvw, row, hf, slope2, online, need_mask, kvw + KW > q0w + 1);
+      fwd_tile<HD, BUF, KW / 32, CAP>(lds, fo, c, qf, o, m, l, kvw, row, hf, slope2, online, need_mask);
     }
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
@@ -559,21 +548,16 @@ __global__ __launch_bounds__(NT, KS == 4 && HD == 64 ? 4 : 2) void score_fwd_ker
 // ---- backward ---------------------------------------------------------------------------------------------------------------
 // 16 scores of a lane's query with keys from k0 on (capped: in units of log 2, else products) -> P = exp(s - lse), zero where masked
 template <bool CAP>
-__device__ __forceinline__ void probs_block(f32x16& s, const ScoreCall& c, int k0, Row row, int hf, float slope2, float lse2, bool need_mask, bool ahead) {
-  const float first = (float)(k0 + hf * 4 - row.q), off = (c.a.slope ? slope2 * first : 0.f) - lse2;
-  const float sl = CAP ? 1.f : c.sl2;
+__device__ __forceinline__ void probs_block(f32x16& s, const ScoreCall& c, int k0, Row row, int hf, float slope2, float lse2, bool need_mask) {
+  const float first = (float)(k0 + hf * 4 - row.q), sl = CAP ? 1.f : c.sl2;
   if (c.a.slope) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] = fmaf(s[e], sl, off) + slope2 * (float)acc_row(e, 0);
-    if (ahead) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] -= 2.f * slope2 * fmaxf(first + (float)acc_row(e, 0), 0.f);
-    }
+    for (int e = 0; e < 16; ++e) s[e] = fmaf(-slope2, fabsf(first + (float)acc_row(e, 0)), fmaf(s[e], sl, -lse2));
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = fast_exp2(s[e]);
   } else {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] = fast_exp2(fmaf(s[e], sl, off));
+    for (int e = 0; e < 16; ++e) s[e] = fast_exp2(fmaf(s[e], sl, -lse2));
   }
   if (need_mask) {
     const int bound = row.last - k0 - hf * 4;
@@ -590,7 +574,7 @@ __device__ __forceinline__ void probs_block(f32x16& s, const ScoreCall& c, int k
 constexpr int DELTA_KEYS = 2 * TK;
 template <int HD, int BUF, bool CAP>
 __device__ __forceinline__ float delta_block(lds_char* lds, const FragOff<HD>& fo, const ScoreCall& c, const bf16x8 (&qf)[HD / 16], const bf16x8 (&dof)[HD / 16],
-                                             int n, int k0, Row row, int hf, float slope2, float lse2, bool need_mask, bool ahead) {
+                                             int n, int k0, Row row, int hf, float slope2, float lse2, bool need_mask) {
   using G = Geo<HD>;
   constexpr int KT = BUF, VT = BUF + G::TILEB, AHEAD = 3;
   bf16x8 kf[AHEAD + 1][2];
@@ -611,7 +595,7 @@ __device__ __forceinline__ float delta_block(lds_char* lds, const FragOff<HD>& f
     SCHED_FENCE;
   }
   if (CAP) cap_block(s, c);
-  probs_block<CAP>(s, c, k0, row, hf, slope2, lse2, need_mask, ahead);
+  probs_block<CAP>(s, c, k0, row, hf, slope2, lse2, need_mask);
   const int bound = need_mask ? row.last - k0 - hf * 4 : 32;
   float sum = 0.f;
 #pragma unroll
@@ -623,7 +607,7 @@ __device__ __forceinline__ float delta_block(lds_char* lds, const FragOff<HD>& f
 template <int HD, int BUF, bool CAP>
 __device__ __forceinline__ void dq_block(lds_char* lds, const FragOff<HD>& fo, const ScoreCall& c, const bf16x8 (&qf)[HD / 16], const bf16x8 (&dof)[HD / 16],
                                          f32x16 (&dq)[HD / 32], int n, int kv0, Row row, int hf, float slope2, float lse2, float dl, const f32x16& ndl,
-                                         bool need_mask, bool ahead) {
+                                         bool need_mask) {
   using G = Geo<HD>;
   constexpr int KT = BUF, VT = BUF + G::TILEB, AHEAD = 3, NDQ = G::NHB * 2, VA = 4;
   bf16x8 kf[AHEAD + 1][2];
@@ -655,7 +639,7 @@ __device__ __forceinline__ void dq_block(lds_char* lds, const FragOff<HD>& fo, c
       dp[e] = (dp[e] - dl) * fmaf(-t, t, 1.f);
     }
   }
-  probs_block<CAP>(s, c, kv0 + n * 32, row, hf, slope2, lse2, need_mask, ahead);
+  probs_block<CAP>(s, c, kv0 + n * 32, row, hf, slope2, lse2, need_mask);
   bf16x8 dsf[2];
 #pragma unroll
   for (int e = 0; e < 16; ++e) dsf[e >> 3][e & 7] = (bf16)(s[e] * dp[e]);
@@ -739,7 +723,7 @@ __device__ __forceinline__ void dq_workgroup(const ScoreCall& c, lds_char* lds, 
         const int k0 = t * TS + kh * 32 + n * 32;
         if (k0 >= end_w) break;
         const bool need_mask = (a.causal && k0 + 32 > max(q0w + 1, vis)) || k0 + 32 > w.len;
-        part += delta_block<HD, BUF, CAP>(lds, fo, c, qf, dof, n, k0, row1, hf1, slope1, lse1, need_mask, k0 + 32 > q0w + 1);
+        part += delta_block<HD, BUF, CAP>(lds, fo, c, qf, dof, n, k0, row1, hf1, slope1, lse1, need_mask);
       }
     };
     add(0, std::integral_constant<int, 0>{});
@@ -770,7 +754,7 @@ __device__ __forceinline__ void dq_workgroup(const ScoreCall& c, lds_char* lds, 
         const int k0 = kvw + n * 32;
         if (n > 0 && k0 >= end_w) continue;            // no query of the wavefront sees this block
         const bool need_mask = (a.causal && k0 + 32 > max(q0w + 1, vis)) || k0 + 32 > w.len;
-        dq_block<HD, BUF, CAP>(lds, fo, c, qf, dof, dq, n, kvw, row, hf, slope2, lse2, dl, ndl, need_mask, k0 + 32 > q0w + 1);
+        dq_block<HD, BUF, CAP>(lds, fo, c, qf, dof, dq, n, kvw, row, hf, slope2, lse2, dl, ndl, need_mask);
       }
     }
     __builtin_amdgcn_s_waitcnt(0);
@@ -875,8 +859,7 @@ __device__ __forceinline__ void dkv_workgroup(const ScoreCall& c, lds_char* lds,
     if (wave < TQ / 64) {                // one query per lane; those past the end get P = 0
       const int qi = q0 + wave * 64 + lane;
       const int64_t at = (int64_t)j * a.rows + w.lo + qi;
-      const float slope2 = bias ? a.slope[j] * LOG2E : 0.f;
-      stat_l = qi < w.len ? -LOG2E * a.lse[at] - (bias ? slope2 * (float)(qi - k0b) : 0.f) : -1e30f;
+      stat_l = qi < w.len ? -LOG2E * a.lse[at] : -1e30f;
       if (!OWN_DELTA) stat_d = qi < w.len ? a.delta[at] : 0.f;
     }
     if constexpr (OWN_DELTA) {           // the pieces of O that go with the pieces of dO this thread has just asked for
@@ -886,7 +869,7 @@ __device__ __forceinline__ void dkv_workgroup(const ScoreCall& c, lds_char* lds,
       for (int n = 0; n < NLD; ++n) of[n] = *reinterpret_cast<const bf16x8*>(oh + (int64_t)min(q0 + n * SWEEP + sl / G::PPR, w.len - 1) * a.ldo + cc * 8);
     }
   };
-  // the statistics of the tile fetched last: the exponents' share of the query (-lse, and the bias up to the workgroup's first key), and -delta
+  // the statistics of the tile fetched last: -lse in units of log 2, and -delta
   auto put_stats = [&](lds_char* buf, int q_of) {
     if (wave < TQ / 64) {
       *(__attribute__((address_space(3))) float*)(buf + LT + (wave * 64 + lane) * 4) = stat_l;
@@ -961,8 +944,7 @@ __device__ __forceinline__ void dkv_workgroup(const ScoreCall& c, lds_char* lds,
       const int tq = t_first + it % per_head, q0 = tq * TQ;
       const bool diag = a.causal && tq <= kt;          // some query of the tile is ahead of some key: masked unless the key is in the prefix
       const int lim0 = key < w.prefix ? -(1 << 30) : key - q0 - hf * 4 - qs * 32;
-      const float slope2 = bias ? a.slope[j0 + it / per_head] * LOG2E : 0.f, kbias = slope2 * (float)(key - k0b);
-      const bool ahead = bias && tq <= kt;             // keys ahead of their query: twice the bias back
+      const float slope2 = bias ? a.slope[j0 + it / per_head] * LOG2E : 0.f;
 #pragma unroll
       for (int qc = 0; qc < NB; ++qc) {
         f32x4 l4[4];
@@ -981,12 +963,10 @@ __device__ __forceinline__ void dkv_workgroup(const ScoreCall& c, lds_char* lds,
         }
         if (bias) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) s[e] = (CAP ? s[e] + l4[e >> 2][e & 3] : fmaf(s[e], c.sl2, l4[e >> 2][e & 3])) + kbias;
-          if (ahead) {
-            const float first = (float)(q0 + (qc * QS + qs) * 32 + hf * 4 - key);
+          for (int e = 0; e < 16; ++e) s[e] = CAP ? s[e] + l4[e >> 2][e & 3] : fmaf(s[e], c.sl2, l4[e >> 2][e & 3]);
+          const float first = (float)(q0 + (qc * QS + qs) * 32 + hf * 4 - key);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] += 2.f * slope2 * fminf(first + (float)acc_row(e, 0), 0.f);
-          }
+          for (int e = 0; e < 16; ++e) s[e] = fmaf(-slope2, fabsf(first + (float)acc_row(e, 0)), s[e]);
 #pragma unroll
           for (int e = 0; e < 16; ++e) s[e] = fast_exp2(s[e]);
         } else {

@@ -5,7 +5,7 @@ import pytest
 
 from tests.score_exact import compare
 from tests.score_util import Attention
-from tests.test_gpu_score_attention import inputs, slopes
+from tests.test_gpu_score_attention import KERNELS, inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -25,3 +25,18 @@ def test_short_sequences_packed_with_long_ones(hd, lens, h, hkv, cap, causal):
     assert p.fwd() == 0 and p.bwd() == 0
     torch.cuda.synchronize()
     compare(p, only=lambda n: n <= 128)
+
+
+@pytest.mark.parametrize("dtype,kernel_set", KERNELS)
+@pytest.mark.parametrize("hd,cap", [(64, 0.0), (128, 0.0), (128, 20.0)])
+@pytest.mark.parametrize("causal,prefix", [(1, 0), (1, 90), (0, 0)])
+def test_steep_slopes(dtype, kernel_set, hd, cap, causal, prefix):
+    """The bias of a pair of rows at distance 0 is 0 and that of neighbours one slope, however steep it is: nothing of the distances to a block's first row
+    is left in them.  (A pair whose bias is beyond 100 has no weight.)"""
+    import torch
+    rows, s = 300, [3.0, 50.0, 1e4, 3e6]
+    q, k, v, do = inputs(dtype, rows, 4, 2, hd, 127)
+    p = Attention(dtype, q, k, v, do, 4, 2, causal, cap=cap, slopes=s, prefixes=[prefix] if prefix else None)
+    assert p.fwd(kernel_set) == 0 and p.bwd(kernel_set) == 0
+    torch.cuda.synchronize()
+    compare(p, exact_delta=(False, False))
