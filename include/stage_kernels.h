@@ -151,7 +151,8 @@ typedef struct {
  * not take, the plain kernels do.  kernel_set as for the attention entries above (in fp32: 0 and 1). */
 int stage_kernel_score_attention_fwd(const stage_score_attention_t* p, const void* q, int64_t ldq, const void* k, int64_t ldk,
                                      const void* v, int64_t ldv, void* o, int64_t ldo, float* lse, int kernel_set, void* hip_stream);
-/* dq, dk, dv overlap no input and not each other.  scratch: stage_kernel_score_attention_bwd_scratch_bytes(p) bytes, 16-byte aligned, not
+/* The probabilities are exp(s - lse) again, with s and lse as fp32 numbers: scores of size S leave them an error of S * 2^-23 of themselves.
+ * dq, dk, dv overlap no input and not each other.  scratch: stage_kernel_score_attention_bwd_scratch_bytes(p) bytes, 16-byte aligned, not
  * shared by calls on different streams.  Results are the same bits from call to call. */
 int stage_kernel_score_attention_bwd(const stage_score_attention_t* p, const void* q, int64_t ldq, const void* k, int64_t ldk,
                                      const void* v, int64_t ldv, const void* o, int64_t ldo, const float* lse, const void* dout,

@@ -15,6 +15,7 @@
 #include "attn_tile.h"
 #include "score.h"
 
+#include <cfloat>
 #include <type_traits>
 
 namespace stg {
@@ -469,7 +470,7 @@ __global__ __launch_bounds__(NT, KS == 4 && HD == 64 ? 4 : 2) void score_fwd_ker
   // Capped scores lie within c2 of zero and a bias only lowers them: up to c2 = 80 exp2 of them and its sums stay well inside fp32, so
   // the running maximum (and the rescaling that comes with it) is not needed.
   const bool online = !CAP || c.c2 > 80.f || slope2 < 0.f;
-  float m = online ? -1e30f : 0.f, l = 0.f;
+  float m = online ? -FLT_MAX : 0.f, l = 0.f;            // (finite: wavefronts and rows that see nothing of a tile take differences of it)
   FragOff<HD> fo;
   fo.init(lane, lds);
   if (KS > 1) fo.hop((kh >> 1) * 2 * G::TILEB + (kh & 1) * 32 * G::ROWB);
@@ -527,6 +528,8 @@ __global__ __launch_bounds__(NT, KS == 4 && HD == 64 ? 4 : 2) void score_fwd_ker
       m = mn;
     }
   }
+  // Exponents are taken from the rounded maximum m, which is off by up to 2^-24 of itself: beyond 2^30 that alone may overflow the sums, or leave nothing of them.
+  if (l < 1e-30f) o[0][0] = INFINITY;
   const unsigned odd = odd_rows(o, row.q < w.len);
   if (row.q < w.len && !(odd >> (lane & 31) & 1)) {
     const float inv = 1.f / l;

@@ -30,7 +30,7 @@ def definition(p, head, at, n, prefix, exact_delta):
     if o["causal"]:
         s = s.masked_fill((i[None, :] > i[:, None]) & (i >= prefix)[None, :], -float("inf"))
     lse = torch.logsumexp(s, 1)
-    P = torch.exp(s - lse[:, None])
+    P = torch.softmax(s, 1)                        # (from the differences to the row's highest: s - lse would lose the sum of scores beyond 1e16)
     del s
     out, mag = P @ v, P @ v.abs()
     r = {"o": (out, (u + F32) * mag), "lse": (lse, F32 * (1.0 + lse.abs()))}
@@ -49,9 +49,9 @@ def definition(p, head, at, n, prefix, exact_delta):
     return r
 
 
-def compare(p, groups=None, exact_delta=(True, True), only=None):
+def compare(p, groups=None, exact_delta=(True, True), only=None, names=("o", "lse", "dq", "dk", "dv")):
     """p: tests.score_util.Attention after fwd and bwd.  groups: the KV heads to look at.  exact_delta: whether blocks that see few keys have their delta from
-    the probabilities in dQ, in dK.  only: predicate on a sequence's length."""
+    the probabilities in dQ, in dK.  only: predicate on a sequence's length.  names: the results to look at."""
     dev = lambda b: torch.tensor(b, device=p.q.device)
     flags = tuple(dev(p.dtype == "bf16" and f) for f in exact_delta)
     grp, hd, u = p.h // p.hkv, p.hd, U[p.dtype]
@@ -66,12 +66,13 @@ def compare(p, groups=None, exact_delta=(True, True), only=None):
                 for name in kv:
                     kv[name] = r[name] if kv[name] is None else tuple(a + b for a, b in zip(kv[name], r[name]))
                 c = slice(j * hd, (j + 1) * hd)
-                within("o", p.o[rows, c], *r["o"], u, (j, at))
-                within("lse", p.lse[j, rows], *r["lse"], 0.0, (j, at))
-                within("dq", p.dq[rows, c], *r["dq"], u, (j, at))
+                for name, got in (("o", p.o[rows, c]), ("lse", p.lse[j, rows]), ("dq", p.dq[rows, c])):
+                    if name in names:
+                        within(name, got, *r[name], 0.0 if name == "lse" else u, (j, at))
             c = slice(g * hd, (g + 1) * hd)
-            within("dk", p.dk[rows, c], *kv["dk"], u, (g, at))
-            within("dv", p.dv[rows, c], *kv["dv"], u, (g, at))
+            for name, got in (("dk", p.dk[rows, c]), ("dv", p.dv[rows, c])):
+                if name in names:
+                    within(name, got, *kv[name], u, (g, at))
 
 
 def within(name, got, want, bound, u, where):

@@ -40,3 +40,21 @@ def test_steep_slopes(dtype, kernel_set, hd, cap, causal, prefix):
     assert p.fwd(kernel_set) == 0 and p.bwd(kernel_set) == 0
     torch.cuda.synchronize()
     compare(p, exact_delta=(False, False))
+
+
+@pytest.mark.parametrize("dtype,kernel_set", KERNELS)
+@pytest.mark.parametrize("hd,cap", [(64, 0.0), (128, 0.0), (128, 2.0 ** 110)])
+@pytest.mark.parametrize("size", [2.0 ** 40, 2.0 ** 53, 2.0 ** 59])
+def test_scores_far_below_zero(dtype, kernel_set, hd, cap, size):
+    """Scores of -1e23 to -1e35 are scores like any others: a row's weight is on its highest, wherever that lies.  (The products are exact; of the softmax
+    nothing but the largest is left, so o is that key's value.)"""
+    import torch
+    rows = 200
+    _, _, v, do = inputs(dtype, rows, 1, 1, hd, 131)
+    q, k = np.zeros((rows, hd), np.float32), np.zeros((rows, hd), np.float32)
+    rank = np.random.default_rng(3).permutation(256)[:rows] // 2                   # 7 bits: exact in bf16, two keys at most share one
+    q[:, 3], k[:, 3] = size, -size * (1.0 + rank / 128.0)
+    p = Attention(dtype, q, k, v, do, 1, 1, 1, cap=cap)
+    assert p.fwd(kernel_set) == 0
+    torch.cuda.synchronize()
+    compare(p, names=("o", "lse"))
