@@ -138,9 +138,11 @@ struct Loader {
 
 // ---- scores -----------------------------------------------------------------------------------------------------------------
 // 16 products x -> capped scores in units of log 2.  Scores that are not pressed against the cap, |y| <= 0.25 or 0.6 with y = x scale / cap, take
-// tanh(y) = y (1 + y^2 (a1 + ...)) with two or four coefficients (fitted by least squares; tanh is off by 8e-8 and 3e-8 at most, less
-// than the rounding of a score of 10), a block with any larger one 1 - 2 / (exp(2 y) + 1), whose two transcendental instructions each
-// cost as much as four others.
+// tanh(y) = y (1 + y^2 (a1 + ...)) with two or four coefficients (fitted by least squares; tanh is off by 8e-8 and 3e-8 at most, a score of
+// 12 under a cap of 50 by 4e-6), a block with any larger one 1 - 2 / (exp(2 y) + 1), whose two transcendental instructions each
+// cost as much as four others.  That form is off by 2^-22 of the cap, which beside one high score the low ones of the block would have too: nothing
+// against the rounding of P to bf16 up to WIDE_CAP (8e-5 of P, a 46th of half a step), above it the low ones keep the polynomial.
+constexpr float WIDE_CAP = 512.f;      // in units of log 2
 __device__ __forceinline__ void cap_block(f32x16& x, const ScoreCall& c) {
   float mx = 0.f;
 #pragma unroll
@@ -157,9 +159,18 @@ __device__ __forceinline__ void cap_block(f32x16& x, const ScoreCall& c) {
       const float y = x[e] * x[e];
       x[e] *= fmaf(y, fmaf(y, fmaf(y, fmaf(y, c.p5[3], c.p5[2]), c.p5[1]), c.p5[0]), c.sl2);
     }
-  } else {
+  } else if (c.c2 <= WIDE_CAP) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) x[e] = fmaf(__builtin_amdgcn_rcpf(fast_exp2(x[e] * c.kx) + 1.f), -2.f * c.c2, c.c2);
+  } else {
+    asm volatile("" : "+v"(x));          // (the block stays in its registers: left to itself this branch gets a second set)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float y = x[e] * x[e], t = fmaf(__builtin_amdgcn_rcpf(fast_exp2(x[e] * c.kx) + 1.f), -2.f * c.c2, c.c2);
+      x[e] = fabsf(x[e]) <= c.middling ? x[e] * fmaf(y, fmaf(y, fmaf(y, fmaf(y, c.p5[3], c.p5[2]), c.p5[1]), c.p5[0]), c.sl2) : t;
+      SCHED_FENCE;
+    }
+    asm volatile("" : "+v"(x));
   }
 }
 

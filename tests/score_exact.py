@@ -49,9 +49,10 @@ def definition(p, head, at, n, prefix, exact_delta):
     return r
 
 
-def compare(p, groups=None, exact_delta=(True, True), only=None, names=("o", "lse", "dq", "dk", "dv")):
+def compare(p, groups=None, exact_delta=(True, True), only=None, names=("o", "lse", "dq", "dk", "dv"), rows=None):
     """p: tests.score_util.Attention after fwd and bwd.  groups: the KV heads to look at.  exact_delta: whether blocks that see few keys have their delta from
-    the probabilities in dQ, in dK.  only: predicate on a sequence's length.  names: the results to look at."""
+    the probabilities in dQ, in dK.  only: predicate on a sequence's length.  names: the results to look at.
+    rows: mask of the rows of o, lse and dq to look at."""
     dev = lambda b: torch.tensor(b, device=p.q.device)
     flags = tuple(dev(p.dtype == "bf16" and f) for f in exact_delta)
     grp, hd, u = p.h // p.hkv, p.hd, U[p.dtype]
@@ -60,17 +61,18 @@ def compare(p, groups=None, exact_delta=(True, True), only=None, names=("o", "ls
             if only is not None and not only(n):
                 continue
             kv = {"dk": None, "dv": None}
-            rows = slice(at, at + n)
+            span = slice(at, at + n)
+            look = torch.ones(n, dtype=torch.bool, device=p.q.device) if rows is None else dev(np.asarray(rows)[span])
             for j in range(g * grp, (g + 1) * grp):
                 r = definition(p, j, at, n, prefix, flags)
                 for name in kv:
                     kv[name] = r[name] if kv[name] is None else tuple(a + b for a, b in zip(kv[name], r[name]))
                 c = slice(j * hd, (j + 1) * hd)
-                for name, got in (("o", p.o[rows, c]), ("lse", p.lse[j, rows]), ("dq", p.dq[rows, c])):
+                for name, got in (("o", p.o[span, c]), ("lse", p.lse[j, span]), ("dq", p.dq[span, c])):
                     if name in names:
-                        within(name, got, *r[name], 0.0 if name == "lse" else u, (j, at))
+                        within(name, got[look], *(t[look] for t in r[name]), 0.0 if name == "lse" else u, (j, at))
             c = slice(g * hd, (g + 1) * hd)
-            for name, got in (("dk", p.dk[rows, c]), ("dv", p.dv[rows, c])):
+            for name, got in (("dk", p.dk[span, c]), ("dv", p.dv[span, c])):
                 if name in names:
                     within(name, got, *kv[name], u, (g, at))
 

@@ -3,6 +3,7 @@ round."""
 import numpy as np
 import pytest
 
+from tests.gpu_util import rnd
 from tests.score_exact import compare
 from tests.score_util import Attention
 from tests.test_gpu_score_attention import KERNELS, inputs
@@ -58,3 +59,21 @@ def test_scores_far_below_zero(dtype, kernel_set, hd, cap, size):
     assert p.fwd(kernel_set) == 0
     torch.cuda.synchronize()
     compare(p, names=("o", "lse"))
+
+
+@pytest.mark.parametrize("dtype,kernel_set", KERNELS)
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("cap", [2e3, 1e5, 1e7])
+def test_large_cap_beside_outliers(dtype, kernel_set, hd, cap):
+    """A cap far above the scores of most rows, with some rows that reach it: the others keep their precision, though they share blocks with them.  (The
+    outliers' own scores are beyond what F32 is for; their dO is zero, so they add nothing to dk and dv.)"""
+    import torch
+    rows = 230
+    q, k, v, do = inputs(dtype, rows, 2, 1, hd, 137)
+    big = np.arange(rows) % 7 == 3
+    q[big] = rnd(q[big] * cap, dtype)
+    do[big] = 0.0
+    p = Attention(dtype, q, k, v, do, 2, 1, 1, cap=cap)
+    assert p.fwd(kernel_set) == 0 and p.bwd(kernel_set) == 0
+    torch.cuda.synchronize()
+    compare(p, exact_delta=(False, False), rows=~big)
