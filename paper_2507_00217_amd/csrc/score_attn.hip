@@ -30,6 +30,7 @@ struct ScoreCall {
   float c2, ic2, kx;             // kx = 2 log2 e scale / cap
   float small, middling;         // |x| up to which the polynomials hold: s = x (sl2 + x^2 (p[0] + x^2 ...))
   float p3[2], p5[4];
+  int wide;                      // the cap is far above the scale (and these two below any |x|)
   int tiles;                     // tiles of a sequence (equal sequences)
   int fold, nsplit;
   float* part;                   // [nsplit][rows][2 * hkv * hd] fp32
@@ -140,9 +141,18 @@ struct Loader {
 // 16 products x -> capped scores in units of log 2.  Scores that are not pressed against the cap, |y| <= 0.25 or 0.6 with y = x scale / cap, take
 // tanh(y) = y (1 + y^2 (a1 + ...)) with two or four coefficients (fitted by least squares; tanh is off by 8e-8 and 3e-8 at most, a score of
 // 12 under a cap of 50 by 4e-6), a block with any larger one 1 - 2 / (exp(2 y) + 1), whose two transcendental instructions each
-// cost as much as four others.  That form is off by 2^-22 of the cap, which beside one high score the low ones of the block would have too: nothing
-// against the rounding of P to bf16 up to WIDE_CAP (8e-5 of P, a 46th of half a step), above it the low ones keep the polynomial.
+// cost as much as four others.  That form is off by 2^-22 of the cap, which beside one high score the low ones of the block have too: up to
+// WIDE_CAP nothing against the rounding of P to bf16 (8e-5 of P, a 46th of half a step).  The coefficients are those of x itself, one product less,
+// and run out of fp32's range where the cap is far above the scale.  For such caps (`wide`) every score goes by itself, cap_one (a cap
+// of 1000, 32 heads of 128 on 8 x 4096, forward and backward: 170 + 551 -> 238 + 752 us).
+constexpr double TANH2[2] = {-0.33322914994946595, 0.12846042911412406};
+constexpr double TANH4[4] = {-0.33332247985930596, 0.13308098290393836, -0.05199433652233533, 0.015319205699263892};
 constexpr float WIDE_CAP = 512.f;      // in units of log 2
+__device__ __forceinline__ float cap_one(float x, const ScoreCall& c) {
+  const float y = x * (c.kx * (0.5f * LN2)), z = y * y;
+  const float low = x * c.sl2 * fmaf(z, fmaf(z, fmaf(z, fmaf(z, (float)TANH4[3], (float)TANH4[2]), (float)TANH4[1]), (float)TANH4[0]), 1.f);
+  return fabsf(y) <= 0.6f ? low : fmaf(__builtin_amdgcn_rcpf(fast_exp2(x * c.kx) + 1.f), -2.f * c.c2, c.c2);
+}
 __device__ __forceinline__ void cap_block(f32x16& x, const ScoreCall& c) {
   float mx = 0.f;
 #pragma unroll
@@ -159,16 +169,14 @@ __device__ __forceinline__ void cap_block(f32x16& x, const ScoreCall& c) {
       const float y = x[e] * x[e];
       x[e] *= fmaf(y, fmaf(y, fmaf(y, fmaf(y, c.p5[3], c.p5[2]), c.p5[1]), c.p5[0]), c.sl2);
     }
-  } else if (c.c2 <= WIDE_CAP) {
+  } else if (!c.wide) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) x[e] = fmaf(__builtin_amdgcn_rcpf(fast_exp2(x[e] * c.kx) + 1.f), -2.f * c.c2, c.c2);
   } else {
-    asm volatile("" : "+v"(x));          // (the block stays in its registers: left to itself this branch gets a second set)
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const float y = x[e] * x[e], t = fmaf(__builtin_amdgcn_rcpf(fast_exp2(x[e] * c.kx) + 1.f), -2.f * c.c2, c.c2);
-      x[e] = fabsf(x[e]) <= c.middling ? x[e] * fmaf(y, fmaf(y, fmaf(y, fmaf(y, c.p5[3], c.p5[2]), c.p5[1]), c.p5[0]), c.sl2) : t;
-      SCHED_FENCE;
+      asm volatile("" : "+v"(x));        // (the block stays in its registers: left to itself this branch gets a second set)
+      x[e] = cap_one(x[e], c);
     }
     asm volatile("" : "+v"(x));
   }
@@ -1198,8 +1206,6 @@ ScoreCall score_call(const ScoreArgs& a) {
   c.raw = 1.f / a.scale;
   c.nsplit = 1;
   if (a.cap > 0.f) {
-    static const double p3[2] = {-0.33322914994946595, 0.12846042911412406};
-    static const double p5[4] = {-0.33332247985930596, 0.13308098290393836, -0.05199433652233533, 0.015319205699263892};
     const double r = (double)a.scale / a.cap, c2 = (double)a.cap * 1.4426950408889634;
     c.c2 = (float)c2;
     c.ic2 = (float)(1.0 / c2);
@@ -1208,9 +1214,11 @@ ScoreCall score_call(const ScoreArgs& a) {
     c.middling = (float)(0.6 / r);
     double f = c2 * r * r * r;
     for (int i = 0; i < 4; ++i, f *= r * r) {
-      if (i < 2) c.p3[i] = (float)(p3[i] * f);
-      c.p5[i] = (float)(p5[i] * f);
+      if (i < 2) c.p3[i] = (float)(TANH2[i] * f);
+      c.p5[i] = (float)(TANH4[i] * f);
     }
+    c.wide = c.c2 > WIDE_CAP || fabsf(c.p5[3]) < FLT_MIN;
+    if (c.wide) c.small = c.middling = -1.f;
   }
   return c;
 }

@@ -9,10 +9,11 @@ import numpy as np
 import torch
 
 from oracle import score_oracle as sc
-from tests.score_util import F32, U
+from tests import score_util
+from tests.score_util import U
 
 
-def definition(p, head, at, n, prefix, exact_delta):
+def definition(p, head, at, n, prefix, exact_delta, F32):
     """One query head of one sequence -> {"o", "lse", "dq", "dk", "dv"}: (value, bound without the output's rounding)."""
     h, hkv, hd, o = p.h, p.hkv, p.hd, p.opts
     u = U[p.dtype] if p.dtype == "bf16" else 0.0
@@ -49,10 +50,10 @@ def definition(p, head, at, n, prefix, exact_delta):
     return r
 
 
-def compare(p, groups=None, exact_delta=(True, True), only=None, names=("o", "lse", "dq", "dk", "dv"), rows=None):
+def compare(p, groups=None, exact_delta=(True, True), only=None, names=("o", "lse", "dq", "dk", "dv"), rows=None, f32=score_util.F32):
     """p: tests.score_util.Attention after fwd and bwd.  groups: the KV heads to look at.  exact_delta: whether blocks that see few keys have their delta from
     the probabilities in dQ, in dK.  only: predicate on a sequence's length.  names: the results to look at.
-    rows: mask of the rows of o, lse and dq to look at."""
+    rows: mask of the rows of o, lse and dq to look at.  f32: in the place of F32, for scores beyond 100."""
     dev = lambda b: torch.tensor(b, device=p.q.device)
     flags = tuple(dev(p.dtype == "bf16" and f) for f in exact_delta)
     grp, hd, u = p.h // p.hkv, p.hd, U[p.dtype]
@@ -64,7 +65,7 @@ def compare(p, groups=None, exact_delta=(True, True), only=None, names=("o", "ls
             span = slice(at, at + n)
             look = torch.ones(n, dtype=torch.bool, device=p.q.device) if rows is None else dev(np.asarray(rows)[span])
             for j in range(g * grp, (g + 1) * grp):
-                r = definition(p, j, at, n, prefix, flags)
+                r = definition(p, j, at, n, prefix, flags, f32)
                 for name in kv:
                     kv[name] = r[name] if kv[name] is None else tuple(a + b for a, b in zip(kv[name], r[name]))
                 c = slice(j * hd, (j + 1) * hd)

@@ -77,3 +77,23 @@ def test_large_cap_beside_outliers(dtype, kernel_set, hd, cap):
     assert p.fwd(kernel_set) == 0 and p.bwd(kernel_set) == 0
     torch.cuda.synchronize()
     compare(p, exact_delta=(False, False), rows=~big)
+    compare(p, names=("lse",))                       # of the outliers too: a score near a large cap is off by no more of itself than any other
+
+
+@pytest.mark.parametrize("dtype,kernel_set", KERNELS)
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("scale,cap", [(1e-10, 5.0), (1e-20, 30.0), (1e-3, 300.0)])
+def test_small_scale_under_a_cap(dtype, kernel_set, hd, scale, cap):
+    """Queries and keys whose products are as large as the scale is small: scores of ordinary size, some of them near the cap.
+
+    Scores go up to two thirds of 300, past the 100 that F32 is for, so what fp32 may do to a P is counted: its exponent is made by at most 8 roundings
+    (scale, cap, sums, lse) of numbers up to 2 cap + log(rows), its product q.k by at most 64 of partial sums up to D = scale sum |q k|, each 2^-24."""
+    import torch
+    rows = 230
+    q, k, v, do = inputs(dtype, rows, 2, 1, hd, 139)
+    big = np.float32(2.0 ** round(np.log2(cap / 6.0 / scale / hd ** 0.5) / 2))                # scores of cap / 6 in the mean, up to two thirds of it
+    D = scale * float(big) ** 2 * max(float((np.abs(q[:, j * hd:(j + 1) * hd]) @ np.abs(k).T).max()) for j in range(2))
+    p = Attention(dtype, q * big, k * big, v, do, 2, 1, 1, scale=scale, cap=cap)
+    assert p.fwd(kernel_set) == 0 and p.bwd(kernel_set) == 0
+    torch.cuda.synchronize()
+    compare(p, exact_delta=(False, False), f32=2.0 ** -24 * (8 * (2 * cap + np.log(rows)) + 64 * D))
