@@ -129,7 +129,7 @@ int stage_kernel_attention_bwd_ws(int dtype, int b, int s, int h, int hkv, int h
  *   a query sees the keys of its own sequence: all of them, or (causal) those up to itself and the sequence's prefix.
  * Sequence i is rows seq_start[i] .. seq_start[i+1] - 1; empty ones are allowed.  Rows before the first or behind the last are not read,
  * and what belongs to them in the outputs is left as it was.  What a query does not see reaches none of its results, infinities and NaN
- * included (rows that hold them take a slow way). */
+ * included (rows that see one, or lie close to one behind the mask, are computed a second time: such a pass takes up to ten times as long). */
 typedef struct {
   int32_t dtype;
   int32_t rows;              /* >= 1, at most 2^23 */

@@ -184,35 +184,12 @@ __device__ __forceinline__ void cap_block(f32x16& x, const ScoreCall& c) {
 
 // ---- infinities and NaN behind the mask ----------------------------------------------------------------------------------------
 // The products of a tile take all of its rows, those that a query does not see with weight zero, which is right as long as they are finite:
-// zero times an infinity or NaN is NaN.  The loops carry no branch for it.  A row that comes out not finite is computed again, by its
-// wavefront alone and from the pairs that count only: a lane takes one key (query) of 64 at a time, then every 64th column of the sum.
-__device__ __forceinline__ float wave_max(float v) {
-  for (int x = 1; x < 64; x <<= 1) v = fmaxf(v, __shfl_xor(v, x));
-  return v;
-}
-__device__ __forceinline__ float wave_sum(float v) {
-  for (int x = 1; x < 64; x <<= 1) v += __shfl_xor(v, x);
-  return v;
-}
-template <int HD> __device__ __forceinline__ float dot_rows(const bf16* x, const bf16* y) {
-  float s = 0.f;
-#pragma unroll 1
-  for (int t = 0; t < HD; t += 8) {
-    const bf16x8 u = *reinterpret_cast<const bf16x8*>(x + t), v = *reinterpret_cast<const bf16x8*>(y + t);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) s = fmaf((float)u[e], (float)v[e], s);
-  }
-  return s;
-}
-// acc (columns lane, lane + 64) += sum over the n rows from p on of weight (lane x: row x's) times the row
-template <int HD> __device__ __forceinline__ void add_rows(float (&acc)[HD / 64], float weight, const bf16* p, int64_t ld, int n, int lane) {
-#pragma unroll 1
-  for (int x = 0; x < n; ++x) {
-    const float f = __shfl(weight, x);
-#pragma unroll
-    for (int k = 0; k < HD / 64; ++k) acc[k] = fmaf(f, (float)p[x * ld + lane + 64 * k], acc[k]);
-  }
-}
+// zero times an infinity or NaN is NaN.  The loops carry no branch for it.  Rows that come out not finite, though their own statistics are not
+// NaN, are computed again: 32 of them at a time by their wavefront alone, in blocks of 32 x 32 with operands straight from memory.  Only in blocks
+// that the mask cuts does a product go row by row and leave out the pairs that do not count, so a walk costs a few times what the tiles cost, at any
+// length.  (16384 rows, 8 heads of 128 on 2, causal, biased, forward + backward: 551 + 1724 us; with an infinity in the first value 3400 + 1990, a NaN in
+// the first query 580 + 8300, where one workgroup's walk is what all wait for, NaN everywhere 470 + 1760.)
+
 // the rows (of 32) of a wavefront's accumulators, one to a lane and its partner 32 further on, that hold an infinity or NaN
 template <int N> __device__ __forceinline__ unsigned odd_rows(const f32x16 (&acc)[N], bool live) {
   float t = 0.f;
@@ -235,109 +212,250 @@ __device__ __forceinline__ ScoreCall call_again() {
   for (unsigned i = 0; i < sizeof(ScoreCall) / 8; ++i) u.w[i] = p[i];
   return u.c;
 }
-__device__ __forceinline__ int lane_again() { return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)); }
-// forward, queries: block qb of 32 of the tile of BQ that `rank` is, head j
-template <int HD, int BQ> __device__ __forceinline__ void again_fwd(int j, int rank, int qb, unsigned rows) {
-  const ScoreCall c = call_again();
-  const ScoreArgs& a = c.a;
-  const int lane = lane_again(), g = j / (a.h / a.hkv);
-  const Work w = find_work<BQ, true>(c, rank, lane);
-  const int q0 = w.t * BQ + qb * 32;
-  const bf16* kp = (const bf16*)a.k + (int64_t)w.lo * a.ldk + g * HD;
-  const bf16* vp = (const bf16*)a.v + (int64_t)w.lo * a.ldv + g * HD;
-  const float slope = a.slope ? a.slope[j] : 0.f;
-#pragma unroll 1
-  for (; rows; rows &= rows - 1) {
-    const int q = q0 + __builtin_ctz(rows), end = a.causal ? max(q + 1, w.prefix) : w.len;
-    const bf16* qp = (const bf16*)a.q + (int64_t)(w.lo + q) * a.ldq + j * HD;
-    float m = -INFINITY, l = 0.f, acc[HD / 64] = {}, d;
-#pragma unroll 1
-    for (int u0 = 0; u0 < end; u0 += 64) {
-      const int u = u0 + lane;
-      const float s = u < end ? shaped(dot_rows<HD>(qp, kp + (int64_t)u * a.ldk), a, slope, q - u, d) : -INFINITY;
-      const float mn = fmaxf(m, wave_max(s)), sub = mn == -INFINITY ? 0.f : mn;
-      const float p = u < end ? expf(s - sub) : 0.f, alpha = expf(m - sub);
-      l = l * alpha + wave_sum(p);
-      m = mn;
-#pragma unroll
-      for (int k = 0; k < HD / 64; ++k) acc[k] *= alpha;
-      add_rows<HD>(acc, p, vp + (int64_t)u0 * a.ldv, a.ldv, min(64, end - u0), lane);
-    }
-#pragma unroll
-    for (int k = 0; k < HD / 64; ++k) ((bf16*)a.o)[(int64_t)(w.lo + q) * a.ldo + j * HD + lane + 64 * k] = (bf16)(acc[k] / l);
-    if (lane == 0 && a.lse) a.lse[(int64_t)j * a.rows + w.lo + q] = m + logf(l);
-  }
+// (inside the walks' loops, where the compiler would keep in registers what follows from the lane's number)
+__device__ __forceinline__ int lane_again() { 
+  int all = -1;
+  asm volatile("" : "+s"(all));
+  return __builtin_amdgcn_mbcnt_hi(all, __builtin_amdgcn_mbcnt_lo(all, 0));
 }
-template <int HD, int BQ> __device__ __forceinline__ void again_dq(int j, int rank, int qb, unsigned rows) {
-  const ScoreCall c = call_again();
-  const ScoreArgs& a = c.a;
-  const int lane = lane_again(), g = j / (a.h / a.hkv);
-  const Work w = find_work<BQ, true>(c, rank, lane);
-  const int q0 = w.t * BQ + qb * 32;
-  const bf16* kp = (const bf16*)a.k + (int64_t)w.lo * a.ldk + g * HD;
-  const bf16* vp = (const bf16*)a.v + (int64_t)w.lo * a.ldv + g * HD;
-  const float slope = a.slope ? a.slope[j] : 0.f;
-#pragma unroll 1
-  for (; rows; rows &= rows - 1) {
-    const int q = q0 + __builtin_ctz(rows), end = a.causal ? max(q + 1, w.prefix) : w.len;
-    const bf16* qp = (const bf16*)a.q + (int64_t)(w.lo + q) * a.ldq + j * HD;
-    const bf16* dp = (const bf16*)a.dout + (int64_t)(w.lo + q) * a.lddo + j * HD;
-    const float lse = a.lse[(int64_t)j * a.rows + w.lo + q], delta = a.delta[(int64_t)j * a.rows + w.lo + q];
-    float acc[HD / 64] = {};
-#pragma unroll 1
-    for (int u0 = 0; u0 < end; u0 += 64) {
-      const int u = u0 + lane;
-      float ds = 0.f, d;
-      if (u < end) {
-        const float s = shaped(dot_rows<HD>(qp, kp + (int64_t)u * a.ldk), a, slope, q - u, d);
-        ds = expf(s - lse) * (dot_rows<HD>(dp, vp + (int64_t)u * a.ldv) - delta) * d;
+
+// A product's score in units of log 2, and the cap's derivative there
+template <bool CAP> __device__ __forceinline__ float walk_score(float x, const ScoreCall& c, float& dcap) {
+  const float s = CAP ? cap_one(x, c) : x * c.sl2, t = CAP ? s * c.ic2 : 0.f;
+  dcap = fmaf(-t, t, 1.f);
+  return s;
+}
+// A matrix' rows of one sequence, columns of one head
+struct Rows { const bf16* p; int64_t ld; };
+// products over head_dim of rows x0 .. x0 + 31 of x (an accumulator's rows) with rows y0 .. y0 + 31 of y (its lanes); rows from n on are zeros
+template <int HD> __device__ __forceinline__ f32x16 walk_product(Rows x, int x0, Rows y, int y0, int n, int lane) {
+  f32x16 s;
+  zero(s);
+#pragma unroll HD == 128 ? 8 : 2
+  for (int kk = 0; kk < HD / 16; ++kk) s = MFMA(frag_rows_global(x.p, x.ld, x0, n, kk * 16, lane), frag_rows_global(y.p, y.ld, y0, n, kk * 16, lane), s);
+  return s;
+}
+// A walk's own rows are one to a lane, and each sees an interval of the others.
+struct Seen {
+  int from, to;                                        // within the sequence
+  __device__ __forceinline__ bool has(int x) const { return x >= from && x < to; }
+  // whether some own row does not see all rows of the sequence in the block from x0 on
+  __device__ __forceinline__ bool cuts(int x0, int own, int n) const { return __any(own < n && (from > x0 || to < min(x0 + 32, n))); }
+};
+// acc += x^T . w for the block of rows x0 .. of x: on the matrix cores, w rounded once, or (cut) row by row, each for the lanes that see it
+template <int HD> __device__ __forceinline__ void walk_add(f32x16 (&acc)[HD / 32], const f32x16& w, Seen see, bool cut, Rows x, int x0, int n, int lane) {
+  const int hf = lane >> 5;
+  auto stay = [&] {                                    // the sums stay in their registers: left to themselves the two ways get a set each
+#pragma unroll
+    for (int hb = 0; hb < HD / 32; ++hb) asm volatile("" : "+v"(acc[hb]));
+  };
+  stay();
+  if (!cut) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      bf16x8 wf;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) wf[e] = (bf16)w[h * 8 + e];
+#pragma unroll
+      for (int hb = 0; hb < HD / 32; ++hb) {
+        bf16x8 f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int row = x0 + acc_row(h * 8 + e, hf);
+          const bf16 v = x.p[(int64_t)min(row, n - 1) * x.ld + hb * 32 + (lane & 31)];
+          f[e] = row < n ? v : (bf16)0.f;
+        }
+        acc[hb] = MFMA(f, wf, acc[hb]);
       }
-      add_rows<HD>(acc, ds, kp + (int64_t)u0 * a.ldk, a.ldk, min(64, end - u0), lane);
+      SCHED_FENCE;                                     // few registers, so that the loops keep theirs
     }
+    stay();
+    return;
+  }
+#pragma unroll 1
+  for (int r = 0; r < min(32, n - x0); ++r) {
+    const int e = (r >> 3) * 4 + (r & 3), from = (lane & 31) + ((r >> 2) & 1) * 32;      // who holds that row's weight
+    const float f = __shfl(w[e], from);
+    const bool counts = see.has(x0 + r);
+    const bf16* xr = x.p + (int64_t)(x0 + r) * x.ld + hf * 4;
 #pragma unroll
-    for (int k = 0; k < HD / 64; ++k) ((bf16*)a.dq)[(int64_t)(w.lo + q) * a.lddq + j * HD + lane + 64 * k] = (bf16)(acc[k] * a.scale);
+    for (int hb = 0; hb < HD / 32; ++hb)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) {
+        const bf16x4 v = *reinterpret_cast<const bf16x4*>(xr + hb * 32 + q4 * 8);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[hb][q4 * 4 + i] = counts ? fmaf(f, (float)v[i], acc[hb][q4 * 4 + i]) : acc[hb][q4 * 4 + i];
+        SCHED_FENCE;
+      }
+    stay();
   }
 }
-// dV (dk = false) or dK: block kw of 32 keys of the tile of TQ that `rank` is, of the KV head and split bx
-template <int HD, int TQ, bool OWN_DELTA> __device__ __forceinline__ void again_dkv(int bx, int rank, int kw, bool dk, unsigned rows) {
+template <int HD> __device__ __forceinline__ void store_rows(const f32x16 (&acc)[HD / 32], float f, bf16* out, int hf) {
+#pragma unroll
+  for (int hb = 0; hb < HD / 32; ++hb)
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) {
+      bf16x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = (bf16)(acc[hb][q4 * 4 + e] * f);
+      *reinterpret_cast<bf16x4*>(out + hb * 32 + q4 * 8 + hf * 4) = v;
+    }
+}
+// forward: queries, block qb of 32 of the tile of BQ that `rank` is, head j
+template <int HD, int BQ, bool CAP> __device__ __forceinline__ void again_fwd(int j, int rank, int qb, unsigned rows) {
+  const ScoreCall c = call_again();
+  const ScoreArgs& a = c.a;
+  const int lane = lane_again(), hf = lane >> 5, g = j / (a.h / a.hkv);
+  const Work w = find_work<BQ, true>(c, rank, lane);
+  const int q0 = w.t * BQ + qb * 32, q = q0 + (lane & 31), vis = a.causal ? w.prefix : w.len, end = max(min(q0 + 32, w.len), vis);
+  const Rows Q{(const bf16*)a.q + (int64_t)w.lo * a.ldq + j * HD, a.ldq}, K{(const bf16*)a.k + (int64_t)w.lo * a.ldk + g * HD, a.ldk},
+      V{(const bf16*)a.v + (int64_t)w.lo * a.ldv + g * HD, a.ldv};
+  const float slope2 = a.slope ? a.slope[j] * LOG2E : 0.f;
+  f32x16 acc[HD / 32];
+#pragma unroll
+  for (int hb = 0; hb < HD / 32; ++hb) zero(acc[hb]);
+  float m = -INFINITY, l = 0.f;
+#pragma unroll 1
+  for (int k0 = 0; k0 < end; k0 += 32) {
+    const int lane = lane_again(), hf = lane >> 5, q = q0 + (lane & 31);
+    f32x16 s = walk_product<HD>(K, k0, Q, q0, w.len, lane);
+    const Seen see{0, min(max(a.causal ? q + 1 : 0, vis), w.len)};
+    float mx = -INFINITY, d;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      s[e] = fmaf(-slope2, fabsf((float)(k0 + acc_row(e, hf) - q)), walk_score<CAP>(s[e], c, d));
+      s[e] = see.has(k0 + acc_row(e, hf)) ? s[e] : -INFINITY;
+      mx = fmaxf(mx, s[e]);
+    }
+    const float mn = fmaxf(m, half_max(mx, hf)), sub = mn == -INFINITY ? 0.f : mn, alpha = fast_exp2(m - sub);
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) { s[e] = fast_exp2(s[e] - sub); sum += s[e]; }
+    l = l * alpha + half_sum(sum, hf);
+    m = mn;
+#pragma unroll
+    for (int hb = 0; hb < HD / 32; ++hb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[hb][e] *= alpha;
+    walk_add<HD>(acc, s, see, see.cuts(k0, q, w.len), V, k0, w.len, lane);
+  }
+  if (!(rows >> (lane & 31) & 1)) return;
+  store_rows<HD>(acc, 1.f / l, (bf16*)a.o + (int64_t)(w.lo + q) * a.ldo + j * HD, hf);
+  if (hf == 0 && a.lse) a.lse[(int64_t)j * a.rows + w.lo + q] = (m + log2f(l)) * LN2;
+}
+template <int HD, int BQ, bool CAP> __device__ __forceinline__ void again_dq(int j, int rank, int qb, unsigned rows) {
+  const ScoreCall c = call_again();
+  const ScoreArgs& a = c.a;
+  const int lane = lane_again(), hf = lane >> 5, g = j / (a.h / a.hkv);
+  const Work w = find_work<BQ, true>(c, rank, lane);
+  const int q0 = w.t * BQ + qb * 32, q = q0 + (lane & 31), vis = a.causal ? w.prefix : w.len, end = max(min(q0 + 32, w.len), vis);
+  const Rows Q{(const bf16*)a.q + (int64_t)w.lo * a.ldq + j * HD, a.ldq}, K{(const bf16*)a.k + (int64_t)w.lo * a.ldk + g * HD, a.ldk},
+      V{(const bf16*)a.v + (int64_t)w.lo * a.ldv + g * HD, a.ldv}, D{(const bf16*)a.dout + (int64_t)w.lo * a.lddo + j * HD, a.lddo};
+  const float slope2 = a.slope ? a.slope[j] * LOG2E : 0.f;
+  const int64_t at = (int64_t)j * a.rows + w.lo + min(q, w.len - 1);
+  const float lse2 = a.lse[at] * LOG2E, delta = a.delta[at];
+  f32x16 acc[HD / 32];
+#pragma unroll
+  for (int hb = 0; hb < HD / 32; ++hb) zero(acc[hb]);
+#pragma unroll 1
+  for (int k0 = 0; k0 < end; k0 += 32) {
+    const int lane = lane_again(), hf = lane >> 5, q = q0 + (lane & 31);
+    f32x16 s = walk_product<HD>(K, k0, Q, q0, w.len, lane);
+    const f32x16 dp = walk_product<HD>(V, k0, D, q0, w.len, lane);
+    const Seen see{0, min(max(a.causal ? q + 1 : 0, vis), w.len)};
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      float d;
+      const float x = walk_score<CAP>(s[e], c, d), p = fast_exp2(fmaf(-slope2, fabsf((float)(k0 + acc_row(e, hf) - q)), x - lse2));
+      s[e] = see.has(k0 + acc_row(e, hf)) ? p * ((dp[e] - delta) * d) : 0.f;
+    }
+    walk_add<HD>(acc, s, see, see.cuts(k0, q, w.len), K, k0, w.len, lane);
+  }
+  if (rows >> (lane & 31) & 1) store_rows<HD>(acc, a.scale, (bf16*)a.dq + (int64_t)(w.lo + q) * a.lddq + j * HD, hf);
+}
+// Which keys of block kw of 32 are seen by a query whose lse (dK: or delta) is NaN: so is every column of theirs, whatever is behind the mask.
+template <int TQ, bool OWN_DELTA> __device__ __forceinline__ unsigned settled_keys(int bx, int rank, int kw, bool dk) {
   const ScoreCall c = call_again();
   const ScoreArgs& a = c.a;
   const int lane = lane_again(), g = bx / c.nsplit, sp = bx % c.nsplit, grp = a.h / a.hkv / c.nsplit, j0 = g * (a.h / a.hkv) + sp * grp;
   const Work w = find_work<TQ, false>(c, rank, lane);
-  const int k0 = w.t * TQ + kw * 32, dkv = a.hkv * HD;
-  const int64_t ldout = dk ? a.lddk : a.lddv, ldpart = 2 * dkv;
-  bf16* out = (bf16*)(dk ? a.dk : a.dv) + (int64_t)w.lo * ldout + g * HD;
-  float* part = c.nsplit > 1 ? c.part + ((int64_t)sp * a.rows + w.lo) * ldpart + g * HD + (dk ? 0 : dkv) : nullptr;
+  const int k0 = w.t * TQ + kw * 32, key = k0 + (lane & 31);
+  int last = -1;
 #pragma unroll 1
-  for (; rows; rows &= rows - 1) {
-    const int u = k0 + __builtin_ctz(rows), begin = a.causal && u >= w.prefix ? u : 0;
-    const bf16* kp = (const bf16*)a.k + (int64_t)(w.lo + u) * a.ldk + g * HD;
-    const bf16* vp = (const bf16*)a.v + (int64_t)(w.lo + u) * a.ldv + g * HD;
-    float acc[HD / 64] = {};
+  for (int j = j0; j < j0 + grp; ++j)
 #pragma unroll 1
-    for (int j = j0; j < j0 + grp; ++j) {
-      const float slope = a.slope ? a.slope[j] : 0.f;
-      const bf16* qp = (const bf16*)a.q + (int64_t)w.lo * a.ldq + j * HD;
-      const bf16* dp = (const bf16*)a.dout + (int64_t)w.lo * a.lddo + j * HD;
-      const bf16* op = (const bf16*)a.o + (int64_t)w.lo * a.ldo + j * HD;
-#pragma unroll 1
-      for (int i0 = begin; i0 < w.len; i0 += 64) {
-        const int i = i0 + lane;
-        float f = 0.f, d;
-        if (i < w.len) {
-          const bf16* di = dp + (int64_t)i * a.lddo;
-          f = expf(shaped(dot_rows<HD>(qp + (int64_t)i * a.ldq, kp), a, slope, i - u, d) - a.lse[(int64_t)j * a.rows + w.lo + i]);
-          if (dk) f *= (dot_rows<HD>(di, vp) - (OWN_DELTA ? dot_rows<HD>(di, op + (int64_t)i * a.ldo) : a.delta[(int64_t)j * a.rows + w.lo + i])) * d;
-        }
-        add_rows<HD>(acc, f, dk ? qp + (int64_t)i0 * a.ldq : dp + (int64_t)i0 * a.lddo, dk ? a.ldq : a.lddo, min(64, w.len - i0), lane);
-      }
+    for (int i = lane; i < w.len; i += 64) {
+      const int64_t at = (int64_t)j * a.rows + w.lo + i;
+      const float x = dk && !OWN_DELTA ? a.lse[at] != a.lse[at] ? a.lse[at] : a.delta[at] : a.lse[at];
+      if (x != x) last = max(last, i);
     }
 #pragma unroll
-    for (int k = 0; k < HD / 64; ++k) {
-      const float v = dk ? acc[k] * a.scale : acc[k];
-      if (part) part[u * ldpart + lane + 64 * k] = v;
-      else out[u * ldout + lane + 64 * k] = (bf16)v;
+  for (int x = 1; x < 64; x <<= 1) last = max(last, __shfl_xor(last, x));
+  const uint64_t is = __ballot(key < w.len && (a.causal && key >= w.prefix ? key : 0) <= last);
+  return __builtin_amdgcn_readfirstlane((unsigned)(is | is >> 32));
+}
+// dV (dk = false) or dK: block kw of 32 keys of the tile of TQ that `rank` is, of the KV head and split bx
+template <int HD, int TQ, bool CAP, bool OWN_DELTA> __device__ __forceinline__ void again_dkv(int bx, int rank, int kw, bool dk, unsigned rows) {
+  const ScoreCall c = call_again();
+  const ScoreArgs& a = c.a;
+  const int lane = lane_again(), hf = lane >> 5, g = bx / c.nsplit, sp = bx % c.nsplit, grp = a.h / a.hkv / c.nsplit, j0 = g * (a.h / a.hkv) + sp * grp;
+  const Work w = find_work<TQ, false>(c, rank, lane);
+  const int k0 = w.t * TQ + kw * 32, key = k0 + (lane & 31), dkv = a.hkv * HD;
+  const int first = a.causal && k0 >= w.prefix ? k0 : 0;             // the first query that sees a key of the block
+  const Rows K{(const bf16*)a.k + (int64_t)w.lo * a.ldk + g * HD, a.ldk}, V{(const bf16*)a.v + (int64_t)w.lo * a.ldv + g * HD, a.ldv};
+  f32x16 acc[HD / 32];
+#pragma unroll
+  for (int hb = 0; hb < HD / 32; ++hb) zero(acc[hb]);
+#pragma unroll 1
+  for (int j = j0; j < j0 + grp; ++j) {
+    const float slope2 = a.slope ? a.slope[j] * LOG2E : 0.f;
+    const Rows Q{(const bf16*)a.q + (int64_t)w.lo * a.ldq + j * HD, a.ldq}, D{(const bf16*)a.dout + (int64_t)w.lo * a.lddo + j * HD, a.lddo};
+#pragma unroll 1
+    for (int i0 = first; i0 < w.len; i0 += 32) {
+      const int lane = lane_again(), hf = lane >> 5, key = k0 + (lane & 31);
+      const int i = min(i0 + (lane & 31), w.len - 1);                // the query whose statistics the lane fetches
+      const int64_t at = (int64_t)j * a.rows + w.lo + i;
+      const float lse2 = a.lse[at] * LOG2E;
+      float delta = 0.f;
+      if (dk && OWN_DELTA) {
+        const bf16* o = (const bf16*)a.o + (int64_t)(w.lo + i) * a.ldo + j * HD + hf * (HD / 2);
+        const bf16* d = D.p + i * D.ld + hf * (HD / 2);
+#pragma unroll 1
+        for (int x = 0; x < HD / 2; x += 8) {
+          const bf16x8 u = *reinterpret_cast<const bf16x8*>(o + x), v = *reinterpret_cast<const bf16x8*>(d + x);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) delta = fmaf((float)u[e], (float)v[e], delta);
+        }
+        delta = half_sum(delta, hf);
+      } else if (dk) delta = a.delta[at];
+      f32x16 s = walk_product<HD>(Q, i0, K, k0, w.len, lane), dp;
+      if (dk) dp = walk_product<HD>(D, i0, V, k0, w.len, lane);
+      const Seen see{a.causal && key >= w.prefix ? key : 0, w.len};
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        float d;
+        const float x = walk_score<CAP>(s[e], c, d), le = __shfl(lse2, acc_row(e, hf)), de = __shfl(delta, acc_row(e, hf));
+        const float p = fast_exp2(fmaf(-slope2, fabsf((float)(i0 + acc_row(e, hf) - key)), x - le));
+        s[e] = !see.has(i0 + acc_row(e, hf)) ? 0.f : dk ? p * d * (dp[e] - de) : p;
+        if (e % 4 == 3) SCHED_FENCE;
+      }
+      walk_add<HD>(acc, s, see, see.cuts(i0, key, w.len), dk ? Q : D, i0, w.len, lane);
     }
+  }
+  if (!(rows >> (lane & 31) & 1)) return;
+  const float osc = dk ? a.scale : 1.f;
+  if (c.nsplit == 1) store_rows<HD>(acc, osc, dk ? (bf16*)a.dk + (int64_t)(w.lo + key) * a.lddk + g * HD : (bf16*)a.dv + (int64_t)(w.lo + key) * a.lddv + g * HD, hf);
+  else {
+    float* out = c.part + ((int64_t)sp * a.rows + w.lo + key) * (2 * dkv) + g * HD + (dk ? 0 : dkv);
+#pragma unroll
+    for (int hb = 0; hb < HD / 32; ++hb)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) {
+        f32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = acc[hb][q4 * 4 + e] * osc;
+        *reinterpret_cast<f32x4*>(out + hb * 32 + q4 * 8 + hf * 4) = v;
+      }
   }
 }
 
@@ -547,9 +665,10 @@ __global__ __launch_bounds__(NT, KS == 4 && HD == 64 ? 4 : 2) void score_fwd_ker
       m = mn;
     }
   }
-  // Exponents are taken from the rounded maximum m, which is off by up to 2^-24 of itself: beyond 2^30 that alone may overflow the sums, or leave nothing of them.
-  if (l < 1e-30f) o[0][0] = INFINITY;
-  const unsigned odd = odd_rows(o, row.q < w.len);
+  // Exponents are taken from the rounded maximum m, which is off by up to 2^-24 of itself: beyond 1e9 that alone may overflow the sums, or leave nothing of
+  // them, and the row is computed again.  Below, a sum that is NaN is the row's own: every column of it is, whatever is behind the mask.
+  if (fabsf(m) > 1e9f && m != -FLT_MAX) { l = 1.f; o[0][0] = INFINITY; }
+  const unsigned odd = odd_rows(o, row.q < w.len && l == l);
   if (row.q < w.len && !(odd >> (lane & 31) & 1)) {
     const float inv = 1.f / l;
     bf16* orow = (bf16*)a.o + (int64_t)(w.lo + row.q) * a.ldo + j * HD;
@@ -564,7 +683,7 @@ __global__ __launch_bounds__(NT, KS == 4 && HD == 64 ? 4 : 2) void score_fwd_ker
       }
     if (hf == 0 && a.lse) a.lse[(int64_t)j * a.rows + w.lo + row.q] = (m + log2f(l)) * LN2;
   }
-  if (__builtin_expect(odd != 0, 0)) again_fwd<HD, BQ>(j, blockIdx.x / a.h, qb, odd);
+  if (__builtin_expect(odd != 0, 0)) again_fwd<HD, BQ, CAP>(j, blockIdx.x / a.h, qb, odd);
 }
 
 // ---- backward ---------------------------------------------------------------------------------------------------------------
@@ -815,7 +934,7 @@ __device__ __forceinline__ void dq_workgroup(const ScoreCall& c, lds_char* lds, 
         }
     }
   }
-  const unsigned odd = odd_rows(dq, row.q < w.len);
+  const unsigned odd = odd_rows(dq, row.q < w.len && lse2 == lse2 && dl == dl);      // (one of them is NaN: so is every column of the row)
   if (row.q < w.len && !(odd >> (lane & 31) & 1)) {
     bf16* out = (bf16*)a.dq + (int64_t)(w.lo + row.q) * a.lddq + j * HD;
 #pragma unroll
@@ -828,7 +947,7 @@ __device__ __forceinline__ void dq_workgroup(const ScoreCall& c, lds_char* lds, 
         *reinterpret_cast<bf16x4*>(out + hb * 32 + q4 * 8 + hf * 4) = v;
       }
   }
-  if (__builtin_expect(odd != 0, 0)) again_dq<HD, BQ>(j, rank, qb, odd);
+  if (__builtin_expect(odd != 0, 0)) again_dq<HD, BQ, CAP>(j, rank, qb, odd);
 }
 template <int HD, int NT, int KS, bool CAP>
 __global__ __launch_bounds__(NT, 2) void score_dq_kernel(ScoreCall c) {
@@ -1075,7 +1194,8 @@ __device__ __forceinline__ void dkv_workgroup(const ScoreCall& c, lds_char* lds,
       }
   }
 
-  const unsigned odd = odd_rows(acc, key < w.len);
+  unsigned odd = odd_rows(acc, key < w.len);
+  if (__builtin_expect(odd != 0, 0)) odd &= ~settled_keys<TQ, OWN_DELTA>(bx, rank, kw, role != 0);
   if (key < w.len && !(odd >> (lane & 31) & 1)) {             // role 0 holds dV, role 1 dK (still to be scaled)
     const float osc = role ? a.scale : 1.f;
     if (c.nsplit == 1) {
@@ -1102,7 +1222,7 @@ __device__ __forceinline__ void dkv_workgroup(const ScoreCall& c, lds_char* lds,
         }
     }
   }
-  if (__builtin_expect(odd != 0, 0)) again_dkv<HD, TQ, OWN_DELTA>(bx, rank, kw, role != 0, odd);
+  if (__builtin_expect(odd != 0, 0)) again_dkv<HD, TQ, CAP, OWN_DELTA>(bx, rank, kw, role != 0, odd);
 }
 template <int HD, int TQ, int QS, bool CAP>
 __global__ __launch_bounds__(TQ * 4 * QS, 2) void score_dkv_kernel(ScoreCall c) {
