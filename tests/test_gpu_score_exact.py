@@ -6,7 +6,7 @@ import pytest
 from tests.gpu_util import rnd
 from tests.score_exact import compare
 from tests.score_util import Attention
-from tests.test_gpu_score_attention import KERNELS, inputs
+from tests.test_gpu_score_attention import KERNELS, inputs, slopes
 
 pytestmark = pytest.mark.gpu
 
@@ -97,3 +97,37 @@ def test_small_scale_under_a_cap(dtype, kernel_set, hd, scale, cap):
     assert p.fwd(kernel_set) == 0 and p.bwd(kernel_set) == 0
     torch.cuda.synchronize()
     compare(p, exact_delta=(False, False), f32=2.0 ** -24 * (8 * (2 * cap + np.log(rows)) + 64 * D))
+
+
+def packed(lens, behind=0):
+    return dict(starts=np.concatenate(([0], np.cumsum(lens))), n_seq=len(lens)), int(np.sum(lens)) + behind
+
+
+# what the rules choose where they choose it: every kernel at sizes it is made for, two KV heads with all of their query heads
+SIZES = {
+    "wide, capped": ("bf16", 4096, 32, 8, 128, 3.0, dict(cap=50.0)),
+    "long, biased": ("bf16", 16384, 8, 2, 128, 1.0, dict(slopes=slopes(8))),
+    "documents": ("bf16", [700, 50, 1259, 90, 1100, 400, 33, 1000, 820, 610, 750, 128, 1156], 16, 2, 128, 1.0, dict(behind=96)),
+    "prefixes": ("bf16", [900, 100, 1300, 64, 700, 500, 532], 40, 40, 128, 1.0, dict(prefixes=[300, 60, 800, 10, 0, 490, 100])),
+    "narrow heads in one launch": ("bf16", 2331, 12, 12, 64, 1.0, dict(n_seq=3, slopes=slopes(12))),
+    "narrow heads": ("bf16", 8192, 12, 4, 64, 1.0, {}),
+    "many short": ("bf16", [20 + 7 * (i % 23) for i in range(100)], 16, 16, 64, 2.0, dict(cap=30.0)),
+    "full": ("bf16", 4096, 16, 16, 128, 1.0, dict(n_seq=2, causal=0)),
+    "few heads": ("bf16", 5000, 4, 4, 128, 1.0, {}),
+    "fp32": ("fp32", 1500, 16, 4, 128, 2.0, dict(cap=30.0, slopes=slopes(16), prefixes=[200])),
+}
+
+
+@pytest.mark.parametrize("name", list(SIZES))
+def test_at_the_sizes_of_the_rules(name):
+    import torch
+    dtype, rows, h, hkv, hd, spread, opts = SIZES[name]
+    opts = dict(opts)
+    if not isinstance(rows, int):
+        more, rows = packed(rows, opts.pop("behind", 0))
+        opts.update(more)
+    q, k, v, do = inputs(dtype, rows, h, hkv, hd, 157, spread ** 0.5)
+    p = Attention(dtype, q, k, v, do, h, hkv, opts.pop("causal", 1), **opts)
+    assert p.fwd() == 0 and p.bwd() == 0
+    torch.cuda.synchronize()
+    compare(p, groups=sorted({0, hkv - 1}), exact_delta=(True, "starts" in opts))
