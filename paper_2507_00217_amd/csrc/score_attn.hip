@@ -1281,15 +1281,18 @@ int mean_len(const ScoreArgs& a) { return a.rows / a.n_seq; }
 
 enum Shape { SHAPE_WIDE = 1, SHAPE_NARROW = 2, SHAPE_SPLIT = 3, SHAPE_SPLIT4 = 4 };
 // Forward and dQ: 8 wavefronts x 32 queries, 4 x 32, or 64 queries whose keys 2 or 4 wavefronts share.
-// WIDE only for long equal sequences: it reads every K/V tile once for twice the queries, but its last tiles are twice as much masked
-// (WIDE / NARROW: forward of head_dim 128 32 heads x 4096 149 / 158, 32 x 4 x 2048 228 / 187, 16 x 13 packed in 8192 71 / 62; dQ 189 / 202, 270 / 244,
-// 92 / 84), and in the forward of head_dim 64 never, where NARROW has more wavefronts to a CU (32 x 4096 118 / 90).
+// WIDE reads every K/V tile once for twice the queries, but its last tiles are twice as much masked and its last round of the chip (one workgroup to a
+// CU) leaves twice as much idle: for equal sequences where that round is nearly full, or there are so many rows that it weighs little (WIDE / NARROW,
+// forward and dQ's difference, head_dim 128: up to two rounds, 40 heads x 2800 97 / 99, -6, 32 x 4096 145 / 154, -9, 20 x 6000 197 / 205, -11, 16 x 8192 269 / 291,
+// -27; a little more than two, 40 x 3400 144 / 139, +7, 40 x 3800 171 / 163, +5, 32 x 4500 183 / 180, +3; three and more, 32 x 2 x 3000 170 / 164, +1, 32 x 2 x 4096
+// 285 / 282, -3, 16 x 2 x 6500 354 / 346, -20, 16 x 2 x 8192 523 / 530, -36).  Not for packed ones (16 x 13 in 8192 71 / 62), nor in the
+// forward of head_dim 64, where NARROW has more wavefronts to a CU (32 x 4096 118 / 90).
 // SPLIT below about a round and a half of NARROW (SPLIT / NARROW, head_dim 128: 16 x 3000 58 / 64, 40 x 1500 47 / 40), SPLIT4 for few workgroups
 // with long chains (SPLIT4 / SPLIT: 4 x 5000 60 / 72, 16 x 2048 45 / 36; head_dim 64, whose workgroups sit two to a CU, 16 x 2048 21.5 / 24.7).
 Shape q_shape(const ScoreArgs& a, int width, bool forward) {
   if (width >= 1 && width <= 4) return (Shape)width;
-  const bool long_equal = !a.seq_start && mean_len(a) >= 4096;
-  if (long_equal && !(forward && a.hd == 64) && slots(a, 256) * a.h >= 400) return SHAPE_WIDE;
+  const int64_t wide = slots(a, 256) * a.h;
+  if (!a.seq_start && !(forward && a.hd == 64) && wide >= 400 && ((wide <= 512 && mean_len(a) >= 2500) || mean_len(a) >= 6000)) return SHAPE_WIDE;
   if (slots(a, 128) * a.h >= (forward && a.hd == 64 ? 512 : 450)) return SHAPE_NARROW;
   return forward && slots(a, 64) * a.h <= (a.hd == 64 ? 512 : 384) && mean_len(a) >= 1000 ? SHAPE_SPLIT4 : SHAPE_SPLIT;
 }
@@ -1412,14 +1415,15 @@ hipError_t bwd_t(const ScoreCall& c, int width, hipStream_t s) {
   const int len = mean_len(a);
   // Both passes in one launch while their workgroups (64 queries, 64 keys) number little more than what is resident; with two pairs of
   // wavefronts up to one to a CU, or with long causal chains somewhat more (one launch / two: head_dim 128 8 x 1024 33 / 46, 4 x 5000 157 / 175, 16 x
-  // 2048 115 / 102), with one pair (head_dim 64: three to a CU) for shorter sequences (12 x 3 x 777 32 / 33, 32 x 700 26 / 29, 4 x 5000 140 / 128).
+  // 2048 115 / 102), with one pair (head_dim 64: three to a CU) for shorter sequences (workgroups: 880, 40 x 700 27 / 31; 936, 12 x 3 x 777 33.5 / 33.9; 1024, 32 x
+  // 1000 36 / 38; 1248, 16 x 3 x 777 39 / 42; 1408, 32 x 1400 60 / 59; 1000, 20 x 1600 55 / 53; 4 x 5000 140 / 128).
   // Not for sequences of up to DELTA_KEYS rows: the dK/dV half cannot wait for the dQ half's delta and takes its own from the rounded O.  Nor for packed
   // ones, whose lengths only the device knows: any of them may be that short, whatever their mean.  (That costs small packed batches time: one launch / two,
   // head_dim 128 8 x 3 packed in 600 18 / 26, 4 x 4 in 2048 31 / 41, 4 x 3 in 4000 79 / 79; head_dim 64 8 x 3 in 600 13 / 19, 12 x 3 in 2331 45 / 50.)
   const bool longer = !a.seq_start && len > DELTA_KEYS;
   const bool two_pairs = longer && (2 * total <= RESIDENT || (a.causal && ((total <= RESIDENT && len > 320) || (total <= 700 && len > 1500))));
   if (width == 6 || (width == 0 && two_pairs)) return bwd_fused_launch<HD, 4, 2, CAP>(c, s);
-  const bool one_pair = longer && (HD == 128 ? a.causal && len <= 320 && total <= RESIDENT : len <= 1500 && total <= 960);
+  const bool one_pair = longer && (HD == 128 ? a.causal && len <= 320 && total <= RESIDENT : len <= 1500 && total <= 1280);
   if (width == 5 || (width == 0 && one_pair)) return bwd_fused_launch<HD, 2, 1, CAP>(c, s);
   hipError_t e;      // dQ first: it also leaves delta in the scratch for the dK/dV pass
   switch (q_shape(a, width, false)) {
