@@ -4,7 +4,9 @@
  * The same HIP kernels that stage_forward / stage_backward_input /
  * stage_backward_weight launch, callable one at a time so that each step of
  * the F / B / W path (paper section 3.1, Appendix B) can be checked against
- * its definition and timed against its roofline in isolation.
+ * its definition and timed against its roofline in isolation; and single
+ * operators around a layer's attention block that no stage calls
+ * (stage_kernel_rope_axes, _qk_norm_rope_*, _score_attention_*).
  *
  * All data pointers are DEVICE memory owned by the caller; nothing is
  * allocated, work is enqueued on `hip_stream` (hipStream_t, NULL = default
@@ -148,7 +150,8 @@ typedef struct {
 
 /* q, o: [rows, h*hd]; k, v: [rows, hkv*hd], each with a row stride of its own (elements), so that they may be columns of one buffer.
  * o overlaps no input.  lse: [h, rows] fp32, or NULL when there is no backward.  The tuned kernels want 16-byte aligned pointers and strides; what they do
- * not take, the plain kernels do.  kernel_set as for the attention entries above (in fp32: 0 and 1). */
+ * not take, the plain kernels do.  kernel_set as for the attention entries above (in fp32: 0 and 1; the one-launch backward of 6 and 7
+ * takes dk's row sums of dout * o from o as it is stored, which short sequences lose precision by, so that 0 never takes it for packed ones). */
 int stage_kernel_score_attention_fwd(const stage_score_attention_t* p, const void* q, int64_t ldq, const void* k, int64_t ldk,
                                      const void* v, int64_t ldv, void* o, int64_t ldo, float* lse, int kernel_set, void* hip_stream);
 /* The probabilities are exp(s - lse) again, with s and lse as fp32 numbers: scores of size S leave them an error of S * 2^-23 of themselves.

@@ -539,7 +539,8 @@ __device__ __forceinline__ void fwd_tile(lds_char* lds, const FragOff<HD>& fo, c
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[n][e] = fast_exp2(s[n][e]);
   }
-  // P is rounded to bf16 for its product; the row's sum is of what it was before
+  // P is rounded to bf16 for its product, since the matrix cores take both operands in one type (so are P and dS in the backward, once each; every such
+  // rounding adds to a result's error about what its own does); the row's sum is of what it was before
   bf16x8 pf[NC][2];
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -710,7 +711,7 @@ __device__ __forceinline__ void probs_block(f32x16& s, const ScoreCall& c, int k
 
 // delta = rowsum(dO * O) is what dS = P (dP - delta) subtracts, and where a row's weight sits on few keys it is nearly all of dP: the rounding of
 // O to bf16 is then no longer small against what is left (dQ and dK of sequences of 8 rows, scores of 3 in the mean, off by 5.8e-3 of their norm,
-// of 4096 rows by 3.1e-3, where the roundings of dS and of the results alone are 2.4e-3).  So a block of 32 queries that sees no more than the
+// of 4096 rows by 3.0e-3, where the roundings of dS and of the results alone are 2.35e-3).  So a block of 32 queries that sees no more than the
 // DELTA_KEYS keys that are in LDS before the loop starts gets delta as the sum of P dP, which costs it their two products once more.
 constexpr int DELTA_KEYS = 2 * TK;
 template <int HD, int BUF, bool CAP>
