@@ -1286,7 +1286,8 @@ enum Shape { SHAPE_WIDE = 1, SHAPE_NARROW = 2, SHAPE_SPLIT = 3, SHAPE_SPLIT4 = 4
 // CU) leaves twice as much idle: for equal sequences where that round is nearly full, or there are so many rows that it weighs little (WIDE / NARROW,
 // forward and dQ's difference, head_dim 128: up to two rounds, 40 heads x 2800 97 / 99, -6, 32 x 4096 145 / 154, -9, 20 x 6000 197 / 205, -11, 16 x 8192 269 / 291,
 // -27; a little more than two, 40 x 3400 144 / 139, +7, 40 x 3800 171 / 163, +5, 32 x 4500 183 / 180, +3; three and more, 32 x 2 x 3000 170 / 164, +1, 32 x 2 x 4096
-// 285 / 282, -3, 16 x 2 x 6500 354 / 346, -20, 16 x 2 x 8192 523 / 530, -36).  Not for packed ones (16 x 13 in 8192 71 / 62), nor in the
+// 285 / 282, -3, 16 x 2 x 6500 354 / 346, -20, 16 x 2 x 8192 523 / 530, -36; without a causal mask 40 x 2560 156 / 162, -9, 36 x 3500 221 / 231, -22, but 40 x 3800
+// 339 / 305, +34, 32 x 4500 392 / 352, +42).  Not for packed ones (16 x 13 in 8192 71 / 62), nor in the
 // forward of head_dim 64, where NARROW has more wavefronts to a CU (32 x 4096 118 / 90).
 // SPLIT below about a round and a half of NARROW (SPLIT / NARROW, head_dim 128: 16 x 3000 58 / 64, 40 x 1500 47 / 40), SPLIT4 for few workgroups
 // with long chains (SPLIT4 / SPLIT: 4 x 5000 60 / 72, 16 x 2048 45 / 36; head_dim 64, whose workgroups sit two to a CU, 16 x 2048 21.5 / 24.7).
