@@ -43,7 +43,8 @@ __device__ __forceinline__ int keys_end(const ScoreArgs& a, const SeqSpan& s, in
 // The queries that see key `row` are [queries_begin, s.hi).
 __device__ __forceinline__ int queries_begin(const ScoreArgs& a, const SeqSpan& s, int row) { return a.causal && row >= s.lo + s.prefix ? row : s.lo; }
 
-// Score of a product x, exact to a few roundings (the bf16 kernels have faster forms), and the cap's derivative there.
+// Score of a product x, exact to a few roundings (the bf16 kernels have faster forms), and the cap's derivative there: 1 - t^2 in fp32, here as there, so
+// 2^-23 off, and of a score of eight caps, whose derivative is that small itself, next to nothing is left.
 __device__ __forceinline__ float shaped(float x, const ScoreArgs& a, float slope, int dist, float& dcap) {
   float s = x * a.scale;
   dcap = 1.f;
