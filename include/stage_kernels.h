@@ -5,8 +5,9 @@
  * stage_backward_weight launch, callable one at a time so that each step of
  * the F / B / W path (paper section 3.1, Appendix B) can be checked against
  * its definition and timed against its roofline in isolation; and single
- * operators around a layer's attention block that no stage calls
- * (stage_kernel_rope_axes, _qk_norm_rope_*, _score_attention_*).
+ * operators that no stage calls: around a layer's attention block
+ * (stage_kernel_rope_axes, _qk_norm_rope_*, _score_attention_*), at the end of the
+ * last stage (_token_logprob_*) and between iterations (_grad_*, _adamw).
  *
  * All data pointers are DEVICE memory owned by the caller; nothing is
  * allocated, work is enqueued on `hip_stream` (hipStream_t, NULL = default
@@ -163,6 +164,78 @@ int stage_kernel_score_attention_bwd(const stage_score_attention_t* p, const voi
                                      size_t scratch_bytes, int kernel_set, void* hip_stream);
 /* 0 for a p that the two entries refuse. */
 size_t stage_kernel_score_attention_bwd_scratch_bytes(const stage_score_attention_t* p);
+
+/* What rows of logits say of their tokens, and the gradient of it: where the output head's product ends and the last stage's dY begins.
+ * With m the largest logit x_j of a row and S = sum over j of exp(scale * (x_j - m)):
+ *   logp_j = scale * (x_j - m) - ln S,   p_j = exp(logp_j),   lse = scale * m + ln S,   H = -sum of p_j logp_j.
+ * A logit of -inf is a token that cannot be: p_j = 0.  A row of nothing else has log probabilities of -inf, H = 0 and a gradient of zeros; one with a NaN
+ * or +inf has NaN for its log probabilities, ln S, H and gradient, and -1 for its alternatives. */
+typedef struct {
+  int32_t dtype;             /* of the logits and their gradient */
+  int32_t rows;              /* >= 1, at most 2^23 */
+  int32_t vocab;             /* >= 1, at most 2^24 */
+  int32_t top;               /* alternatives of each row: 0 .. 64, at most vocab */
+  float scale;               /* 1e-30 .. 1e30 (one over a temperature), or 0 for 1 */
+  const int32_t* target;     /* device, [rows]: the row's token; outside 0 .. vocab - 1 the row has none; or NULL: no row has one */
+} stage_token_logprob_t;
+
+/* logits: [rows, vocab] with a row stride ld (elements), aligned to an element.  fp32 outputs, each NULL where it is not wanted: logp [rows] of the
+ * rows' tokens (0 for a row that has none), stats [rows, 2] = (m, ln S) for the backward, entropy [rows] = H, and, for top > 0, the alternatives: the
+ * largest logits in descending order, of equal ones the lowest index first, as top_id [rows, top] and their top_logp [rows, top].
+ * No output overlaps an input or another output.  scratch: stage_kernel_token_logprob_scratch_bytes(p) bytes, 16-byte aligned (NULL where that is 0), not
+ * shared by calls on different streams.  kernel_set: 0 and 1 as above, 2 = every row in several parts wherever it has columns for two.
+ * Results are the same bits from call to call. */
+int stage_kernel_token_logprob_fwd(const stage_token_logprob_t* p, const void* logits, int64_t ld, float* logp, float* stats, float* entropy,
+                                   int32_t* top_id, float* top_logp, void* scratch, size_t scratch_bytes, int kernel_set, void* hip_stream);
+/* dlogits [rows, vocab] (row stride ldd) from the rows' gradients with respect to logp (ignored where a row has no token), H and lse, each [rows] fp32 or
+ * NULL for zeros, not all NULL (dlogp: only with targets; dentropy: only with entropy, which is H from the forward):
+ *   dlogits_j = scale * (p_j * (dlse - dlogp - dentropy * (logp_j + H)) + dlogp * [j is the row's token]).
+ * A row whose three are all zero gets zeros, whatever its logits are.  dlogits may be logits (with ldd = ld); otherwise they must not overlap.
+ * stats and entropy may be those of a wider vocabulary of which logits are some columns (m the largest of all, S over all), as on each of several GPUs
+ * that a vocabulary is spread over; a row whose token lies on another one then has dlse - dlogp for its dlse. */
+int stage_kernel_token_logprob_bwd(const stage_token_logprob_t* p, const void* logits, int64_t ld, const float* stats, const float* entropy,
+                                   const float* dlogp, const float* dentropy, const float* dlse, void* dlogits, int64_t ldd, int kernel_set,
+                                   void* hip_stream);
+/* Both in one call, for gradients that are known before (those of a loss that is a weighted sum): the logits are read once where a row fits a workgroup's registers.
+ * stats is not NULL, nor entropy with dentropy; otherwise as above. */
+int stage_kernel_token_logprob_grad(const stage_token_logprob_t* p, const void* logits, int64_t ld, const float* dlogp, const float* dentropy,
+                                    const float* dlse, void* dlogits, int64_t ldd, float* logp, float* stats, float* entropy, int32_t* top_id,
+                                    float* top_logp, void* scratch, size_t scratch_bytes, int kernel_set, void* hip_stream);
+/* 0 for a p that the entries refuse. */
+size_t stage_kernel_token_logprob_scratch_bytes(const stage_token_logprob_t* p);
+
+/* Gradients of many tensors at once.  Array arguments are HOST arrays of length n, read before the call returns; the pointers in them are device pointers,
+ * aligned to an element; tensors of size 0 are skipped (their pointers are not looked at), others have at most 2^40 elements.  Tensors are fastest where
+ * the arrays' pointers of a tensor lie equally far behind 16-byte boundaries, counted in elements.
+ *
+ * sumsq[0] (device, 8-byte aligned) = the sum of the squares of all elements of all grad[i] [size[i]], formed in 64 bits in a fixed order; with add != 0 what
+ * sumsq holds is added to it (gradients of another type, or what a collective brought from other stages).  scratch:
+ * stage_kernel_grad_sumsq_scratch_bytes() bytes, 16-byte aligned, not shared by calls on different streams. */
+int stage_kernel_grad_sumsq(int dtype, int n, const int64_t* size, const void* const* grad, int add, double* sumsq, void* scratch,
+                            size_t scratch_bytes, void* hip_stream);
+size_t stage_kernel_grad_sumsq_scratch_bytes(void);
+/* out[i] = grad[i] * min(1, max_norm / sqrt(sumsq)), each rounded once; out[i] may be grad[i], otherwise they overlap nothing.  max_norm is finite, > 0.
+ * norm (device, or NULL): receives sqrt(sumsq).  Where sumsq is not finite (a gradient is not) the gradients stay as they are. */
+int stage_kernel_grad_clip(int dtype, int n, const int64_t* size, const void* const* grad, void* const* out, const double* sumsq, float max_norm,
+                           float* norm, void* hip_stream);
+
+/* One AdamW step on many tensors (lists as above), g = the gradient times the factor of stage_kernel_grad_clip where sumsq is given:
+ *   m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2;
+ *   w = w - lr * (weight_decay * w + (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)). */
+typedef struct {
+  int32_t dtype;             /* of the weights w */
+  int32_t grad_dtype;
+  double lr, beta1, beta2, eps, weight_decay;      /* all >= 0 and finite; betas < 1 */
+  const double* sumsq;       /* device, or NULL: gradients are taken as they are (and have to be finite) */
+  const float* lr_now;       /* device, or NULL: read in the place of lr, so that a captured call can be replayed with another */
+  const int32_t* step_now;   /* device, or NULL: read in the place of step */
+  int32_t step;              /* >= 1 (below that, a step_now counts as 1) */
+  float max_norm;            /* with sumsq: finite, > 0 */
+} stage_adamw_t;
+/* bf16 weights: master[i] are their fp32 values, which are updated, and w[i] their rounding; w is not read.  fp32 weights: w is updated, master is NULL.
+ * m, v: fp32.  No two tensors overlap.  Where sumsq is not finite nothing is changed: the step is left out. */
+int stage_kernel_adamw(const stage_adamw_t* p, int n, const int64_t* size, void* const* w, float* const* master, float* const* m, float* const* v,
+                       const void* const* grad, void* hip_stream);
 
 /* stats: [rows, 2] fp32 (mean, rstd). beta ignored for RMSNorm. */
 int stage_kernel_norm_fwd(int dtype, int norm, int rows, int d, float eps, const void* x, const void* gamma,

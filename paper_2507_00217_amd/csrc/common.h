@@ -99,6 +99,34 @@ struct HeadNormArgs {
   float* partial;                // head_norm_partial_bytes(hd) bytes
 };
 
+// Log probabilities of the rows' tokens, entropy and likeliest alternatives, and the logits' gradient (stage_kernel_token_logprob_*)
+constexpr int LOGPROB_MAX_TOP = 64;
+struct LogprobArgs {
+  int rows, vocab, top;
+  float scale;
+  const void* x; int64_t ldx;    // [rows, vocab] logits
+  const int* target;             // [rows] or null
+  float* logp;                   // [rows] or null
+  float* stats;                  // [rows, 2]: largest logit m, ln sum exp(scale (x - m)); forward: or null
+  float* entropy;                // [rows] or null; the backward reads it
+  int* top_id; float* top_logp;  // [rows, top]
+  // gradient only
+  const float* dlogp; const float* dentropy; const float* dlse;      // [rows], each or null
+  void* dx; int64_t lddx;        // [rows, vocab] (may be x)
+};
+
+// Lists of tensors of any sizes (stage_kernel_grad_*, stage_kernel_adamw); the arrays are the caller's, on the host.
+struct TensorList { int n; const int64_t* size; };
+struct AdamWArgs {
+  float beta1, rest1, beta2, rest2, eps;       // rest = 1 - beta
+  double lr, decay, lnbeta1, lnbeta2;          // lnbeta = ln beta
+  const float* lr_now;           // device, or null: in the place of lr
+  const int* step_now;           // device, or null: in the place of step
+  int step;
+  const double* sumsq;           // device, or null: gradients as they are
+  float max_norm;
+};
+
 struct NormArgs {
   int kind;                      // 0 LayerNorm, 1 RMSNorm
   int rows, d;
@@ -188,6 +216,17 @@ bool score32_supported(const ScoreArgs& a);          // fp32
 hipError_t score32_fwd(const ScoreArgs& a, hipStream_t s);
 hipError_t score32_bwd(const ScoreArgs& a, hipStream_t s);
 hipError_t score_bwd_mfma(const ScoreArgs& a, float* part, int width, hipStream_t s);
+
+// log probabilities: plain kernels
+hipError_t logprob_ref(DType dt, const LogprobArgs& a, hipStream_t s);
+hipError_t logprob_grad_ref(DType dt, const LogprobArgs& a, hipStream_t s);
+
+// gradients of many tensors at once, and the weights' update
+constexpr int GRAD_PARTS = 2048;     // workgroups of a launch at most, each of which leaves one partial sum
+hipError_t grad_sumsq(DType dt, TensorList l, const void* const* grad, int add, double* sumsq, double* part, hipStream_t s);
+hipError_t grad_clip(DType dt, TensorList l, const void* const* grad, void* const* out, const double* sumsq, float max_norm, float* norm, hipStream_t s);
+hipError_t adamw(DType dt, DType gdt, const AdamWArgs& a, TensorList l, void* const* w, float* const* master, float* const* m, float* const* v,
+                 const void* const* grad, hipStream_t s);
 
 // tuned gfx950 kernels (bf16 MFMA)
 bool gemm_mfma_supported(const GemmArgs& g);

@@ -1,0 +1,302 @@
+// What happens to a stage's gradients between iterations: their common norm, the clip to a largest one, and the AdamW step.
+//   sumsq = sum g^2,  c = min(1, max_norm / sqrt(sumsq)),  out = c g
+//   m = b1 m + (1 - b1) c g,  v = b2 v + (1 - b2) (c g)^2,  w -= lr (wd w + (m / c1) / (sqrt(v / c2) + eps)),  c_i = 1 - b_i^step
+// Every element is moved once per kernel and a few operations are done on it: what bounds all of it is bytes.
+//
+// A list of tensors is cut into chunks of one size, and a launch walks the chunks of up to LIST tensors, which travel with its arguments: nothing is
+// copied to the device beforehand, so that a captured launch holds all that it needs.
+#include "common.h"
+
+#include <type_traits>
+
+namespace stg {
+namespace {
+
+constexpr int NT = 256;
+constexpr int LIST = 48;
+
+template <typename T> constexpr int vec() { return 16 / (int)sizeof(T); }
+
+// Up to LIST tensors of K arrays each.  `first`: chunks before the tensor.  `head`: elements of it before the first that lies on a boundary of a group in every
+// array, or -1 where there is none in common, which makes the accesses single elements.  (All of a tensor in one entry of 8-byte fields: from an array
+// of bytes beside the arrays of pointers, indexed by the same number t, the compiler made scalar loads at base + t with an offset of 7 t, and scalar loads drop the low two
+// bits of each.)
+template <int K> struct Entry {
+  int64_t first, size, head;
+  const void* p[K];
+};
+template <int K> struct Lists {
+  int64_t n, chunks;
+  Entry<K> e[LIST];
+};
+// One chunk: elements [lo, body) one by one, groups from body on, and what is left of them one by one up to hi
+struct Chunk { int t; int64_t lo, body, hi; bool groups; };
+template <int K, int CHUNK> __device__ __forceinline__ Chunk chunk_of(const Lists<K>& l, int64_t c) {
+  int t = 0;
+  for (int step = 32; step > 0; step >>= 1)
+    if (t + step < l.n && l.e[t + step].first <= c) t += step;
+  const int64_t i = c - l.e[t].first, size = l.e[t].size, head = l.e[t].head > 0 ? l.e[t].head : 0;
+  Chunk r;
+  r.t = t;
+  r.body = min(head + i * CHUNK, size);
+  r.lo = i ? r.body : 0;
+  r.hi = min(head + (i + 1) * CHUNK, size);
+  r.groups = l.e[t].head >= 0;
+  return r;
+}
+
+template <typename T> struct Group {
+  union { uint4 raw; T v[vec<T>()]; } u;
+  __device__ __forceinline__ void load(const T* p) { u.raw = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<uint4*>(p) = u.raw; }
+};
+
+__device__ __forceinline__ double block_sum(double v) {
+  __shared__ double red[NT / 64];
+  for (int w = 32; w > 0; w >>= 1) v += __shfl_xor(v, w, 64);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = red[0];
+  for (int w = 1; w < NT / 64; ++w) v += red[w];
+  return v;
+}
+
+constexpr int SUM_U = 8;
+// Squares are formed and added in 64 bits: no gradient is too large or too small for them, and the vector units take fp64 as fast as memory brings it.
+// part[workgroup] += its chunks' sum, or = where no launch before has left one (`left` of them have).
+template <typename T>
+__global__ __launch_bounds__(NT) void sumsq_kernel(Lists<1> l, double* part, int left) {
+  constexpr int V = vec<T>(), CHUNK = NT * V * SUM_U;
+  double acc[4] = {};
+  for (int64_t c = blockIdx.x; c < l.chunks; c += gridDim.x) {
+    const Chunk k = chunk_of<1, CHUNK>(l, c);
+    const T* g = (const T*)l.e[k.t].p[0];
+    auto one = [&](int64_t i) { const double v = (double)to_f32(g[i]); acc[0] = fma(v, v, acc[0]); };
+    auto group = [&](const Group<T>& q) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) { const double v = (double)to_f32(q.u.v[e]); acc[e & 3] = fma(v, v, acc[e & 3]); }
+    };
+    if (k.hi - k.body == CHUNK) {
+      Group<T> q[SUM_U];
+#pragma unroll
+      for (int u = 0; u < SUM_U; ++u) q[u].load(g + k.body + (int64_t)(u * NT + threadIdx.x) * V);
+#pragma unroll
+      for (int u = 0; u < SUM_U; ++u) group(q[u]);
+    } else {
+      const int64_t n = (k.hi - k.body) / V;
+      for (int64_t i = threadIdx.x; i < n; i += NT) {
+        Group<T> q;
+        q.load(g + k.body + i * V);
+        group(q);
+      }
+      for (int64_t i = k.body + n * V + threadIdx.x; i < k.hi; i += NT) one(i);
+    }
+    for (int64_t i = k.lo + threadIdx.x; i < k.body; i += NT) one(i);
+  }
+  const double s = block_sum((acc[0] + acc[1]) + (acc[2] + acc[3]));
+  if (threadIdx.x == 0) part[blockIdx.x] = ((int)blockIdx.x < left ? part[blockIdx.x] : 0.0) + s;
+}
+
+__global__ __launch_bounds__(NT) void sumsq_total_kernel(const double* part, int parts, int add, double* sumsq) {
+  double s = 0.0;
+  for (int i = threadIdx.x; i < parts; i += NT) s += part[i];
+  s = block_sum(s);
+  if (threadIdx.x == 0) sumsq[0] = add ? sumsq[0] + s : s;
+}
+
+// the factor that brings a norm down to max_norm; 1 where the norm is not finite
+__device__ __forceinline__ float clip_factor(double sumsq, float max_norm) {
+  const double norm = sqrt(sumsq);
+  return norm > (double)max_norm && norm < INFINITY ? (float)((double)max_norm / norm) : 1.f;
+}
+
+constexpr int CLIP_U = 4;
+template <typename T>
+__global__ __launch_bounds__(NT) void clip_kernel(Lists<2> l, const double* sumsq, float max_norm, float* norm) {
+  constexpr int V = vec<T>(), CHUNK = NT * V * CLIP_U;
+  const float f = clip_factor(*sumsq, max_norm);
+  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)sqrt(*sumsq);
+  for (int64_t c = blockIdx.x; c < l.chunks; c += gridDim.x) {
+    const Chunk k = chunk_of<2, CHUNK>(l, c);
+    const T* g = (const T*)l.e[k.t].p[0];
+    T* o = (T*)l.e[k.t].p[1];
+    if (f == 1.f && g == o) continue;            // nothing to change
+    auto one = [&](int64_t i) { o[i] = from_f32<T>(f * to_f32(g[i])); };
+    auto group = [&](Group<T>& q) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) q.u.v[e] = from_f32<T>(f * to_f32(q.u.v[e]));
+    };
+    if (k.groups && k.hi - k.body == CHUNK) {
+      Group<T> q[CLIP_U];
+#pragma unroll
+      for (int u = 0; u < CLIP_U; ++u) q[u].load(g + k.body + (int64_t)(u * NT + threadIdx.x) * V);
+#pragma unroll
+      for (int u = 0; u < CLIP_U; ++u) {
+        group(q[u]);
+        q[u].store(o + k.body + (int64_t)(u * NT + threadIdx.x) * V);
+      }
+    } else {
+      const int64_t n = k.groups ? (k.hi - k.body) / V : 0;
+      for (int64_t i = threadIdx.x; i < n; i += NT) {
+        Group<T> q;
+        q.load(g + k.body + i * V);
+        group(q);
+        q.store(o + k.body + i * V);
+      }
+      for (int64_t i = k.body + n * V + threadIdx.x; i < k.hi; i += NT) one(i);
+    }
+    for (int64_t i = k.lo + threadIdx.x; i < k.body; i += NT) one(i);
+  }
+}
+
+// N elements that lie side by side, on a boundary of N of them
+template <typename T, int N> struct alignas(sizeof(T) * N) Few { T v[N]; };
+
+constexpr int ADAM_V = 4, ADAM_U = 2;
+enum { A_W, A_MASTER, A_M, A_V, A_G };
+// The fp32 weights are `master`; with bf16 weights w receives their rounding.
+template <typename TW, typename TG>
+__global__ __launch_bounds__(NT) void adamw_kernel(Lists<5> l, AdamWArgs a) {
+  constexpr int CHUNK = NT * ADAM_V * ADAM_U;
+  constexpr bool LP = sizeof(TW) == 2;
+  __shared__ float sh[3];
+  float f = 1.f;
+  if (a.sumsq) {
+    if (!(*a.sumsq < INFINITY)) return;
+    f = clip_factor(*a.sumsq, a.max_norm);
+  }
+  if (threadIdx.x == 0) {
+    const double step = a.step_now ? (double)max(*a.step_now, 1) : (double)a.step;
+    sh[0] = a.lr_now ? *a.lr_now : (float)a.lr;
+    sh[1] = (float)(-1.0 / expm1(step * a.lnbeta1));
+    sh[2] = (float)(-1.0 / expm1(step * a.lnbeta2));
+  }
+  __syncthreads();
+  const float lr = sh[0], i1 = sh[1], i2 = sh[2], wd = (float)a.decay;
+  auto update = [&](float g, float& w, float& m, float& v) {
+    g *= f;
+    m = fmaf(a.beta1, m, a.rest1 * g);
+    v = fmaf(a.beta2, v, a.rest2 * g * g);
+    w = fmaf(-lr, fmaf(wd, w, m * i1 / (sqrtf(v * i2) + a.eps)), w);
+  };
+  for (int64_t c = blockIdx.x; c < l.chunks; c += gridDim.x) {
+    const Chunk k = chunk_of<5, CHUNK>(l, c);
+    TW* w = (TW*)l.e[k.t].p[A_W];
+    float *x = (float*)l.e[k.t].p[A_MASTER], *m = (float*)l.e[k.t].p[A_M], *v = (float*)l.e[k.t].p[A_V];
+    const TG* g = (const TG*)l.e[k.t].p[A_G];
+    auto one = [&](int64_t i) {
+      float xi = x[i], mi = m[i], vi = v[i];
+      update(to_f32(g[i]), xi, mi, vi);
+      x[i] = xi; m[i] = mi; v[i] = vi;
+      if (LP) w[i] = from_f32<TW>(xi);
+    };
+    using F4 = Few<float, ADAM_V>;
+    using G4 = Few<TG, ADAM_V>;
+    using W4 = Few<TW, ADAM_V>;
+    const int64_t n = k.groups ? (k.hi - k.body) / ADAM_V : 0;
+#pragma unroll
+    for (int u = 0; u < ADAM_U; ++u) {
+      const int64_t i = u * NT + threadIdx.x, at = k.body + i * ADAM_V;
+      if (i < n) {
+        F4 xi = *(const F4*)(x + at), mi = *(const F4*)(m + at), vi = *(const F4*)(v + at);
+        const G4 gi = *(const G4*)(g + at);
+        W4 wi;
+#pragma unroll
+        for (int e = 0; e < ADAM_V; ++e) {
+          update(to_f32(gi.v[e]), xi.v[e], mi.v[e], vi.v[e]);
+          wi.v[e] = from_f32<TW>(xi.v[e]);
+        }
+        *(F4*)(x + at) = xi; *(F4*)(m + at) = mi; *(F4*)(v + at) = vi;
+        if (LP) *(W4*)(w + at) = wi;
+      }
+    }
+    for (int64_t i = k.body + n * ADAM_V + threadIdx.x; i < k.hi; i += NT) one(i);
+    for (int64_t i = k.lo + threadIdx.x; i < k.body; i += NT) one(i);
+  }
+}
+
+// Calls launch(lists, workgroups) for up to LIST tensors at a time; with `always` once at least.  es: element sizes of the K arrays; the pointers are
+// arr[k][i]; an array may be missing (null), which counts as aligned.
+template <int K, int CHUNK, int V, typename F>
+hipError_t over_lists(const TensorList& t, const void* const* const (&arr)[K], const int (&es)[K], bool always, F launch) {
+  int i = 0;
+  do {
+    Lists<K> l;
+    l.n = l.chunks = 0;
+    for (; i < t.n && l.n < LIST; ++i) {
+      if (t.size[i] == 0) continue;
+      Entry<K>& k = l.e[l.n++];
+      int64_t head = -2;
+      for (int q = 0; q < K; ++q) {
+        k.p[q] = arr[q] ? arr[q][i] : nullptr;
+        if (!arr[q]) continue;
+        const int64_t h = (V - (uintptr_t)arr[q][i] / es[q] % V) % V;
+        head = head == -2 || head == h ? h : -1;
+      }
+      k.first = l.chunks;
+      k.size = t.size[i];
+      k.head = head < k.size ? head : k.size;
+      const int64_t body = k.size - (k.head > 0 ? k.head : 0);
+      l.chunks += body > CHUNK ? (body + CHUNK - 1) / CHUNK : 1;
+    }
+    if (l.n || always) {
+      const int64_t chunks = l.chunks;
+      const hipError_t e = launch(l, (int)(chunks < 1 ? 1 : chunks < GRAD_PARTS ? chunks : GRAD_PARTS));
+      if (e != hipSuccess) return e;
+    }
+    always = false;
+  } while (i < t.n);
+  return hipSuccess;
+}
+
+template <typename T>
+hipError_t sumsq_launch(const TensorList& l, const void* const* grad, int add, double* sumsq, double* part, hipStream_t s) {
+  int left = 0;
+  const hipError_t e = over_lists<1, NT * vec<T>() * SUM_U, vec<T>()>(l, {grad}, {(int)sizeof(T)}, false, [&](const Lists<1>& t, int wgs) {
+    hipLaunchKernelGGL((sumsq_kernel<T>), dim3(wgs), dim3(NT), 0, s, t, part, left);
+    left = left > wgs ? left : wgs;
+    return hipGetLastError();
+  });
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(sumsq_total_kernel, dim3(1), dim3(NT), 0, s, part, left, add, sumsq);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t clip_launch(const TensorList& l, const void* const* grad, void* const* out, const double* sumsq, float max_norm, float* norm, hipStream_t s) {
+  return over_lists<2, NT * vec<T>() * CLIP_U, vec<T>()>(l, {grad, (const void* const*)out}, {(int)sizeof(T), (int)sizeof(T)}, norm != nullptr, [&](const Lists<2>& t, int wgs) {
+    hipLaunchKernelGGL((clip_kernel<T>), dim3(wgs), dim3(NT), 0, s, t, sumsq, max_norm, norm);
+    norm = nullptr;
+    return hipGetLastError();
+  });
+}
+
+template <typename TW, typename TG>
+hipError_t adamw_launch(const AdamWArgs& a, const TensorList& l, void* const* w, float* const* master, float* const* m, float* const* v,
+                        const void* const* grad, hipStream_t s) {
+  const void* const* fp32 = sizeof(TW) == 2 ? (const void* const*)master : (const void* const*)w;
+  const void* const* lp = sizeof(TW) == 2 ? (const void* const*)w : nullptr;
+  return over_lists<5, NT * ADAM_V * ADAM_U, ADAM_V>(l, {lp, fp32, (const void* const*)m, (const void* const*)v, grad}, {2, 4, 4, 4, (int)sizeof(TG)}, false,
+                                                     [&](const Lists<5>& t, int wgs) {
+    hipLaunchKernelGGL((adamw_kernel<TW, TG>), dim3(wgs), dim3(NT), 0, s, t, a);
+    return hipGetLastError();
+  });
+}
+
+}  // namespace
+
+hipError_t grad_sumsq(DType dt, TensorList l, const void* const* grad, int add, double* sumsq, double* part, hipStream_t s) {
+  return dt == DT_F32 ? sumsq_launch<float>(l, grad, add, sumsq, part, s) : sumsq_launch<bf16>(l, grad, add, sumsq, part, s);
+}
+hipError_t grad_clip(DType dt, TensorList l, const void* const* grad, void* const* out, const double* sumsq, float max_norm, float* norm, hipStream_t s) {
+  return dt == DT_F32 ? clip_launch<float>(l, grad, out, sumsq, max_norm, norm, s) : clip_launch<bf16>(l, grad, out, sumsq, max_norm, norm, s);
+}
+hipError_t adamw(DType dt, DType gdt, const AdamWArgs& a, TensorList l, void* const* w, float* const* master, float* const* m, float* const* v,
+                 const void* const* grad, hipStream_t s) {
+  if (dt == DT_F32)
+    return gdt == DT_F32 ? adamw_launch<float, float>(a, l, w, master, m, v, grad, s) : adamw_launch<float, bf16>(a, l, w, master, m, v, grad, s);
+  return gdt == DT_F32 ? adamw_launch<bf16, float>(a, l, w, master, m, v, grad, s) : adamw_launch<bf16, bf16>(a, l, w, master, m, v, grad, s);
+}
+
+}  // namespace stg

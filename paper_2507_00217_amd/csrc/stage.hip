@@ -1243,6 +1243,125 @@ int stage_kernel_score_attention_bwd(const stage_score_attention_t* p, const voi
   return hip_rc(score_bwd_ref((DType)p->dtype, a, (hipStream_t)hip_stream));
 }
 
+// The arguments that the entries of log probabilities share; gradients and outputs are the caller's to fill in.
+static bool logprob_args(const stage_token_logprob_t* p, LogprobArgs* a) {
+  if (!p || !dtype_ok(p->dtype) || p->rows < 1 || p->rows > 1 << 23 || p->vocab < 1 || p->vocab > 1 << 24 || p->top < 0 || p->top > LOGPROB_MAX_TOP ||
+      p->top > p->vocab || !(p->scale == 0.f || (p->scale >= 1e-30f && p->scale <= 1e30f)) || ((uintptr_t)p->target & 3))
+    return false;
+  *a = LogprobArgs{};
+  a->rows = p->rows; a->vocab = p->vocab; a->top = p->top; a->scale = p->scale == 0.f ? 1.f : p->scale; a->target = p->target;
+  return true;
+}
+static bool logprob_rows(int dtype, int vocab, const void* x, int64_t ld) {
+  return x && ld >= vocab && (uintptr_t)x % (dtype == STAGE_DTYPE_FP32 ? 4 : 2) == 0;
+}
+static bool logprob_values(const stage_token_logprob_t* p, float* logp, float* stats, float* entropy, int32_t* top_id, float* top_logp, void* scratch,
+                           size_t scratch_bytes, LogprobArgs* a) {
+  const size_t need = stage_kernel_token_logprob_scratch_bytes(p);
+  if ((p->top > 0 && (!top_id || !top_logp)) || (need > 0 && (!scratch || ((uintptr_t)scratch & 15) || scratch_bytes < need))) return false;
+  a->logp = logp; a->stats = stats; a->entropy = entropy; a->top_id = top_id; a->top_logp = top_logp;
+  return true;
+}
+static bool logprob_grads(const stage_token_logprob_t* p, const float* stats, const float* entropy, const float* dlogp, const float* dentropy,
+                          const float* dlse, void* dlogits, int64_t ldd, const void* logits, int64_t ld, LogprobArgs* a) {
+  if (!stats || (!dlogp && !dentropy && !dlse) || (dlogp && !p->target) || (dentropy && !entropy) || !logprob_rows(p->dtype, p->vocab, dlogits, ldd) ||
+      (dlogits == logits && ldd != ld))
+    return false;
+  a->stats = (float*)stats; a->entropy = (float*)entropy; a->dlogp = dlogp; a->dentropy = dentropy; a->dlse = dlse; a->dx = dlogits; a->lddx = ldd;
+  return true;
+}
+
+int stage_kernel_token_logprob_fwd(const stage_token_logprob_t* p, const void* logits, int64_t ld, float* logp, float* stats, float* entropy,
+                                   int32_t* top_id, float* top_logp, void* scratch, size_t scratch_bytes, int kernel_set, void* hip_stream) {
+  LogprobArgs a;
+  if (!logprob_args(p, &a) || !logprob_rows(p->dtype, p->vocab, logits, ld) ||
+      !logprob_values(p, logp, stats, entropy, top_id, top_logp, scratch, scratch_bytes, &a))
+    return STAGE_E_INVAL;
+  a.x = logits; a.ldx = ld;
+  return hip_rc(logprob_ref((DType)p->dtype, a, (hipStream_t)hip_stream));
+}
+
+int stage_kernel_token_logprob_bwd(const stage_token_logprob_t* p, const void* logits, int64_t ld, const float* stats, const float* entropy,
+                                   const float* dlogp, const float* dentropy, const float* dlse, void* dlogits, int64_t ldd, int kernel_set,
+                                   void* hip_stream) {
+  LogprobArgs a;
+  if (!logprob_args(p, &a) || !logprob_rows(p->dtype, p->vocab, logits, ld) ||
+      !logprob_grads(p, stats, entropy, dlogp, dentropy, dlse, dlogits, ldd, logits, ld, &a))
+    return STAGE_E_INVAL;
+  a.x = logits; a.ldx = ld;
+  return hip_rc(logprob_grad_ref((DType)p->dtype, a, (hipStream_t)hip_stream));
+}
+
+int stage_kernel_token_logprob_grad(const stage_token_logprob_t* p, const void* logits, int64_t ld, const float* dlogp, const float* dentropy,
+                                    const float* dlse, void* dlogits, int64_t ldd, float* logp, float* stats, float* entropy, int32_t* top_id,
+                                    float* top_logp, void* scratch, size_t scratch_bytes, int kernel_set, void* hip_stream) {
+  LogprobArgs a;
+  if (!logprob_args(p, &a) || !logprob_rows(p->dtype, p->vocab, logits, ld) ||
+      !logprob_values(p, logp, stats, entropy, top_id, top_logp, scratch, scratch_bytes, &a) ||
+      !logprob_grads(p, stats, entropy, dlogp, dentropy, dlse, dlogits, ldd, logits, ld, &a))
+    return STAGE_E_INVAL;
+  a.x = logits; a.ldx = ld;
+  const hipError_t e = logprob_ref((DType)p->dtype, a, (hipStream_t)hip_stream);
+  if (e != hipSuccess) return hip_rc(e);
+  return hip_rc(logprob_grad_ref((DType)p->dtype, a, (hipStream_t)hip_stream));
+}
+
+size_t stage_kernel_token_logprob_scratch_bytes(const stage_token_logprob_t* p) {
+  LogprobArgs a;
+  return logprob_args(p, &a) ? 0 : 0;
+}
+
+// Lists of tensors: sizes within bounds, and a pointer, aligned to es bytes, for each that has elements
+static bool tensor_sizes(int n, const int64_t* size) {
+  if (n < 0 || (n > 0 && !size)) return false;
+  for (int i = 0; i < n; ++i)
+    if (size[i] < 0 || size[i] > (int64_t)1 << 40) return false;
+  return true;
+}
+static bool tensor_list(int n, const int64_t* size, const void* const* p, int es) {
+  if (n > 0 && !p) return false;
+  for (int i = 0; i < n; ++i)
+    if (size[i] > 0 && (!p[i] || (uintptr_t)p[i] % es)) return false;
+  return true;
+}
+static int bytes_of(int dtype) { return dtype == STAGE_DTYPE_FP32 ? 4 : 2; }
+
+int stage_kernel_grad_sumsq(int dtype, int n, const int64_t* size, const void* const* grad, int add, double* sumsq, void* scratch,
+                            size_t scratch_bytes, void* hip_stream) {
+  if (!dtype_ok(dtype) || !tensor_sizes(n, size) || !tensor_list(n, size, grad, bytes_of(dtype)) || (add != 0 && add != 1) || !sumsq ||
+      ((uintptr_t)sumsq & 7) || !scratch || ((uintptr_t)scratch & 15) || scratch_bytes < stage_kernel_grad_sumsq_scratch_bytes())
+    return STAGE_E_INVAL;
+  return hip_rc(grad_sumsq((DType)dtype, TensorList{n, size}, grad, add, sumsq, (double*)scratch, (hipStream_t)hip_stream));
+}
+
+size_t stage_kernel_grad_sumsq_scratch_bytes(void) { return GRAD_PARTS * sizeof(double); }
+
+int stage_kernel_grad_clip(int dtype, int n, const int64_t* size, const void* const* grad, void* const* out, const double* sumsq, float max_norm,
+                           float* norm, void* hip_stream) {
+  if (!dtype_ok(dtype) || !tensor_sizes(n, size) || !tensor_list(n, size, grad, bytes_of(dtype)) ||
+      !tensor_list(n, size, (const void* const*)out, bytes_of(dtype)) || !sumsq || ((uintptr_t)sumsq & 7) || !(max_norm > 0.f) || !std::isfinite(max_norm) ||
+      ((uintptr_t)norm & 3))
+    return STAGE_E_INVAL;
+  return hip_rc(grad_clip((DType)dtype, TensorList{n, size}, grad, out, sumsq, max_norm, norm, (hipStream_t)hip_stream));
+}
+
+int stage_kernel_adamw(const stage_adamw_t* p, int n, const int64_t* size, void* const* w, float* const* master, float* const* m, float* const* v,
+                       const void* const* grad, void* hip_stream) {
+  const auto list = [&](const void* const* q, int es) { return tensor_list(n, size, q, es); };
+  const auto hyper = [](double x) { return x >= 0.0 && std::isfinite(x); };
+  if (!p || !dtype_ok(p->dtype) || !dtype_ok(p->grad_dtype) || !hyper(p->lr) || !hyper(p->beta1) || !hyper(p->beta2) || p->beta1 >= 1.0 || p->beta2 >= 1.0 ||
+      !hyper(p->eps) || !hyper(p->weight_decay) || ((uintptr_t)p->sumsq & 7) || ((uintptr_t)p->lr_now & 3) || ((uintptr_t)p->step_now & 3) || p->step < 1 ||
+      (p->sumsq && (!(p->max_norm > 0.f) || !std::isfinite(p->max_norm))) || !tensor_sizes(n, size) ||
+      !list((const void* const*)w, bytes_of(p->dtype)) || !list((const void* const*)m, 4) || !list((const void* const*)v, 4) || !list(grad, bytes_of(p->grad_dtype)) ||
+      (p->dtype == STAGE_DTYPE_FP32 ? master != nullptr : !list((const void* const*)master, 4)))
+    return STAGE_E_INVAL;
+  AdamWArgs a{};
+  a.beta1 = (float)p->beta1; a.rest1 = (float)(1.0 - p->beta1); a.beta2 = (float)p->beta2; a.rest2 = (float)(1.0 - p->beta2); a.eps = (float)p->eps;
+  a.lr = p->lr; a.decay = p->weight_decay; a.lnbeta1 = log(p->beta1); a.lnbeta2 = log(p->beta2);
+  a.lr_now = p->lr_now; a.step_now = p->step_now; a.step = p->step; a.sumsq = p->sumsq; a.max_norm = p->max_norm;
+  return hip_rc(adamw((DType)p->dtype, (DType)p->grad_dtype, a, TensorList{n, size}, w, master, m, v, grad, (hipStream_t)hip_stream));
+}
+
 int stage_kernel_norm_fwd(int dtype, int norm, int rows, int d, float eps, const void* x, const void* gamma,
                           const void* beta, void* out, float* stats, void* hip_stream) {
   if (!dtype_ok(dtype) || (norm != 0 && norm != 1) || rows <= 0 || d <= 0 || !x || !gamma || (norm == 0 && !beta) || !out || !stats)

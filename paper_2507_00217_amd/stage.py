@@ -56,6 +56,17 @@ class ScoreAttention(C.Structure):
         ("scale", C.c_float), ("softcap", C.c_float), ("slope", C.c_void_p), ("seq_start", C.c_void_p), ("prefix", C.c_void_p)]
 
 
+class TokenLogprob(C.Structure):
+    """stage_token_logprob_t of include/stage_kernels.h; `target` is the address of a device tensor that the caller keeps."""
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "rows", "vocab", "top")] + [("scale", C.c_float), ("target", C.c_void_p)]
+
+
+class AdamW(C.Structure):
+    """stage_adamw_t of include/stage_kernels.h; the pointers are addresses of device tensors that the caller keeps."""
+    _fields_ = [("dtype", C.c_int32), ("grad_dtype", C.c_int32)] + [(n, C.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")] + [
+        ("sumsq", C.c_void_p), ("lr_now", C.c_void_p), ("step_now", C.c_void_p), ("step", C.c_int32), ("max_norm", C.c_float)]
+
+
 class StageSizes(C.Structure):
     _fields_ = [(n, C.c_size_t) for n in ("weights", "grads", "stash", "workspace")]
 
@@ -81,6 +92,7 @@ def lib() -> C.CDLL:
         vp, ip = C.c_void_p, C.POINTER(C.c_int)
         cfgp, opp, sopp = C.POINTER(StageConfig), C.POINTER(StageOp), C.POINTER(StageSubOp)
         axp, scp, mat = C.POINTER(RopeAxes), C.POINTER(ScoreAttention), [vp, C.c_int64]      # a matrix: address and row stride
+        tlp, sizes, vps = C.POINTER(TokenLogprob), C.POINTER(C.c_int64), C.POINTER(vp)
         sig = {
             "stage_query_sizes": (C.c_int, [cfgp, C.POINTER(StageSizes)]),
             "stage_validate_schedule": (C.c_int, [cfgp, opp, C.c_int, ip, ip]),
@@ -115,6 +127,14 @@ def lib() -> C.CDLL:
             "stage_kernel_score_attention_fwd": (C.c_int, [scp] + mat * 4 + [vp, C.c_int, vp]),
             "stage_kernel_score_attention_bwd": (C.c_int, [scp] + mat * 4 + [vp] + mat * 4 + [vp, C.c_size_t, C.c_int, vp]),
             "stage_kernel_score_attention_bwd_scratch_bytes": (C.c_size_t, [scp]),
+            "stage_kernel_token_logprob_fwd": (C.c_int, [tlp] + mat + [vp] * 6 + [C.c_size_t, C.c_int, vp]),
+            "stage_kernel_token_logprob_bwd": (C.c_int, [tlp] + mat + [vp] * 5 + mat + [C.c_int, vp]),
+            "stage_kernel_token_logprob_grad": (C.c_int, [tlp] + mat + [vp] * 3 + mat + [vp] * 6 + [C.c_size_t, C.c_int, vp]),
+            "stage_kernel_token_logprob_scratch_bytes": (C.c_size_t, [tlp]),
+            "stage_kernel_grad_sumsq": (C.c_int, [C.c_int, C.c_int, sizes, vps, C.c_int, vp, vp, C.c_size_t, vp]),
+            "stage_kernel_grad_sumsq_scratch_bytes": (C.c_size_t, []),
+            "stage_kernel_grad_clip": (C.c_int, [C.c_int, C.c_int, sizes, vps, vps, vp, C.c_float, vp, vp]),
+            "stage_kernel_adamw": (C.c_int, [C.POINTER(AdamW), C.c_int, sizes, vps, vps, vps, vps, vps, vp]),
             "stage_probe_mfma_ceiling": (C.c_int, [C.c_int, C.c_int, vp, C.c_size_t, C.POINTER(C.c_double), C.POINTER(C.c_double), vp]),
         }
         for name, (res, args) in sig.items():
