@@ -172,8 +172,8 @@ size_t stage_kernel_score_attention_bwd_scratch_bytes(const stage_score_attentio
  * or +inf has NaN for its log probabilities, ln S, H and gradient, and -1 for its alternatives. */
 typedef struct {
   int32_t dtype;             /* of the logits and their gradient */
-  int32_t rows;              /* >= 1, at most 2^23 */
-  int32_t vocab;             /* >= 1, at most 2^24 */
+  int32_t rows;              /* >= 1, at most 2^21 */
+  int32_t vocab;             /* >= 1, at most 2^22 */
   int32_t top;               /* alternatives of each row: 0 .. 64, at most vocab */
   float scale;               /* 1e-30 .. 1e30 (one over a temperature), or 0 for 1 */
   const int32_t* target;     /* device, [rows]: the row's token; outside 0 .. vocab - 1 the row has none; or NULL: no row has one */

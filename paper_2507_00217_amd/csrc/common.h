@@ -221,6 +221,12 @@ hipError_t score_bwd_mfma(const ScoreArgs& a, float* part, int width, hipStream_
 hipError_t logprob_ref(DType dt, const LogprobArgs& a, hipStream_t s);
 hipError_t logprob_grad_ref(DType dt, const LogprobArgs& a, hipStream_t s);
 
+// and with rows in registers; split: every row in several parts.  logprob_both: values and gradient.
+size_t logprob_scratch_bytes(DType dt, const LogprobArgs& a);
+hipError_t logprob(DType dt, const LogprobArgs& a, bool split, void* scratch, hipStream_t s);
+hipError_t logprob_grad(DType dt, const LogprobArgs& a, hipStream_t s);
+hipError_t logprob_both(DType dt, const LogprobArgs& a, bool split, void* scratch, hipStream_t s);
+
 // gradients of many tensors at once, and the weights' update
 constexpr int GRAD_PARTS = 2048;     // workgroups of a launch at most, each of which leaves one partial sum
 hipError_t grad_sumsq(DType dt, TensorList l, const void* const* grad, int add, double* sumsq, double* part, hipStream_t s);

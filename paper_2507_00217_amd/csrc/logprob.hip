@@ -1,0 +1,507 @@
+// Log probabilities of the rows' tokens, entropy, likeliest alternatives and the logits' gradient, every logit read once.
+//   m = max x,  e_j = 2^(c (x_j - m)) with c = scale log2 e,  S = sum e_j,  T = sum e_j c (m - x_j) (terms of one sign)
+//   ln p_j = scale (x_j - m) - ln S,  H = ln S + ln 2 T / S
+//   dx_j = scale [p_j (dlse - dlogp - dH (ln p_j + H)) + dlogp [j = token]]
+// An element costs a few operations and an exponential: what bounds it is bytes.
+//
+// A row, or a part of one, lies in the registers of one workgroup: up to 128 Ki columns of bf16 in 64 registers of each of 1024 threads, half of a compute
+// unit's registers.  So the maximum is known before the first exponential, no sum is ever rescaled, and the gradient is formed from the registers
+// too.  Rows that are wider, or too few to fill the chip, are cut into parts; a second launch joins what the parts found.
+//
+// Alternatives: the k-th largest of the maxima of 64 groups of threads is a lower bound of the k-th largest logit, found in 16 steps of a ballot; the
+// few elements that reach it go to a list in LDS, and each one's rank is the number of list entries before it.  Lists that overflow (rows of ties, or with
+// fewer tokens left than alternatives) are left, and the alternatives are taken out of the row one by one: a thread reads its columns again whenever its best is taken.
+#include "common.h"
+
+#include <type_traits>
+
+namespace stg {
+namespace {
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float FAR = -1e4f;           // an exponent below which 2^x is zero many times over, and x still a number
+constexpr int CAND = 512;
+constexpr int MAX_PARTS = 64;
+typedef unsigned long long u64;
+
+enum { VALUES = 0, TOP = 1, GRAD = 2, GRAD_H = 3 };      // GRAD: neither H nor its gradient
+
+template <typename T> constexpr int vec() { return 16 / (int)sizeof(T); }
+
+__device__ __forceinline__ float max3(float a, float b, float c) {     // fmaxf would first quiet each operand
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+template <typename T> struct Piece;
+template <> struct Piece<bf16> {
+  uint4 w;
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+    const unsigned d[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __builtin_bit_cast(float, d[i] << 16);
+      f[2 * i + 1] = __builtin_bit_cast(float, d[i] & 0xffff0000u);
+    }
+  }
+  __device__ __forceinline__ void none() { w = make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }
+};
+template <> struct Piece<float> {
+  uint4 w;
+  __device__ __forceinline__ void get(float (&f)[4]) const {
+    f[0] = __builtin_bit_cast(float, w.x); f[1] = __builtin_bit_cast(float, w.y); f[2] = __builtin_bit_cast(float, w.z); f[3] = __builtin_bit_cast(float, w.w);
+  }
+  __device__ __forceinline__ void none() { w = make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }
+};
+// From here on the pieces are taken for others: what was unpacked of them is not kept for a later pass, which would be twice the registers.
+template <typename P> __device__ __forceinline__ void forget(P& p) { asm volatile("" : "+v"(p.w.x), "+v"(p.w.y), "+v"(p.w.z), "+v"(p.w.w)); }
+template <typename T> union Out {
+  uint4 w;
+  T v[vec<T>()];
+};
+
+template <int CTRL> __device__ __forceinline__ float dpp(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+// over the lanes of a group (a 64th of the workgroup), and over a wavefront
+template <int LANES, typename Op> __device__ __forceinline__ float lanes(float v, Op op) {
+  v = op(v, dpp<0xB1>(v));                        // the neighbour
+  v = op(v, dpp<0x4E>(v));                        // the other two of four
+  if (LANES >= 8) v = op(v, dpp<0x141>(v));       // mirrored in eight
+  if (LANES >= 16) v = op(v, dpp<0x140>(v));      // mirrored in sixteen
+  if (LANES >= 32) v = op(v, __shfl_xor(v, 16, 64));
+  if (LANES >= 64) v = op(v, __shfl_xor(v, 32, 64));
+  return v;
+}
+__device__ __forceinline__ float wave_max(float v) { return lanes<64>(v, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float wave_sum(float v) { return lanes<64>(v, [](float a, float b) { return a + b; }); }
+
+// an order of fp32 numbers as one of unsigned ones; zeros of both signs are one
+__device__ __forceinline__ unsigned ordered(float f) {
+  const unsigned u = __builtin_bit_cast(unsigned, f + 0.f);
+  return u ^ ((int)u < 0 ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ float disordered(unsigned u) { return __builtin_bit_cast(float, u ^ ((int)u < 0 ? 0x80000000u : 0xffffffffu)); }
+// the larger logit first, of equal ones the lower column; 0 comes behind all
+__device__ __forceinline__ u64 key_of(float f, int col) { return (u64)ordered(f) << 32 | (unsigned)~col; }
+__device__ __forceinline__ int col_of(u64 key) { return (int)~(unsigned)key; }
+__device__ __forceinline__ float value_of(u64 key) { return disordered((unsigned)(key >> 32)); }
+
+__device__ __forceinline__ float log_prob(float x, float m, float scale, float ln) {
+  return x == -INFINITY && ln == ln ? -INFINITY : scale * (x - m) - ln;
+}
+
+// What a row's gradient is made of: dx = p (a - b (ln p + h)) + at the token w, all times scale already
+struct Weights {
+  float a, b, h, w;
+  int token;
+  bool none;
+};
+__device__ __forceinline__ Weights weights_of(const LogprobArgs& a, int64_t row, bool with_h) {
+  Weights r;
+  r.token = a.target ? a.target[row] : -1;
+  const bool has = r.token >= 0 && r.token < a.vocab;
+  const float w = a.dlogp && has ? a.dlogp[row] : 0.f, dh = with_h && a.dentropy ? a.dentropy[row] : 0.f, dl = a.dlse ? a.dlse[row] : 0.f;
+  if (!has) r.token = -1;
+  r.a = a.scale * (dl - w);
+  r.b = a.scale * dh;
+  r.w = a.scale * w;
+  r.h = 0.f;
+  r.none = w == 0.f && dh == 0.f && dl == 0.f;
+  return r;
+}
+template <bool H> __device__ __forceinline__ float grad_of(float x, float m, float c, float log2s, const Weights& w) {
+  const float u = fmaf(x - m, c, -log2s), p = __builtin_amdgcn_exp2f(u);
+  return H ? p * fmaf(-w.b, fmaf(fmaxf(u, FAR), LN2, w.h), w.a) : p * w.a;
+}
+
+// How a row's columns lie: `lead` before the first 16-byte boundary, `full` pieces, and the rest
+template <typename T> struct Span {
+  int n, lead, full, tail;
+  __device__ __forceinline__ Span(const T* x, int cols) : n(cols) {
+    constexpr int V = vec<T>();
+    lead = min(n, (int)((V - (unsigned)((uintptr_t)x / sizeof(T)) % V) % V));
+    full = (n - lead) / V;
+    tail = lead + full * V;
+  }
+  // the column that thread t takes by itself, or -1
+  __device__ __forceinline__ int edge(int t) const { return t < lead ? t : t - lead < n - tail ? tail + t - lead : -1; }
+};
+
+// One row, or part `blockIdx.x % parts` of one.  parts > 1: what it found goes to rec (m, S, T) and keys.
+template <typename T, int NT, int NV, int MODE>
+__global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a, int parts, int cols, float4* rec, u64* keys) {
+  constexpr int V = vec<T>(), WAVES = NT / 64;
+  constexpr bool H = MODE != GRAD, G = MODE == GRAD || MODE == GRAD_H;
+  __shared__ float gmax[64], red[2][WAVES];
+  __shared__ u64 cand[MODE == TOP ? CAND : 1], best[MODE == TOP ? WAVES : 1];
+  __shared__ int ncand;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int64_t unit = blockIdx.x, row = parts > 1 ? unit / parts : unit;
+  const int c0 = parts > 1 ? (int)(unit % parts) * cols : 0;
+  const T* x = (const T*)a.x + row * a.ldx + c0;
+  const Span<T> sp(x, min(cols, a.vocab - c0));
+  const int whole = sp.full / NT;                  // pieces that every thread has
+  Piece<T> v[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    if (k < whole) v[k].w = *reinterpret_cast<const uint4*>(x + sp.lead + (k * NT + t) * V);
+    else {
+      v[k].none();
+      if (k * NT + t < sp.full) v[k].w = *reinterpret_cast<const uint4*>(x + sp.lead + (k * NT + t) * V);
+    }
+  }
+  const int ecol = sp.edge(t);
+  const float xe = ecol >= 0 ? to_f32(x[ecol]) : -INFINITY;
+  Weights w{};
+  if (G || parts == 1) w = weights_of(a, row, MODE == GRAD_H);
+  float xt = w.token >= 0 && parts == 1 ? to_f32(x[w.token]) : 0.f;
+
+  float vm[MODE == TOP ? NV : 1], tm = xe;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    if (k * NT >= sp.full) { if (MODE == TOP) vm[k] = -INFINITY; continue; }
+    float f[V], mx;
+    v[k].get(f);
+    mx = max3(f[0], f[1], f[2]);
+#pragma unroll
+    for (int e = 3; e + 1 < V; e += 2) mx = max3(mx, f[e], f[e + 1]);
+    tm = max3(tm, mx, f[V - 1]);
+    if (MODE == TOP) vm[k] = max3(mx, mx, f[V - 1]);
+  }
+  const float gm = lanes<NT / 64>(tm, [](float p, float q) { return fmaxf(p, q); });
+  if (t % (NT / 64) == 0) gmax[t / (NT / 64)] = gm;
+  if (MODE == TOP && t == 0) ncand = 0;
+  __syncthreads();
+  const float group = gmax[lane], m = wave_max(group), at = m == -INFINITY ? 0.f : m;
+
+  if (MODE == TOP) {
+    unsigned reach = 0;                            // the leading 16 bits of the k-th largest group's maximum
+    const unsigned mine = ordered(group);
+#pragma unroll
+    for (int b = 31; b >= 16; --b) {
+      const unsigned next = reach | 1u << b;
+      if (__builtin_popcountll(__ballot(mine >= next)) >= a.top) reach = next;
+    }
+    const float bar = reach <= 0x007fffffu ? -INFINITY : disordered(reach);
+    auto offer = [&](bool has, float f, int col) {
+      const u64 mask = __ballot(has && f >= bar);
+      if (mask) {
+        int first = 0;
+        if (lane == 0) first = atomicAdd(&ncand, __builtin_popcountll(mask));
+        first = __builtin_amdgcn_readfirstlane(first) + __builtin_popcountll(mask & ((1ull << lane) - 1));
+        if (has && f >= bar && first < CAND) cand[first] = key_of(f, c0 + col);
+      }
+    };
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const bool has = k * NT + t < sp.full;
+      forget(v[k]);
+      if (__ballot(has && vm[k] >= bar)) {
+        float f[V];
+        v[k].get(f);
+#pragma unroll
+        for (int e = 0; e < V; ++e) offer(has, f[e], sp.lead + (k * NT + t) * V + e);
+      }
+    }
+    if (wave == 0) offer(ecol >= 0, xe, ecol);
+  }
+
+  const float c = a.scale * LOG2E;
+  float s = 0.f, h = 0.f;
+  auto term = [&](float f) {
+    const float z = (f - at) * c, e = __builtin_amdgcn_exp2f(z);
+    s += e;
+    if (H) h = fmaf(e, -fmaxf(z, FAR), h);
+  };
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    if (k * NT >= sp.full) continue;
+    float f[V];
+    forget(v[k]);
+    v[k].get(f);
+#pragma unroll
+    for (int e = 0; e < V; ++e) term(f[e]);
+  }
+  term(xe);
+  s = wave_sum(s);
+  if (H) h = wave_sum(h);
+  if (lane == 0) { red[0][wave] = s; red[1][wave] = h; }
+  asm volatile("" : "+v"(xt));                     // has arrived before any thread puts a gradient in its place
+  __syncthreads();
+  s = red[0][0];
+  h = red[1][0];
+#pragma unroll
+  for (int i = 1; i < WAVES; ++i) { s += red[0][i]; h += red[1][i]; }
+
+  const bool bad = !(s < INFINITY);
+  const float ln = bad ? NAN : logf(s), entropy = s == 0.f ? 0.f : ln + LN2 * h / s;
+  if (t == 0) {
+    if (parts > 1) rec[unit] = make_float4(m, s, h, 0.f);
+    else {
+      if (a.logp) a.logp[row] = w.token >= 0 ? log_prob(xt, at, a.scale, ln) : 0.f;
+      if (a.stats) { a.stats[2 * row] = m; a.stats[2 * row + 1] = ln; }
+      if (H && a.entropy) a.entropy[row] = entropy;
+    }
+  }
+
+  if (MODE == TOP) {
+    auto put = [&](int rank, u64 key) {
+      if (parts > 1) keys[unit * a.top + rank] = key;
+      else {
+        a.top_id[row * a.top + rank] = bad ? -1 : col_of(key);
+        a.top_logp[row * a.top + rank] = bad ? NAN : log_prob(value_of(key), at, a.scale, ln);
+      }
+    };
+    const int n = ncand;
+    if (bad) {
+      for (int i = t; i < a.top; i += NT) put(i, 0);
+    } else if (n <= CAND) {
+      for (int i = t; i < n; i += NT) {
+        const u64 key = cand[i];
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += cand[j] > key;
+        if (rank < a.top) put(rank, key);
+      }
+      for (int i = n + t; i < a.top; i += NT) put(i, 0);      // a part with fewer columns
+    } else {
+      u64 last = ~0ull, mine = 0;
+      for (int r = 0; r < a.top; ++r) {
+        if (mine == 0 || mine == last) {           // the thread's largest behind the last one taken
+          mine = 0;
+          auto look = [&](float f, int col) {
+            const u64 key = key_of(f, c0 + col);
+            if (key < last && key > mine) mine = key;
+          };
+          for (int i = t; i < sp.full; i += NT) {
+            Piece<T> p;
+            float f[V];
+            p.w = *reinterpret_cast<const uint4*>(x + sp.lead + i * V);
+            p.get(f);
+#pragma unroll
+            for (int e = 0; e < V; ++e) look(f[e], sp.lead + i * V + e);
+          }
+          if (ecol >= 0) look(xe, ecol);
+        }
+        u64 b = mine;
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) { const u64 o = __shfl_xor(b, d, 64); b = o > b ? o : b; }
+        if (lane == 0) best[wave] = b;
+        __syncthreads();
+        b = best[0];
+        for (int i = 1; i < WAVES; ++i) b = best[i] > b ? best[i] : b;
+        __syncthreads();
+        if (t == 0) put(r, b);
+        last = b;
+      }
+    }
+  }
+
+  if (G) {
+    T* dx = (T*)a.dx + row * a.lddx;
+    if (MODE == GRAD_H) w.h = entropy;
+    const bool none = w.none || m == -INFINITY, together = (((uintptr_t)dx ^ (uintptr_t)x) & 15) == 0;
+    const float log2s = ln * LOG2E;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      if (k * NT + t >= sp.full) continue;
+      float f[V];
+      forget(v[k]);
+      v[k].get(f);
+      Out<T> o;
+#pragma unroll
+      for (int e = 0; e < V; ++e) o.v[e] = from_f32<T>(none ? 0.f : grad_of<MODE == GRAD_H>(f[e], at, c, log2s, w));
+      T* to = dx + sp.lead + (k * NT + t) * V;
+      if (together) *reinterpret_cast<uint4*>(to) = o.w;
+      else
+#pragma unroll
+        for (int e = 0; e < V; ++e) to[e] = o.v[e];
+    }
+    if (ecol >= 0) dx[ecol] = from_f32<T>(none ? 0.f : grad_of<MODE == GRAD_H>(xe, at, c, log2s, w));
+    // the token's, by the thread that has stored it above, so that this store comes behind that one
+    const int piece = w.token - sp.lead;
+    const bool inside = piece >= 0 && w.token < sp.tail;
+    if (w.token >= 0 && !none && (inside ? piece / V % NT == t : ecol == w.token))
+      dx[w.token] = from_f32<T>(grad_of<MODE == GRAD_H>(xt, at, c, log2s, w) + w.w);
+  }
+}
+
+// Joins the parts of a row.
+constexpr int NTJ = 256;
+template <typename T>
+__global__ __launch_bounds__(NTJ) void logprob_join_kernel(LogprobArgs a, int parts, const float4* rec, const u64* keys) {
+  __shared__ u64 cand[MAX_PARTS * LOGPROB_MAX_TOP];
+  __shared__ u64 bars[NTJ / 64];
+  __shared__ int ncand;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int64_t row = blockIdx.x;
+  const float4 r = lane < parts ? rec[row * parts + lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+  const float m = wave_max(r.x), at = m == -INFINITY ? 0.f : m, c = a.scale * LOG2E;
+  // a part whose maximum is -inf has S = T = 0 (or NaN, which stays one)
+  const float z = fmaxf((r.x - at) * c, FAR), f = __builtin_amdgcn_exp2f(z);
+  const float s = wave_sum(r.y * f), h = wave_sum(fmaf(r.y, -z, r.z) * f);
+  const bool bad = !(s < INFINITY);
+  const float ln = bad ? NAN : logf(s);
+  if (t == 0) {
+    const int token = a.target ? a.target[row] : -1;
+    if (a.logp) a.logp[row] = token >= 0 && token < a.vocab ? log_prob(to_f32(((const T*)a.x)[row * a.ldx + token]), at, a.scale, ln) : 0.f;
+    if (a.stats) { a.stats[2 * row] = m; a.stats[2 * row + 1] = ln; }
+    if (a.entropy) a.entropy[row] = s == 0.f ? 0.f : ln + LN2 * h / s;
+    ncand = 0;
+  }
+  if (a.top == 0) return;
+  keys += row * parts * a.top;
+  // The part whose last key is the largest has `top` keys that reach it, so none below it is among the first.
+  u64 bar = 0;
+  for (int p = t; p < parts; p += NTJ) { const u64 k = keys[p * a.top + a.top - 1]; bar = k > bar ? k : bar; }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) { const u64 o = __shfl_xor(bar, d, 64); bar = o > bar ? o : bar; }
+  if (lane == 0) bars[wave] = bar;
+  __syncthreads();
+  bar = bars[0];
+  for (int i = 1; i < NTJ / 64; ++i) bar = bars[i] > bar ? bars[i] : bar;
+  for (int i = t; i < parts * a.top; i += NTJ) {
+    const u64 k = keys[i];
+    if (k >= bar && k != 0) cand[atomicAdd(&ncand, 1)] = k;
+  }
+  __syncthreads();
+  const int n = ncand;
+  for (int i = t; i < (bad ? a.top : n); i += NTJ) {
+    const u64 key = bad ? 0 : cand[i];
+    int rank = bad ? i : 0;
+    if (!bad)
+      for (int j = 0; j < n; ++j) rank += cand[j] > key;
+    if (rank < a.top) {
+      a.top_id[row * a.top + rank] = bad ? -1 : col_of(key);
+      a.top_logp[row * a.top + rank] = bad ? NAN : log_prob(value_of(key), at, a.scale, ln);
+    }
+  }
+}
+
+// The gradient from a row's statistics: GV pieces of a row to each thread.
+constexpr int NTG = 256, GV = 4;
+template <typename T, bool H>
+__global__ __launch_bounds__(NTG) void logprob_grad_kernel(LogprobArgs a, int chunks) {
+  constexpr int V = vec<T>();
+  const int t = threadIdx.x;
+  const int64_t row = blockIdx.x / chunks;
+  const int chunk = blockIdx.x % chunks;
+  const T* x = (const T*)a.x + row * a.ldx;
+  T* dx = (T*)a.dx + row * a.lddx;
+  const Span<T> sp(x, a.vocab);
+  Weights w = weights_of(a, row, H);
+  const float m = a.stats[2 * row], log2s = a.stats[2 * row + 1] * LOG2E, c = a.scale * LOG2E;
+  if (H) w.h = a.entropy[row];
+  const bool none = w.none || m == -INFINITY, together = (((uintptr_t)dx ^ (uintptr_t)x) & 15) == 0;
+  const int first = chunk * NTG * GV + t;
+  Piece<T> v[GV];
+  const int ecol = chunk == chunks - 1 ? sp.edge(t) : -1;
+  const int piece = w.token - sp.lead;
+  const bool inside = piece >= 0 && w.token < sp.tail;
+  // the token's is stored behind the others, by the same thread
+  const bool owner = w.token >= 0 && !none && (inside ? piece / V / (NTG * GV) == chunk && piece / V % NTG == t : ecol == w.token);
+  float xe = 0.f, xt = 0.f;
+  if (!none) {
+#pragma unroll
+    for (int k = 0; k < GV; ++k)
+      if (first + k * NTG < sp.full) v[k].w = *reinterpret_cast<const uint4*>(x + sp.lead + (int64_t)(first + k * NTG) * V);
+    if (ecol >= 0) xe = to_f32(x[ecol]);
+    if (owner) xt = to_f32(x[w.token]);
+  }
+#pragma unroll
+  for (int k = 0; k < GV; ++k) {
+    if (first + k * NTG >= sp.full) continue;
+    Out<T> o;
+    o.w = make_uint4(0, 0, 0, 0);
+    if (!none) {
+      float f[V];
+      v[k].get(f);
+#pragma unroll
+      for (int e = 0; e < V; ++e) o.v[e] = from_f32<T>(grad_of<H>(f[e], m, c, log2s, w));
+    }
+    T* to = dx + sp.lead + (int64_t)(first + k * NTG) * V;
+    if (together) *reinterpret_cast<uint4*>(to) = o.w;
+    else
+#pragma unroll
+      for (int e = 0; e < V; ++e) to[e] = o.v[e];
+  }
+  if (ecol >= 0) dx[ecol] = from_f32<T>(none ? 0.f : grad_of<H>(xe, m, c, log2s, w));
+  if (owner) dx[w.token] = from_f32<T>(grad_of<H>(xt, m, c, log2s, w) + w.w);
+}
+
+template <typename T> constexpr int most_cols() { return 1024 * 16 * vec<T>(); }
+
+// Parts of a row: as many as it takes, and where the rows do not fill the chip up to a workgroup per compute unit, none below 512 pieces.
+template <typename T> int parts_of(const LogprobArgs& a, int forced) {
+  const int need = (a.vocab + most_cols<T>() - 1) / most_cols<T>();
+  const int fill = a.rows < 256 ? 256 / a.rows : 1, room = a.vocab / (512 * vec<T>());
+  int p = fill < room ? fill : room;
+  p = p > need ? p : need;
+  if (forced) p = p > 3 ? p : a.vocab < 3 ? a.vocab : 3;
+  return p < 1 ? 1 : p > MAX_PARTS ? MAX_PARTS : p;
+}
+size_t part_bytes(const LogprobArgs& a, int parts) { return parts > 1 ? (size_t)a.rows * parts * (sizeof(float4) + a.top * sizeof(u64)) : 0; }
+
+template <typename T, int MODE>
+hipError_t values_launch(const LogprobArgs& a, int parts, void* scratch, hipStream_t s) {
+  // columns of a part: whole pieces; the last part may come out empty of some
+  const int V = vec<T>(), cols = parts > 1 ? ((a.vocab + parts - 1) / parts + V - 1) / V * V : a.vocab;
+  const int used = (a.vocab + cols - 1) / cols;
+  float4* rec = (float4*)scratch;
+  u64* keys = (u64*)(rec + (int64_t)a.rows * used);
+  auto launch = [&](auto nt, auto nv) {
+    constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
+    hipLaunchKernelGGL((logprob_kernel<T, NT, NV, MODE>), dim3((unsigned)((int64_t)a.rows * used)), dim3(NT), 0, s, a, used, cols, rec, keys);
+    return hipGetLastError();
+  };
+  using std::integral_constant;
+  const int pieces = (cols + V - 1) / V;
+  const hipError_t e = pieces <= 256       ? launch(integral_constant<int, 256>{}, integral_constant<int, 1>{})
+                       : pieces <= 1024    ? launch(integral_constant<int, 256>{}, integral_constant<int, 4>{})
+                       : pieces <= 2048    ? launch(integral_constant<int, 256>{}, integral_constant<int, 8>{})
+                       : pieces <= 4096    ? launch(integral_constant<int, 512>{}, integral_constant<int, 8>{})
+                       : pieces <= 8192    ? launch(integral_constant<int, 1024>{}, integral_constant<int, 8>{})
+                                           : launch(integral_constant<int, 1024>{}, integral_constant<int, 16>{});
+  if (e != hipSuccess || used == 1) return e;
+  hipLaunchKernelGGL((logprob_join_kernel<T>), dim3(a.rows), dim3(NTJ), 0, s, a, used, rec, keys);
+  return hipGetLastError();
+}
+
+template <typename T> hipError_t grad_launch(const LogprobArgs& a, hipStream_t s) {
+  const int per = NTG * GV * vec<T>(), chunks = (a.vocab + per - 1) / per;
+  const dim3 grid((unsigned)((int64_t)a.rows * chunks));
+  if (a.dentropy) hipLaunchKernelGGL((logprob_grad_kernel<T, true>), grid, dim3(NTG), 0, s, a, chunks);
+  else hipLaunchKernelGGL((logprob_grad_kernel<T, false>), grid, dim3(NTG), 0, s, a, chunks);
+  return hipGetLastError();
+}
+
+template <typename T> hipError_t values(const LogprobArgs& a, bool forced, void* scratch, hipStream_t s) {
+  const int parts = parts_of<T>(a, forced);
+  return a.top > 0 ? values_launch<T, TOP>(a, parts, scratch, s) : values_launch<T, VALUES>(a, parts, scratch, s);
+}
+template <typename T> hipError_t both(const LogprobArgs& a, bool forced, void* scratch, hipStream_t s) {
+  if (a.top == 0 && parts_of<T>(a, forced) == 1)
+    return a.entropy ? values_launch<T, GRAD_H>(a, 1, scratch, s) : values_launch<T, GRAD>(a, 1, scratch, s);
+  const hipError_t e = values<T>(a, forced, scratch, s);
+  return e == hipSuccess ? grad_launch<T>(a, s) : e;
+}
+
+}  // namespace
+
+size_t logprob_scratch_bytes(DType dt, const LogprobArgs& a) {
+  size_t most = 0;
+  for (const int forced : {0, 1}) {
+    const size_t n = part_bytes(a, dt == DT_F32 ? parts_of<float>(a, forced) : parts_of<bf16>(a, forced));
+    most = n > most ? n : most;
+  }
+  return most;
+}
+hipError_t logprob(DType dt, const LogprobArgs& a, bool split, void* scratch, hipStream_t s) {
+  return dt == DT_F32 ? values<float>(a, split, scratch, s) : values<bf16>(a, split, scratch, s);
+}
+hipError_t logprob_grad(DType dt, const LogprobArgs& a, hipStream_t s) { return dt == DT_F32 ? grad_launch<float>(a, s) : grad_launch<bf16>(a, s); }
+hipError_t logprob_both(DType dt, const LogprobArgs& a, bool split, void* scratch, hipStream_t s) {
+  return dt == DT_F32 ? both<float>(a, split, scratch, s) : both<bf16>(a, split, scratch, s);
+}
+
+}  // namespace stg

@@ -1245,7 +1245,7 @@ int stage_kernel_score_attention_bwd(const stage_score_attention_t* p, const voi
 
 // The arguments that the entries of log probabilities share; gradients and outputs are the caller's to fill in.
 static bool logprob_args(const stage_token_logprob_t* p, LogprobArgs* a) {
-  if (!p || !dtype_ok(p->dtype) || p->rows < 1 || p->rows > 1 << 23 || p->vocab < 1 || p->vocab > 1 << 24 || p->top < 0 || p->top > LOGPROB_MAX_TOP ||
+  if (!p || !dtype_ok(p->dtype) || p->rows < 1 || p->rows > 1 << 21 || p->vocab < 1 || p->vocab > 1 << 22 || p->top < 0 || p->top > LOGPROB_MAX_TOP ||
       p->top > p->vocab || !(p->scale == 0.f || (p->scale >= 1e-30f && p->scale <= 1e30f)) || ((uintptr_t)p->target & 3))
     return false;
   *a = LogprobArgs{};
@@ -1278,6 +1278,7 @@ int stage_kernel_token_logprob_fwd(const stage_token_logprob_t* p, const void* l
       !logprob_values(p, logp, stats, entropy, top_id, top_logp, scratch, scratch_bytes, &a))
     return STAGE_E_INVAL;
   a.x = logits; a.ldx = ld;
+  if (kernel_set != 1) return hip_rc(logprob((DType)p->dtype, a, kernel_set == 2, scratch, (hipStream_t)hip_stream));
   return hip_rc(logprob_ref((DType)p->dtype, a, (hipStream_t)hip_stream));
 }
 
@@ -1289,6 +1290,7 @@ int stage_kernel_token_logprob_bwd(const stage_token_logprob_t* p, const void* l
       !logprob_grads(p, stats, entropy, dlogp, dentropy, dlse, dlogits, ldd, logits, ld, &a))
     return STAGE_E_INVAL;
   a.x = logits; a.ldx = ld;
+  if (kernel_set != 1) return hip_rc(logprob_grad((DType)p->dtype, a, (hipStream_t)hip_stream));
   return hip_rc(logprob_grad_ref((DType)p->dtype, a, (hipStream_t)hip_stream));
 }
 
@@ -1301,6 +1303,7 @@ int stage_kernel_token_logprob_grad(const stage_token_logprob_t* p, const void* 
       !logprob_grads(p, stats, entropy, dlogp, dentropy, dlse, dlogits, ldd, logits, ld, &a))
     return STAGE_E_INVAL;
   a.x = logits; a.ldx = ld;
+  if (kernel_set != 1) return hip_rc(logprob_both((DType)p->dtype, a, kernel_set == 2, scratch, (hipStream_t)hip_stream));
   const hipError_t e = logprob_ref((DType)p->dtype, a, (hipStream_t)hip_stream);
   if (e != hipSuccess) return hip_rc(e);
   return hip_rc(logprob_grad_ref((DType)p->dtype, a, (hipStream_t)hip_stream));
@@ -1308,7 +1311,7 @@ int stage_kernel_token_logprob_grad(const stage_token_logprob_t* p, const void* 
 
 size_t stage_kernel_token_logprob_scratch_bytes(const stage_token_logprob_t* p) {
   LogprobArgs a;
-  return logprob_args(p, &a) ? 0 : 0;
+  return logprob_args(p, &a) ? logprob_scratch_bytes((DType)p->dtype, a) : 0;
 }
 
 // Lists of tensors: sizes within bounds, and a pointer, aligned to es bytes, for each that has elements

@@ -130,7 +130,7 @@ def grad(p, x=A(), ld=100, w=A(), dh=A(), dl=A(), dx=A(1 << 20), ldd=100, logp=A
     return S.lib().stage_kernel_token_logprob_grad(p, x, ld, w, dh, dl, dx, ldd, logp, stats, entropy, ids, tops, scratch, n, 0, None)
 
 
-@pytest.mark.parametrize("kw", [dict(dtype=2), dict(dtype=-1), dict(rows=0), dict(rows=-1), dict(rows=(1 << 23) + 1), dict(vocab=0), dict(vocab=(1 << 24) + 1), dict(top=-1),
+@pytest.mark.parametrize("kw", [dict(dtype=2), dict(dtype=-1), dict(rows=0), dict(rows=-1), dict(rows=(1 << 21) + 1), dict(vocab=0), dict(vocab=(1 << 22) + 1), dict(top=-1),
                                 dict(top=65), dict(vocab=10, top=11), dict(scale=-1.0), dict(scale=math.nan), dict(scale=math.inf), dict(scale=1e-31), dict(scale=1e31),
                                 dict(target=A(2))])
 def test_logprob_refuses_the_problem(kw):
@@ -153,6 +153,18 @@ def test_logprob_refuses_the_tensors():
         assert f(p, dx=None) == S.E_INVAL and f(p, ldd=99) == S.E_INVAL and f(p, dx=A(1)) == S.E_INVAL and f(p, dx=A(), ldd=101) == S.E_INVAL
         assert f(p, stats=None) == S.E_INVAL and f(p, entropy=None) == S.E_INVAL and f(p, w=None, dh=None, dl=None) == S.E_INVAL
         assert f(free) == S.E_INVAL
+
+
+def test_logprob_refuses_the_scratch():
+    from paper_2507_00217_amd import stage as S
+    for kw in (dict(rows=1, vocab=200000), dict(rows=1, vocab=200000, top=64, dtype=0), dict(rows=3, vocab=1 << 22)):
+        p = tlp(**kw)
+        n = S.lib().stage_kernel_token_logprob_scratch_bytes(C.byref(p))
+        assert n > 0
+        for f in (fwd, grad):
+            more = {} if f is fwd else dict(ldd=p.vocab)
+            assert f(C.byref(p), ld=p.vocab, scratch=None, **more) == S.E_INVAL and f(C.byref(p), ld=p.vocab, n=n - 1, **more) == S.E_INVAL
+            assert f(C.byref(p), ld=p.vocab, scratch=A(8), **more) == S.E_INVAL
 
 
 def ptrs(*v):
