@@ -4,13 +4,16 @@
 //   dx_j = scale [p_j (dlse - dlogp - dH (ln p_j + H)) + dlogp [j = token]]
 // An element costs a few operations and an exponential: what bounds it is bytes.
 //
-// A row, or a part of one, lies in the registers of one workgroup: up to 128 Ki columns of bf16 in 64 registers of each of 1024 threads, half of a compute
-// unit's registers.  So the maximum is known before the first exponential, no sum is ever rescaled, and the gradient is formed from the registers
-// too.  Rows that are wider, or too few to fill the chip, are cut into parts; a second launch joins what the parts found.
+// Values alone are a walk over the row: every thread keeps a maximum and sums of its own, which are brought to the row's maximum at the end, so that loads are never waited for
+// by more than their own thread, and little is held in registers.  Rows that are too few to fill the chip are cut into parts, and a second launch joins what the parts found.
 //
-// Alternatives: the k-th largest of the maxima of 64 groups of threads is a lower bound of the k-th largest logit, found in 16 steps of a ballot; the
-// few elements that reach it go to a list in LDS, and each one's rank is the number of list entries before it.  Lists that overflow (rows of ties, or with
-// fewer tokens left than alternatives) are left, and the alternatives are taken out of the row one by one: a thread reads its columns again whenever its best is taken.
+// With the gradient in the same call a row lies in the registers of one workgroup: up to 128 Ki columns of bf16 in 64 registers of each of 1024 threads, half of a compute
+// unit's registers.  The logits are read once, and as soon as a piece's gradient is stored its registers take a piece of the workgroup's next row.
+//
+// Alternatives: the k-th largest of the maxima of 64 groups of threads is a lower bound of the k-th largest logit, found in 16 steps of a ballot.  The walk has left the maximum of
+// every 16 or 32 columns in LDS; the few that reach the bound are read again, their elements that reach it go to a list in LDS, and each one's rank is the number of list
+// entries before it.  Lists that overflow (rows of ties, or with fewer tokens left than alternatives) are left, and the alternatives are taken out of the row one by one: a
+// thread reads its columns again whenever its best is taken.
 #include "common.h"
 
 #include <type_traits>
@@ -23,8 +26,6 @@ constexpr float FAR = -1e4f;           // an exponent below which 2^x is zero ma
 constexpr int CAND = 512;
 constexpr int MAX_PARTS = 64;
 typedef unsigned long long u64;
-
-enum { VALUES = 0, TOP = 1, GRAD = 2, GRAD_H = 3 };      // GRAD: neither H nor its gradient
 
 template <typename T> constexpr int vec() { return 16 / (int)sizeof(T); }
 
@@ -115,6 +116,41 @@ template <bool H> __device__ __forceinline__ float grad_of(float x, float m, flo
   return H ? p * fmaf(-w.b, fmaf(fmaxf(u, FAR), LN2, w.h), w.a) : p * w.a;
 }
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+template <bool H> __device__ __forceinline__ void piece_out(const float (&f)[8], float m, float c, float log2s, const Weights& w, Out<bf16>& o) {
+  unsigned d[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const f32x2 g = {grad_of<H>(f[2 * i], m, c, log2s, w), grad_of<H>(f[2 * i + 1], m, c, log2s, w)};
+    d[i] = __builtin_bit_cast(unsigned, __builtin_convertvector(g, bf16x2));
+  }
+  o.w = make_uint4(d[0], d[1], d[2], d[3]);
+}
+template <bool H> __device__ __forceinline__ void piece_out(const float (&f)[4], float m, float c, float log2s, const Weights& w, Out<float>& o) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o.v[i] = grad_of<H>(f[i], m, c, log2s, w);
+}
+template <typename T, bool H> __device__ __forceinline__ void piece_grad(const Piece<T>& p, float m, float c, float log2s, const Weights& w, Out<T>& o) {
+  float f[vec<T>()];
+  p.get(f);
+  piece_out<H>(f, m, c, log2s, w, o);
+}
+template <typename T> __device__ __forceinline__ void put_apart(T* to, const Out<T>& o, bool together) {
+  if (together) *reinterpret_cast<uint4*>(to) = o.w;
+  else
+#pragma unroll
+    for (int e = 0; e < vec<T>(); ++e) to[e] = o.v[e];
+}
+// entries of a list before `key`; the list is filled up with zeros to a multiple of eight
+__device__ __forceinline__ int rank_of(u64 key, const u64* list, int n) {
+  int rank = 0;
+  for (int j = 0; j < n; j += 8)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) rank += list[j + e] > key;
+  return rank;
+}
+
 // How a row's columns lie: `lead` before the first 16-byte boundary, `full` pieces, and the rest
 template <typename T> struct Span {
   int n, lead, full, tail;
@@ -128,54 +164,96 @@ template <typename T> struct Span {
   __device__ __forceinline__ int edge(int t) const { return t < lead ? t : t - lead < n - tail ? tail + t - lead : -1; }
 };
 
-// One row, or part `blockIdx.x % parts` of one.  parts > 1: what it found goes to rec (m, S, T) and keys.
-template <typename T, int NT, int NV, int MODE>
-__global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a, int parts, int cols, float4* rec, u64* keys) {
+template <typename T> __device__ __forceinline__ float piece_max(const Piece<T>& p) {
+  constexpr int V = vec<T>();
+  float f[V];
+  p.get(f);
+  float m = max3(f[0], f[1], f[2]);
+#pragma unroll
+  for (int e = 3; e < V; e += 2) m = max3(m, f[e], e + 1 < V ? f[e + 1] : f[e]);
+  return m;
+}
+__device__ __forceinline__ float max_of(float a, float b) { return fmaxf(a, b); }
+// what exponents are taken from: the maximum, or zero where there is nothing but -inf
+__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
+
+// One row, or part `blockIdx.x % parts` of one, whose findings go to rec (m, S, T) and keys.  WALK pieces of every thread are loaded while the WALK before them are worked on.
+constexpr int WALK = 4;
+template <typename T, int NT, bool TOP>
+__global__ __launch_bounds__(NT, 8) void logprob_kernel(LogprobArgs a, int parts, int cols, float4* rec, u64* keys) {
   constexpr int V = vec<T>(), WAVES = NT / 64;
-  constexpr bool H = MODE != GRAD, G = MODE == GRAD || MODE == GRAD_H;
+  extern __shared__ float group_max[];             // TOP: [groups][NT]
   __shared__ float gmax[64], red[2][WAVES];
-  __shared__ u64 cand[MODE == TOP ? CAND : 1], best[MODE == TOP ? WAVES : 1];
+  __shared__ u64 cand[TOP ? CAND : 1], best[TOP ? WAVES : 1];
   __shared__ int ncand;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int64_t unit = blockIdx.x, row = parts > 1 ? unit / parts : unit;
   const int c0 = parts > 1 ? (int)(unit % parts) * cols : 0;
   const T* x = (const T*)a.x + row * a.ldx + c0;
   const Span<T> sp(x, min(cols, a.vocab - c0));
-  const int whole = sp.full / NT;                  // pieces that every thread has
-  Piece<T> v[NV];
+  const int groups = (sp.full + NT * WALK - 1) / (NT * WALK);
+  auto load = [&](Piece<T> (&v)[WALK], int g) {
 #pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    if (k < whole) v[k].w = *reinterpret_cast<const uint4*>(x + sp.lead + (k * NT + t) * V);
-    else {
-      v[k].none();
-      if (k * NT + t < sp.full) v[k].w = *reinterpret_cast<const uint4*>(x + sp.lead + (k * NT + t) * V);
+    for (int u = 0; u < WALK; ++u) {
+      const int i = (g * WALK + u) * NT + t;
+      if ((g + 1) * WALK * NT <= sp.full) v[u].w = *reinterpret_cast<const uint4*>(x + sp.lead + i * V);
+      else {
+        v[u].none();
+        if (i < sp.full) v[u].w = *reinterpret_cast<const uint4*>(x + sp.lead + i * V);
+      }
     }
-  }
+  };
+  Piece<T> now[WALK];
+  if (groups > 0) load(now, 0);
   const int ecol = sp.edge(t);
   const float xe = ecol >= 0 ? to_f32(x[ecol]) : -INFINITY;
-  Weights w{};
-  if (G || parts == 1) w = weights_of(a, row, MODE == GRAD_H);
-  float xt = w.token >= 0 && parts == 1 ? to_f32(x[w.token]) : 0.f;
-
-  float vm[MODE == TOP ? NV : 1], tm = xe;
-#pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    if (k * NT >= sp.full) { if (MODE == TOP) vm[k] = -INFINITY; continue; }
-    float f[V], mx;
-    v[k].get(f);
-    mx = max3(f[0], f[1], f[2]);
-#pragma unroll
-    for (int e = 3; e + 1 < V; e += 2) mx = max3(mx, f[e], f[e + 1]);
-    tm = max3(tm, mx, f[V - 1]);
-    if (MODE == TOP) vm[k] = max3(mx, mx, f[V - 1]);
+  const int token = a.target ? a.target[row] : -1;
+  const bool has_token = token >= 0 && token < a.vocab;
+  const float xt = has_token && t == 0 && parts == 1 ? to_f32(x[token]) : 0.f;
+  if (TOP) {
+    for (int i = t; i < CAND; i += NT) cand[i] = 0;
+    if (t == 0) ncand = 0;
   }
-  const float gm = lanes<NT / 64>(tm, [](float p, float q) { return fmaxf(p, q); });
-  if (t % (NT / 64) == 0) gmax[t / (NT / 64)] = gm;
-  if (MODE == TOP && t == 0) ncand = 0;
-  __syncthreads();
-  const float group = gmax[lane], m = wave_max(group), at = m == -INFINITY ? 0.f : m;
 
-  if (MODE == TOP) {
+  const float c = a.scale * LOG2E;
+  float tm = xe, tb = base_of(xe), s = 0.f, h = 0.f;
+  auto term = [&](float f) {
+    const float z = (f - tb) * c, e = __builtin_amdgcn_exp2f(z);
+    s += e;
+    h = fmaf(e, -fmaxf(z, FAR), h);
+  };
+  auto move = [&](float m) {                       // to a maximum of m
+    const float b = base_of(m), z = fmaxf((tm - b) * c, FAR), f = __builtin_amdgcn_exp2f(z);
+    h = fmaf(s, -z, h) * f;
+    s *= f;
+    tm = m;
+    tb = b;
+  };
+  term(xe);
+  for (int g = 0; g < groups; ++g) {
+    Piece<T> next[WALK];
+    if (g + 1 < groups) load(next, g + 1);
+    float m = piece_max(now[0]);
+#pragma unroll
+    for (int u = 1; u < WALK; ++u) m = max_of(m, piece_max(now[u]));
+    if (TOP) group_max[g * NT + t] = m;
+    move(max_of(tm, m));
+#pragma unroll
+    for (int u = 0; u < WALK; ++u) {
+      float f[V];
+      now[u].get(f);
+#pragma unroll
+      for (int e = 0; e < V; ++e) term(f[e]);
+      now[u] = next[u];
+    }
+  }
+  const float gm = lanes<NT / 64>(tm, max_of);
+  if (t % (NT / 64) == 0) gmax[t / (NT / 64)] = gm;
+  __syncthreads();
+  const float group = gmax[lane], m = wave_max(group), at = base_of(m);
+  move(m);
+
+  if (TOP) {
     unsigned reach = 0;                            // the leading 16 bits of the k-th largest group's maximum
     const unsigned mine = ordered(group);
 #pragma unroll
@@ -193,41 +271,28 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a, int parts, i
         if (has && f >= bar && first < CAND) cand[first] = key_of(f, c0 + col);
       }
     };
+    for (int g = 0; g < groups; ++g) {
+      const bool reaches = group_max[g * NT + t] >= bar;
+      if (!__ballot(reaches)) continue;
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const bool has = k * NT + t < sp.full;
-      forget(v[k]);
-      if (__ballot(has && vm[k] >= bar)) {
+      for (int u = 0; u < WALK; ++u) {
+        const int i = (g * WALK + u) * NT + t;
+        const bool has = reaches && i < sp.full;
+        Piece<T> p;
+        p.none();
+        if (has) p.w = *reinterpret_cast<const uint4*>(x + sp.lead + i * V);
         float f[V];
-        v[k].get(f);
+        p.get(f);
 #pragma unroll
-        for (int e = 0; e < V; ++e) offer(has, f[e], sp.lead + (k * NT + t) * V + e);
+        for (int e = 0; e < V; ++e) offer(has, f[e], sp.lead + i * V + e);
       }
     }
     if (wave == 0) offer(ecol >= 0, xe, ecol);
   }
 
-  const float c = a.scale * LOG2E;
-  float s = 0.f, h = 0.f;
-  auto term = [&](float f) {
-    const float z = (f - at) * c, e = __builtin_amdgcn_exp2f(z);
-    s += e;
-    if (H) h = fmaf(e, -fmaxf(z, FAR), h);
-  };
-#pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    if (k * NT >= sp.full) continue;
-    float f[V];
-    forget(v[k]);
-    v[k].get(f);
-#pragma unroll
-    for (int e = 0; e < V; ++e) term(f[e]);
-  }
-  term(xe);
   s = wave_sum(s);
-  if (H) h = wave_sum(h);
+  h = wave_sum(h);
   if (lane == 0) { red[0][wave] = s; red[1][wave] = h; }
-  asm volatile("" : "+v"(xt));                     // has arrived before any thread puts a gradient in its place
   __syncthreads();
   s = red[0][0];
   h = red[1][0];
@@ -235,94 +300,175 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a, int parts, i
   for (int i = 1; i < WAVES; ++i) { s += red[0][i]; h += red[1][i]; }
 
   const bool bad = !(s < INFINITY);
-  const float ln = bad ? NAN : logf(s), entropy = s == 0.f ? 0.f : ln + LN2 * h / s;
+  const float ln = bad ? NAN : logf(s);
   if (t == 0) {
     if (parts > 1) rec[unit] = make_float4(m, s, h, 0.f);
     else {
+      if (a.logp) a.logp[row] = has_token ? log_prob(xt, at, a.scale, ln) : 0.f;
+      if (a.stats) { a.stats[2 * row] = m; a.stats[2 * row + 1] = ln; }
+      if (a.entropy) a.entropy[row] = s == 0.f ? 0.f : ln + LN2 * h / s;
+    }
+  }
+  if (!TOP) return;
+  auto put = [&](int rank, u64 key) {
+    if (parts > 1) keys[unit * a.top + rank] = key;
+    else {
+      a.top_id[row * a.top + rank] = bad ? -1 : col_of(key);
+      a.top_logp[row * a.top + rank] = bad ? NAN : log_prob(value_of(key), at, a.scale, ln);
+    }
+  };
+  const int n = ncand;
+  if (bad) {
+    for (int i = t; i < a.top; i += NT) put(i, 0);
+  } else if (n <= CAND) {
+    for (int i = t; i < n; i += NT) {
+      const u64 key = cand[i];
+      const int rank = rank_of(key, cand, n);
+      if (rank < a.top) put(rank, key);
+    }
+    for (int i = n + t; i < a.top; i += NT) put(i, 0);      // a part with fewer columns
+  } else {
+    u64 last = ~0ull, mine = 0;
+    for (int r = 0; r < a.top; ++r) {
+      if (mine == 0 || mine == last) {             // the thread's largest behind the last one taken
+        mine = 0;
+        auto look = [&](float f, int col) {
+          const u64 key = key_of(f, c0 + col);
+          if (key < last && key > mine) mine = key;
+        };
+        for (int i = t; i < sp.full; i += NT) {
+          Piece<T> p;
+          float f[V];
+          p.w = *reinterpret_cast<const uint4*>(x + sp.lead + i * V);
+          p.get(f);
+#pragma unroll
+          for (int e = 0; e < V; ++e) look(f[e], sp.lead + i * V + e);
+        }
+        if (ecol >= 0) look(xe, ecol);
+      }
+      u64 b = mine;
+#pragma unroll
+      for (int d = 32; d > 0; d >>= 1) { const u64 o = __shfl_xor(b, d, 64); b = o > b ? o : b; }
+      if (lane == 0) best[wave] = b;
+      __syncthreads();
+      b = best[0];
+      for (int i = 1; i < WAVES; ++i) b = best[i] > b ? best[i] : b;
+      __syncthreads();
+      if (t == 0) put(r, b);
+      last = b;
+    }
+  }
+}
+
+// Values and gradient of whole rows, blockIdx.x and every gridDim.x-th behind it.  H: with the entropy.
+template <typename T, int NT, int NV, bool H>
+__global__ __launch_bounds__(NT) void logprob_both_kernel(LogprobArgs a) {
+  constexpr int V = vec<T>(), WAVES = NT / 64;
+  __shared__ float red[3][WAVES];
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const float c = a.scale * LOG2E;
+  auto load = [&](Piece<T>& p, const T* x, const Span<T>& sp, int k) {
+    if ((k + 1) * NT <= sp.full) p.w = *reinterpret_cast<const uint4*>(x + sp.lead + (k * NT + t) * V);
+    else {
+      p.none();
+      if (k * NT + t < sp.full) p.w = *reinterpret_cast<const uint4*>(x + sp.lead + (k * NT + t) * V);
+    }
+  };
+  Piece<T> v[NV];
+  int64_t row = blockIdx.x;
+  const T* x = (const T*)a.x + row * a.ldx;
+  Span<T> sp(x, a.vocab);
+#pragma unroll
+  for (int k = 0; k < NV; ++k) load(v[k], x, sp, k);
+  for (;;) {
+    const int ecol = sp.edge(t);
+    const float xe = ecol >= 0 ? to_f32(x[ecol]) : -INFINITY;
+    Weights w = weights_of(a, row, H);
+    float xt = w.token >= 0 ? to_f32(x[w.token]) : 0.f;
+
+    float m = xe;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      if (k * NT < sp.full) m = max_of(m, piece_max(v[k]));
+    m = wave_max(m);
+    if (lane == 0) red[2][wave] = m;
+    __syncthreads();
+    m = wave_max(lane < WAVES ? red[2][lane] : -INFINITY);
+    const float at = base_of(m);
+
+    float s = 0.f, h = 0.f;
+    auto term = [&](float f) {
+      const float z = (f - at) * c, e = __builtin_amdgcn_exp2f(z);
+      s += e;
+      if (H) h = fmaf(e, -fmaxf(z, FAR), h);
+    };
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      if (k * NT >= sp.full) continue;
+      float f[V];
+      forget(v[k]);
+      v[k].get(f);
+#pragma unroll
+      for (int e = 0; e < V; ++e) term(f[e]);
+    }
+    term(xe);
+    s = wave_sum(s);
+    if (H) h = wave_sum(h);
+    if (lane == 0) { red[0][wave] = s; red[1][wave] = h; }
+    asm volatile("" : "+v"(xt));                   // has arrived before any thread puts a gradient in its place
+    __syncthreads();
+    s = wave_sum(lane < WAVES ? red[0][lane] : 0.f);
+    if (H) h = wave_sum(lane < WAVES ? red[1][lane] : 0.f);
+
+    const bool bad = !(s < INFINITY);
+    const float ln = bad ? NAN : logf(s), entropy = s == 0.f ? 0.f : ln + LN2 * h / s;
+    if (t == 0) {
       if (a.logp) a.logp[row] = w.token >= 0 ? log_prob(xt, at, a.scale, ln) : 0.f;
       if (a.stats) { a.stats[2 * row] = m; a.stats[2 * row + 1] = ln; }
       if (H && a.entropy) a.entropy[row] = entropy;
     }
-  }
 
-  if (MODE == TOP) {
-    auto put = [&](int rank, u64 key) {
-      if (parts > 1) keys[unit * a.top + rank] = key;
-      else {
-        a.top_id[row * a.top + rank] = bad ? -1 : col_of(key);
-        a.top_logp[row * a.top + rank] = bad ? NAN : log_prob(value_of(key), at, a.scale, ln);
-      }
-    };
-    const int n = ncand;
-    if (bad) {
-      for (int i = t; i < a.top; i += NT) put(i, 0);
-    } else if (n <= CAND) {
-      for (int i = t; i < n; i += NT) {
-        const u64 key = cand[i];
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += cand[j] > key;
-        if (rank < a.top) put(rank, key);
-      }
-      for (int i = n + t; i < a.top; i += NT) put(i, 0);      // a part with fewer columns
-    } else {
-      u64 last = ~0ull, mine = 0;
-      for (int r = 0; r < a.top; ++r) {
-        if (mine == 0 || mine == last) {           // the thread's largest behind the last one taken
-          mine = 0;
-          auto look = [&](float f, int col) {
-            const u64 key = key_of(f, c0 + col);
-            if (key < last && key > mine) mine = key;
-          };
-          for (int i = t; i < sp.full; i += NT) {
-            Piece<T> p;
-            float f[V];
-            p.w = *reinterpret_cast<const uint4*>(x + sp.lead + i * V);
-            p.get(f);
-#pragma unroll
-            for (int e = 0; e < V; ++e) look(f[e], sp.lead + i * V + e);
-          }
-          if (ecol >= 0) look(xe, ecol);
-        }
-        u64 b = mine;
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) { const u64 o = __shfl_xor(b, d, 64); b = o > b ? o : b; }
-        if (lane == 0) best[wave] = b;
-        __syncthreads();
-        b = best[0];
-        for (int i = 1; i < WAVES; ++i) b = best[i] > b ? best[i] : b;
-        __syncthreads();
-        if (t == 0) put(r, b);
-        last = b;
-      }
-    }
-  }
-
-  if (G) {
     T* dx = (T*)a.dx + row * a.lddx;
-    if (MODE == GRAD_H) w.h = entropy;
+    if (H) w.h = entropy;
     const bool none = w.none || m == -INFINITY, together = (((uintptr_t)dx ^ (uintptr_t)x) & 15) == 0;
     const float log2s = ln * LOG2E;
+    const int64_t after = row + gridDim.x;
+    const bool more = after < a.rows;
+    const T* xn = more ? (const T*)a.x + after * a.ldx : x;
+    Span<T> spn(xn, more ? a.vocab : 0);
+    if (together && !none) {
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      if (k * NT + t >= sp.full) continue;
-      float f[V];
-      forget(v[k]);
-      v[k].get(f);
-      Out<T> o;
+      for (int k = 0; k < NV; ++k) {
+        if (k * NT + t < sp.full) {
+          Out<T> o;
+          forget(v[k]);
+          piece_grad<T, H>(v[k], at, c, log2s, w, o);
+          *reinterpret_cast<uint4*>(dx + sp.lead + (k * NT + t) * V) = o.w;
+        }
+        load(v[k], xn, spn, k);
+      }
+    } else {
 #pragma unroll
-      for (int e = 0; e < V; ++e) o.v[e] = from_f32<T>(none ? 0.f : grad_of<MODE == GRAD_H>(f[e], at, c, log2s, w));
-      T* to = dx + sp.lead + (k * NT + t) * V;
-      if (together) *reinterpret_cast<uint4*>(to) = o.w;
-      else
-#pragma unroll
-        for (int e = 0; e < V; ++e) to[e] = o.v[e];
+      for (int k = 0; k < NV; ++k) {
+        if (k * NT + t < sp.full) {
+          Out<T> o;
+          forget(v[k]);
+          piece_grad<T, H>(v[k], at, c, log2s, w, o);
+          if (none) o.w = make_uint4(0, 0, 0, 0);
+          put_apart(dx + sp.lead + (k * NT + t) * V, o, together);
+        }
+        load(v[k], xn, spn, k);
+      }
     }
-    if (ecol >= 0) dx[ecol] = from_f32<T>(none ? 0.f : grad_of<MODE == GRAD_H>(xe, at, c, log2s, w));
+    if (ecol >= 0) dx[ecol] = from_f32<T>(none ? 0.f : grad_of<H>(xe, at, c, log2s, w));
     // the token's, by the thread that has stored it above, so that this store comes behind that one
     const int piece = w.token - sp.lead;
     const bool inside = piece >= 0 && w.token < sp.tail;
-    if (w.token >= 0 && !none && (inside ? piece / V % NT == t : ecol == w.token))
-      dx[w.token] = from_f32<T>(grad_of<MODE == GRAD_H>(xt, at, c, log2s, w) + w.w);
+    if (w.token >= 0 && !none && (inside ? piece / V % NT == t : ecol == w.token)) dx[w.token] = from_f32<T>(grad_of<H>(xt, at, c, log2s, w) + w.w);
+    if (!more) break;
+    row = after;
+    x = xn;
+    sp = spn;
   }
 }
 
@@ -330,7 +476,7 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a, int parts, i
 constexpr int NTJ = 256;
 template <typename T>
 __global__ __launch_bounds__(NTJ) void logprob_join_kernel(LogprobArgs a, int parts, const float4* rec, const u64* keys) {
-  __shared__ u64 cand[MAX_PARTS * LOGPROB_MAX_TOP];
+  __shared__ u64 cand[MAX_PARTS * LOGPROB_MAX_TOP + 8];
   __shared__ u64 bars[NTJ / 64];
   __shared__ int ncand;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
@@ -366,11 +512,11 @@ __global__ __launch_bounds__(NTJ) void logprob_join_kernel(LogprobArgs a, int pa
   }
   __syncthreads();
   const int n = ncand;
+  if (t < 8) cand[n + t] = 0;
+  __syncthreads();
   for (int i = t; i < (bad ? a.top : n); i += NTJ) {
     const u64 key = bad ? 0 : cand[i];
-    int rank = bad ? i : 0;
-    if (!bad)
-      for (int j = 0; j < n; ++j) rank += cand[j] > key;
+    const int rank = bad ? i : rank_of(key, cand, n);
     if (rank < a.top) {
       a.top_id[row * a.top + rank] = bad ? -1 : col_of(key);
       a.top_logp[row * a.top + rank] = bad ? NAN : log_prob(value_of(key), at, a.scale, ln);
@@ -412,28 +558,17 @@ __global__ __launch_bounds__(NTG) void logprob_grad_kernel(LogprobArgs a, int ch
   for (int k = 0; k < GV; ++k) {
     if (first + k * NTG >= sp.full) continue;
     Out<T> o;
-    o.w = make_uint4(0, 0, 0, 0);
-    if (!none) {
-      float f[V];
-      v[k].get(f);
-#pragma unroll
-      for (int e = 0; e < V; ++e) o.v[e] = from_f32<T>(grad_of<H>(f[e], m, c, log2s, w));
-    }
-    T* to = dx + sp.lead + (int64_t)(first + k * NTG) * V;
-    if (together) *reinterpret_cast<uint4*>(to) = o.w;
-    else
-#pragma unroll
-      for (int e = 0; e < V; ++e) to[e] = o.v[e];
+    if (none) o.w = make_uint4(0, 0, 0, 0);
+    else piece_grad<T, H>(v[k], m, c, log2s, w, o);
+    put_apart(dx + sp.lead + (int64_t)(first + k * NTG) * V, o, together);
   }
   if (ecol >= 0) dx[ecol] = from_f32<T>(none ? 0.f : grad_of<H>(xe, m, c, log2s, w));
   if (owner) dx[w.token] = from_f32<T>(grad_of<H>(xt, m, c, log2s, w) + w.w);
 }
 
-template <typename T> constexpr int most_cols() { return 1024 * 16 * vec<T>(); }
-
-// Parts of a row: as many as it takes, and where the rows do not fill the chip up to a workgroup per compute unit, none below 512 pieces.
+// Parts of a row: where the rows do not fill the chip up to a workgroup per compute unit, none below 512 pieces; and so many that a part's group maxima take at most 32 KiB.
 template <typename T> int parts_of(const LogprobArgs& a, int forced) {
-  const int need = (a.vocab + most_cols<T>() - 1) / most_cols<T>();
+  const int most = 8192 * WALK * vec<T>(), need = (a.vocab + most - 1) / most;
   const int fill = a.rows < 256 ? 256 / a.rows : 1, room = a.vocab / (512 * vec<T>());
   int p = fill < room ? fill : room;
   p = p > need ? p : need;
@@ -442,29 +577,42 @@ template <typename T> int parts_of(const LogprobArgs& a, int forced) {
 }
 size_t part_bytes(const LogprobArgs& a, int parts) { return parts > 1 ? (size_t)a.rows * parts * (sizeof(float4) + a.top * sizeof(u64)) : 0; }
 
-template <typename T, int MODE>
+using std::integral_constant;
+template <typename T, bool TOP>
 hipError_t values_launch(const LogprobArgs& a, int parts, void* scratch, hipStream_t s) {
-  // columns of a part: whole pieces; the last part may come out empty of some
+  // columns of a part: whole pieces, so that the last parts may have none left
   const int V = vec<T>(), cols = parts > 1 ? ((a.vocab + parts - 1) / parts + V - 1) / V * V : a.vocab;
-  const int used = (a.vocab + cols - 1) / cols;
+  const int used = (a.vocab + cols - 1) / cols, pieces = (cols + V - 1) / V;
   float4* rec = (float4*)scratch;
   u64* keys = (u64*)(rec + (int64_t)a.rows * used);
-  auto launch = [&](auto nt, auto nv) {
-    constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
-    hipLaunchKernelGGL((logprob_kernel<T, NT, NV, MODE>), dim3((unsigned)((int64_t)a.rows * used)), dim3(NT), 0, s, a, used, cols, rec, keys);
+  auto launch = [&](auto nt) {
+    constexpr int NT = decltype(nt)::value;
+    const int groups = (pieces + NT * WALK - 1) / (NT * WALK);
+    hipLaunchKernelGGL((logprob_kernel<T, NT, TOP>), dim3((unsigned)((int64_t)a.rows * used)), dim3(NT), TOP ? groups * NT * sizeof(float) : 0, s, a, used, cols, rec, keys);
     return hipGetLastError();
   };
-  using std::integral_constant;
-  const int pieces = (cols + V - 1) / V;
-  const hipError_t e = pieces <= 256       ? launch(integral_constant<int, 256>{}, integral_constant<int, 1>{})
-                       : pieces <= 1024    ? launch(integral_constant<int, 256>{}, integral_constant<int, 4>{})
-                       : pieces <= 2048    ? launch(integral_constant<int, 256>{}, integral_constant<int, 8>{})
-                       : pieces <= 4096    ? launch(integral_constant<int, 512>{}, integral_constant<int, 8>{})
-                       : pieces <= 8192    ? launch(integral_constant<int, 1024>{}, integral_constant<int, 8>{})
-                                           : launch(integral_constant<int, 1024>{}, integral_constant<int, 16>{});
+  const hipError_t e = pieces <= 2048 ? launch(integral_constant<int, 256>{}) : pieces <= 8192 ? launch(integral_constant<int, 512>{}) : launch(integral_constant<int, 1024>{});
   if (e != hipSuccess || used == 1) return e;
   hipLaunchKernelGGL((logprob_join_kernel<T>), dim3(a.rows), dim3(NTJ), 0, s, a, used, rec, keys);
   return hipGetLastError();
+}
+
+// Rows in registers: at most this many pieces
+constexpr int MOST_PIECES = 1024 * 16;
+template <typename T, bool H> hipError_t both_launch(const LogprobArgs& a, hipStream_t s) {
+  auto launch = [&](auto nt, auto nv, int per_cu) {
+    constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
+    const int wgs = cu_count() * per_cu;
+    hipLaunchKernelGGL((logprob_both_kernel<T, NT, NV, H>), dim3(a.rows < wgs ? a.rows : wgs), dim3(NT), 0, s, a);
+    return hipGetLastError();
+  };
+  const int pieces = (a.vocab + vec<T>() - 1) / vec<T>();
+  return pieces <= 256    ? launch(integral_constant<int, 256>{}, integral_constant<int, 1>{}, 8)
+         : pieces <= 1024 ? launch(integral_constant<int, 256>{}, integral_constant<int, 4>{}, 8)
+         : pieces <= 2048 ? launch(integral_constant<int, 256>{}, integral_constant<int, 8>{}, 6)
+         : pieces <= 4096 ? launch(integral_constant<int, 512>{}, integral_constant<int, 8>{}, 3)
+         : pieces <= 8192 ? launch(integral_constant<int, 1024>{}, integral_constant<int, 8>{}, 1)
+                          : launch(integral_constant<int, 1024>{}, integral_constant<int, 16>{}, 1);
 }
 
 template <typename T> hipError_t grad_launch(const LogprobArgs& a, hipStream_t s) {
@@ -477,11 +625,11 @@ template <typename T> hipError_t grad_launch(const LogprobArgs& a, hipStream_t s
 
 template <typename T> hipError_t values(const LogprobArgs& a, bool forced, void* scratch, hipStream_t s) {
   const int parts = parts_of<T>(a, forced);
-  return a.top > 0 ? values_launch<T, TOP>(a, parts, scratch, s) : values_launch<T, VALUES>(a, parts, scratch, s);
+  return a.top > 0 ? values_launch<T, true>(a, parts, scratch, s) : values_launch<T, false>(a, parts, scratch, s);
 }
 template <typename T> hipError_t both(const LogprobArgs& a, bool forced, void* scratch, hipStream_t s) {
-  if (a.top == 0 && parts_of<T>(a, forced) == 1)
-    return a.entropy ? values_launch<T, GRAD_H>(a, 1, scratch, s) : values_launch<T, GRAD>(a, 1, scratch, s);
+  if (a.top == 0 && parts_of<T>(a, forced) == 1 && a.vocab <= MOST_PIECES * vec<T>())
+    return a.entropy ? both_launch<T, true>(a, s) : both_launch<T, false>(a, s);
   const hipError_t e = values<T>(a, forced, scratch, s);
   return e == hipSuccess ? grad_launch<T>(a, s) : e;
 }
