@@ -10,10 +10,9 @@
 // With the gradient in the same call a row lies in the registers of one workgroup: up to 128 Ki columns of bf16 in 64 registers of each of 1024 threads, half of a compute
 // unit's registers.  The logits are read once, and as soon as a piece's gradient is stored its registers take a piece of the workgroup's next row.
 //
-// Alternatives: the k-th largest of the maxima of 64 groups of threads is a lower bound of the k-th largest logit, found in 16 steps of a ballot.  The walk has left the maximum of
-// every 16 or 32 columns in LDS; the few that reach the bound are read again, their elements that reach it go to a list in LDS, and each one's rank is the number of list
-// entries before it.  Lists that overflow (rows of ties, or with fewer tokens left than alternatives) are left, and the alternatives are taken out of the row one by one: a
-// thread reads its columns again whenever its best is taken.
+// Alternatives: the k-th largest of the maxima of 256 groups of threads is a lower bound of the k-th largest logit, found bit by bit with ballots.  The walk has left the maximum
+// of every 16 or 32 columns in LDS; the few that reach the bound are read again, their elements that reach it go to a list in LDS, and each one's rank is the number of
+// list entries before it.  No more than k groups reach the bound, so lists that overflow are rows of ties, which have a way of their own, and rows made for it.
 #include "common.h"
 
 #include <type_traits>
@@ -23,7 +22,9 @@ namespace {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float FAR = -1e4f;           // an exponent below which 2^x is zero many times over, and x still a number
+constexpr float EDGE = 1e6f;          // magnitude of c m up to which its rounding, 2^-24 of it, is far from a whole exponent
 constexpr int CAND = 512;
+constexpr int BARS = 256;              // groups of threads whose maxima are compared
 constexpr int MAX_PARTS = 64;
 typedef unsigned long long u64;
 
@@ -142,6 +143,12 @@ template <typename T> __device__ __forceinline__ void put_apart(T* to, const Out
 #pragma unroll
     for (int e = 0; e < vec<T>(); ++e) to[e] = o.v[e];
 }
+// n more entries of a list: the first one's place.  (The address is hidden from the compiler, which would make a loop over the lanes of additions to one address.)
+__device__ __forceinline__ int list_take(int* length, int n) {
+  unsigned at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) int*)length;
+  asm volatile("" : "+v"(at));
+  return __hip_atomic_fetch_add((__attribute__((address_space(3))) int*)(uintptr_t)at, n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+}
 // entries of a list before `key`; the list is filled up with zeros to a multiple of eight
 __device__ __forceinline__ int rank_of(u64 key, const u64* list, int n) {
   int rank = 0;
@@ -178,12 +185,14 @@ __device__ __forceinline__ float max_of(float a, float b) { return fmaxf(a, b); 
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
 
 // One row, or part `blockIdx.x % parts` of one, whose findings go to rec (m, S, T) and keys.  WALK pieces of every thread are loaded while the WALK before them are worked on.
+// (Workgroups that go on to a next row, whose first pieces they load before the sums are joined, take registers that leave six wavefronts to a SIMD in the place of eight:
+// 2048 rows x 128000 with 20 alternatives 112 us against 118, but 4000 x 32000 75 against 58.)
 constexpr int WALK = 4;
-template <typename T, int NT, bool TOP>
+template <typename T, int NT, bool TOP, bool H>
 __global__ __launch_bounds__(NT, 8) void logprob_kernel(LogprobArgs a, int parts, int cols, float4* rec, u64* keys) {
   constexpr int V = vec<T>(), WAVES = NT / 64;
   extern __shared__ float group_max[];             // TOP: [groups][NT]
-  __shared__ float gmax[64], red[2][WAVES];
+  __shared__ float gmax[BARS], red[2][WAVES];
   __shared__ u64 cand[TOP ? CAND : 1], best[TOP ? WAVES : 1];
   __shared__ int ncand;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
@@ -204,32 +213,36 @@ __global__ __launch_bounds__(NT, 8) void logprob_kernel(LogprobArgs a, int parts
     }
   };
   Piece<T> now[WALK];
-  if (groups > 0) load(now, 0);
+  load(now, 0);
+  const int token = a.target ? a.target[row] : -1;
   const int ecol = sp.edge(t);
   const float xe = ecol >= 0 ? to_f32(x[ecol]) : -INFINITY;
-  const int token = a.target ? a.target[row] : -1;
-  const bool has_token = token >= 0 && token < a.vocab;
-  const float xt = has_token && t == 0 && parts == 1 ? to_f32(x[token]) : 0.f;
   if (TOP) {
     for (int i = t; i < CAND; i += NT) cand[i] = 0;
     if (t == 0) ncand = 0;
   }
 
-  const float c = a.scale * LOG2E;
-  float tm = xe, tb = base_of(xe), s = 0.f, h = 0.f;
+  // Sums of 2^(c x - base), base the rounding of c times the maximum so far: one fma an element, and no matter what base was rounded to.  A maximum so low that c times
+  // it is beyond -EDGE counts as that; rows whose own is beyond either way are walked again below.
+  const float c = a.scale * LOG2E, low = -EDGE / c;
+  auto base_at = [&](float m) {
+    float b = fmaxf(m, low) * c;
+    asm("" : "+v"(b));                             // rounded here: the compiler would subtract the product itself from another base
+    return b;
+  };
+  float tm = -INFINITY, base = base_at(tm), s = 0.f, h = 0.f;
   auto term = [&](float f) {
-    const float z = (f - tb) * c, e = __builtin_amdgcn_exp2f(z);
+    const float z = fmaf(f, c, -base), e = __builtin_amdgcn_exp2f(z);
     s += e;
-    h = fmaf(e, -fmaxf(z, FAR), h);
+    if (H) h = fmaf(e, -fmaxf(z, FAR), h);
   };
   auto move = [&](float m) {                       // to a maximum of m
-    const float b = base_of(m), z = fmaxf((tm - b) * c, FAR), f = __builtin_amdgcn_exp2f(z);
-    h = fmaf(s, -z, h) * f;
+    const float to = base_at(m), z = fmaxf(base - to, FAR), f = __builtin_amdgcn_exp2f(z);
+    if (H) h = fmaf(s, -z, h) * f;
     s *= f;
     tm = m;
-    tb = b;
+    base = to;
   };
-  term(xe);
   for (int g = 0; g < groups; ++g) {
     Piece<T> next[WALK];
     if (g + 1 < groups) load(next, g + 1);
@@ -247,66 +260,98 @@ __global__ __launch_bounds__(NT, 8) void logprob_kernel(LogprobArgs a, int parts
       now[u] = next[u];
     }
   }
-  const float gm = lanes<NT / 64>(tm, max_of);
-  if (t % (NT / 64) == 0) gmax[t / (NT / 64)] = gm;
+  const bool has_token = token >= 0 && token < a.vocab;
+  const float xt = has_token && t == 0 && parts == 1 ? to_f32(x[token]) : 0.f;
+  move(max_of(tm, xe));
+  term(xe);
+  const float gm = NT > BARS ? max_of(tm, dpp<0xB1>(tm)) : tm;
+  if (t % (NT / BARS) == 0) gmax[t / (NT / BARS)] = gm;
   __syncthreads();
-  const float group = gmax[lane], m = wave_max(group), at = base_of(m);
-  move(m);
-
-  if (TOP) {
-    unsigned reach = 0;                            // the leading 16 bits of the k-th largest group's maximum
-    const unsigned mine = ordered(group);
+  float group[BARS / 64];
 #pragma unroll
-    for (int b = 31; b >= 16; --b) {
-      const unsigned next = reach | 1u << b;
-      if (__builtin_popcountll(__ballot(mine >= next)) >= a.top) reach = next;
-    }
-    const float bar = reach <= 0x007fffffu ? -INFINITY : disordered(reach);
-    auto offer = [&](bool has, float f, int col) {
-      const u64 mask = __ballot(has && f >= bar);
-      if (mask) {
-        int first = 0;
-        if (lane == 0) first = atomicAdd(&ncand, __builtin_popcountll(mask));
-        first = __builtin_amdgcn_readfirstlane(first) + __builtin_popcountll(mask & ((1ull << lane) - 1));
-        if (has && f >= bar && first < CAND) cand[first] = key_of(f, c0 + col);
-      }
+  for (int i = 0; i < BARS / 64; ++i) group[i] = gmax[i * 64 + lane];
+  float m = group[0];
+#pragma unroll
+  for (int i = 1; i < BARS / 64; ++i) m = max_of(m, group[i]);
+  m = wave_max(m);
+  const float at = base_of(m);
+  move(m);
+  // what base is more than c m, so that ln S is that of 2^(c (x - m))
+  float more = fmaf(-m, c, base);
+  if (!(fabsf(m * c) < EDGE) && m != -INFINITY) {
+    s = h = more = 0.f;
+    auto far_term = [&](float f) {
+      const float z = (f - m) * c, e = __builtin_amdgcn_exp2f(z);
+      s += e;
+      if (H) h = fmaf(e, -fmaxf(z, FAR), h);
     };
+    for (int i = t; i < sp.full; i += NT) {
+      Piece<T> p;
+      float f[V];
+      p.w = *reinterpret_cast<const uint4*>(x + sp.lead + i * V);
+      p.get(f);
+#pragma unroll
+      for (int e = 0; e < V; ++e) far_term(f[e]);
+    }
+    if (ecol >= 0) far_term(xe);
+  }
+
+  float bar = 0.f;
+  auto offer = [&](float f, int col) {
+    const int slot = list_take(&ncand, 1);
+    if (slot < CAND) cand[slot] = key_of(f, c0 + col);
+  };
+  // the elements that reach the bar, or are beyond it
+  auto collect = [&](auto wanted) {
     for (int g = 0; g < groups; ++g) {
-      const bool reaches = group_max[g * NT + t] >= bar;
-      if (!__ballot(reaches)) continue;
+      if (!wanted(group_max[g * NT + t])) continue;
+      Piece<T> p[WALK];
+      load(p, g);
 #pragma unroll
       for (int u = 0; u < WALK; ++u) {
         const int i = (g * WALK + u) * NT + t;
-        const bool has = reaches && i < sp.full;
-        Piece<T> p;
-        p.none();
-        if (has) p.w = *reinterpret_cast<const uint4*>(x + sp.lead + i * V);
+        if (!(i < sp.full && wanted(piece_max(p[u])))) continue;
         float f[V];
-        p.get(f);
+        p[u].get(f);
 #pragma unroll
-        for (int e = 0; e < V; ++e) offer(has, f[e], sp.lead + i * V + e);
+        for (int e = 0; e < V; ++e)
+          if (wanted(f[e])) offer(f[e], sp.lead + i * V + e);
       }
     }
-    if (wave == 0) offer(ecol >= 0, xe, ecol);
+    if (ecol >= 0 && wanted(xe)) offer(xe, ecol);
+  };
+  if (TOP) {
+    unsigned reach = 0, mine[BARS / 64];           // the k-th largest group's maximum, which bf16 has in its leading 16 bits
+#pragma unroll
+    for (int i = 0; i < BARS / 64; ++i) mine[i] = ordered(group[i]);
+#pragma unroll
+    for (int b = 31; b >= (sizeof(T) == 2 ? 16 : 0); --b) {
+      const unsigned next = reach | 1u << b;
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < BARS / 64; ++i) n += __builtin_popcountll(__ballot(mine[i] >= next));
+      if (n >= a.top) reach = next;
+    }
+    bar = reach <= 0x007fffffu ? -INFINITY : disordered(reach);
+    collect([&](float f) { return f >= bar; });
   }
 
   s = wave_sum(s);
-  h = wave_sum(h);
+  if (H) h = wave_sum(h);
   if (lane == 0) { red[0][wave] = s; red[1][wave] = h; }
   __syncthreads();
-  s = red[0][0];
-  h = red[1][0];
-#pragma unroll
-  for (int i = 1; i < WAVES; ++i) { s += red[0][i]; h += red[1][i]; }
+  s = wave_sum(lane < WAVES ? red[0][lane] : 0.f);
+  if (H) h = wave_sum(lane < WAVES ? red[1][lane] : 0.f);
 
   const bool bad = !(s < INFINITY);
-  const float ln = bad ? NAN : logf(s);
+  // sum 2^z with z = c (x - m) - more, and the entropy's mean of -z: -more of it is more of the logarithm
+  const float ln = bad ? NAN : s == 0.f ? -INFINITY : logf(s) + LN2 * more;
   if (t == 0) {
-    if (parts > 1) rec[unit] = make_float4(m, s, h, 0.f);
+    if (parts > 1) rec[unit] = make_float4(m, s, h, s == 0.f ? 0.f : more);
     else {
       if (a.logp) a.logp[row] = has_token ? log_prob(xt, at, a.scale, ln) : 0.f;
       if (a.stats) { a.stats[2 * row] = m; a.stats[2 * row + 1] = ln; }
-      if (a.entropy) a.entropy[row] = s == 0.f ? 0.f : ln + LN2 * h / s;
+      if (H && a.entropy) a.entropy[row] = s == 0.f ? 0.f : logf(s) + LN2 * h / s;
     }
   }
   if (!TOP) return;
@@ -317,46 +362,73 @@ __global__ __launch_bounds__(NT, 8) void logprob_kernel(LogprobArgs a, int parts
       a.top_logp[row * a.top + rank] = bad ? NAN : log_prob(value_of(key), at, a.scale, ln);
     }
   };
-  const int n = ncand;
-  if (bad) {
-    for (int i = t; i < a.top; i += NT) put(i, 0);
-  } else if (n <= CAND) {
+  auto put_list = [&](int n) {
     for (int i = t; i < n; i += NT) {
       const u64 key = cand[i];
       const int rank = rank_of(key, cand, n);
       if (rank < a.top) put(rank, key);
     }
+  };
+  int n = ncand;
+  if (bad) {
+    for (int i = t; i < a.top; i += NT) put(i, 0);
+    return;
+  }
+  if (n <= CAND) {
+    put_list(n);
     for (int i = n + t; i < a.top; i += NT) put(i, 0);      // a part with fewer columns
-  } else {
-    u64 last = ~0ull, mine = 0;
-    for (int r = 0; r < a.top; ++r) {
-      if (mine == 0 || mine == last) {             // the thread's largest behind the last one taken
-        mine = 0;
-        auto look = [&](float f, int col) {
-          const u64 key = key_of(f, c0 + col);
-          if (key < last && key > mine) mine = key;
-        };
-        for (int i = t; i < sp.full; i += NT) {
-          Piece<T> p;
-          float f[V];
-          p.w = *reinterpret_cast<const uint4*>(x + sp.lead + i * V);
-          p.get(f);
-#pragma unroll
-          for (int e = 0; e < V; ++e) look(f[e], sp.lead + i * V + e);
-        }
-        if (ecol >= 0) look(xe, ecol);
+    return;
+  }
+  // More than the list takes: as a rule columns that are equal to the bar (a constant row, or the -inf of one with fewer tokens left than alternatives).  The list then takes
+  // those beyond it, and one wavefront finds the first of the equal ones.
+  __syncthreads();
+  for (int i = t; i < CAND; i += NT) cand[i] = 0;
+  if (t == 0) ncand = 0;
+  __syncthreads();
+  collect([&](float f) { return f > bar; });
+  __syncthreads();
+  n = ncand;
+  if (n <= CAND) {
+    put_list(n);
+    if (wave == 0)
+      for (int col = lane, rank = n; rank < a.top && col - lane < sp.n; col += 64) {
+        const bool equal = col < sp.n && to_f32(x[col]) == bar;
+        const u64 mask = __ballot(equal);
+        const int at_rank = rank + __builtin_popcountll(mask & ((1ull << lane) - 1));
+        if (equal && at_rank < a.top) put(at_rank, key_of(bar, c0 + col));
+        rank += __builtin_popcountll(mask);
       }
-      u64 b = mine;
+    return;
+  }
+  // Still more: one by one.
+  u64 last = ~0ull, mine = 0;
+  for (int r = 0; r < a.top; ++r) {
+    if (mine == 0 || mine == last) {               // the thread's largest behind the last one taken
+      mine = 0;
+      auto look = [&](float f, int col) {
+        const u64 key = key_of(f, c0 + col);
+        if (key < last && key > mine) mine = key;
+      };
+      for (int i = t; i < sp.full; i += NT) {
+        Piece<T> p;
+        float f[V];
+        p.w = *reinterpret_cast<const uint4*>(x + sp.lead + i * V);
+        p.get(f);
 #pragma unroll
-      for (int d = 32; d > 0; d >>= 1) { const u64 o = __shfl_xor(b, d, 64); b = o > b ? o : b; }
-      if (lane == 0) best[wave] = b;
-      __syncthreads();
-      b = best[0];
-      for (int i = 1; i < WAVES; ++i) b = best[i] > b ? best[i] : b;
-      __syncthreads();
-      if (t == 0) put(r, b);
-      last = b;
+        for (int e = 0; e < V; ++e) look(f[e], sp.lead + i * V + e);
+      }
+      if (ecol >= 0) look(xe, ecol);
     }
+    u64 b = mine;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) { const u64 o = __shfl_xor(b, d, 64); b = o > b ? o : b; }
+    if (lane == 0) best[wave] = b;
+    __syncthreads();
+    b = best[0];
+    for (int i = 1; i < WAVES; ++i) b = best[i] > b ? best[i] : b;
+    __syncthreads();
+    if (t == 0) put(r, b);
+    last = b;
   }
 }
 
@@ -477,14 +549,13 @@ constexpr int NTJ = 256;
 template <typename T>
 __global__ __launch_bounds__(NTJ) void logprob_join_kernel(LogprobArgs a, int parts, const float4* rec, const u64* keys) {
   __shared__ u64 cand[MAX_PARTS * LOGPROB_MAX_TOP + 8];
-  __shared__ u64 bars[NTJ / 64];
   __shared__ int ncand;
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int t = threadIdx.x, lane = t & 63;
   const int64_t row = blockIdx.x;
   const float4 r = lane < parts ? rec[row * parts + lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
   const float m = wave_max(r.x), at = m == -INFINITY ? 0.f : m, c = a.scale * LOG2E;
   // a part whose maximum is -inf has S = T = 0 (or NaN, which stays one)
-  const float z = fmaxf((r.x - at) * c, FAR), f = __builtin_amdgcn_exp2f(z);
+  const float z = fmaxf(fmaf(r.x - at, c, r.w), FAR), f = __builtin_amdgcn_exp2f(z);
   const float s = wave_sum(r.y * f), h = wave_sum(fmaf(r.y, -z, r.z) * f);
   const bool bad = !(s < INFINITY);
   const float ln = bad ? NAN : logf(s);
@@ -497,18 +568,17 @@ __global__ __launch_bounds__(NTJ) void logprob_join_kernel(LogprobArgs a, int pa
   }
   if (a.top == 0) return;
   keys += row * parts * a.top;
-  // The part whose last key is the largest has `top` keys that reach it, so none below it is among the first.
-  u64 bar = 0;
-  for (int p = t; p < parts; p += NTJ) { const u64 k = keys[p * a.top + a.top - 1]; bar = k > bar ? k : bar; }
+  // With j = ceil(top / parts) and r = ceil(top / j): r parts have j keys each that reach the r-th largest of the parts' j-th keys, so nothing below it is among the first.
+  const int j = (a.top + parts - 1) / parts, r_th = (a.top + j - 1) / j;
+  const unsigned jth = lane < parts ? (unsigned)(keys[lane * a.top + j - 1] >> 32) : 0;
+  unsigned bar = 0;
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) { const u64 o = __shfl_xor(bar, d, 64); bar = o > bar ? o : bar; }
-  if (lane == 0) bars[wave] = bar;
+  for (int b = 31; b >= 0; --b)
+    if (__builtin_popcountll(__ballot(jth >= (bar | 1u << b))) >= r_th) bar |= 1u << b;
   __syncthreads();
-  bar = bars[0];
-  for (int i = 1; i < NTJ / 64; ++i) bar = bars[i] > bar ? bars[i] : bar;
   for (int i = t; i < parts * a.top; i += NTJ) {
     const u64 k = keys[i];
-    if (k >= bar && k != 0) cand[atomicAdd(&ncand, 1)] = k;
+    if ((unsigned)(k >> 32) >= bar && k != 0) cand[list_take(&ncand, 1)] = k;
   }
   __syncthreads();
   const int n = ncand;
@@ -578,7 +648,7 @@ template <typename T> int parts_of(const LogprobArgs& a, int forced) {
 size_t part_bytes(const LogprobArgs& a, int parts) { return parts > 1 ? (size_t)a.rows * parts * (sizeof(float4) + a.top * sizeof(u64)) : 0; }
 
 using std::integral_constant;
-template <typename T, bool TOP>
+template <typename T, bool TOP, bool H>
 hipError_t values_launch(const LogprobArgs& a, int parts, void* scratch, hipStream_t s) {
   // columns of a part: whole pieces, so that the last parts may have none left
   const int V = vec<T>(), cols = parts > 1 ? ((a.vocab + parts - 1) / parts + V - 1) / V * V : a.vocab;
@@ -588,10 +658,10 @@ hipError_t values_launch(const LogprobArgs& a, int parts, void* scratch, hipStre
   auto launch = [&](auto nt) {
     constexpr int NT = decltype(nt)::value;
     const int groups = (pieces + NT * WALK - 1) / (NT * WALK);
-    hipLaunchKernelGGL((logprob_kernel<T, NT, TOP>), dim3((unsigned)((int64_t)a.rows * used)), dim3(NT), TOP ? groups * NT * sizeof(float) : 0, s, a, used, cols, rec, keys);
+    hipLaunchKernelGGL((logprob_kernel<T, NT, TOP, H>), dim3((unsigned)((int64_t)a.rows * used)), dim3(NT), TOP ? groups * NT * sizeof(float) : 0, s, a, used, cols, rec, keys);
     return hipGetLastError();
   };
-  const hipError_t e = pieces <= 2048 ? launch(integral_constant<int, 256>{}) : pieces <= 8192 ? launch(integral_constant<int, 512>{}) : launch(integral_constant<int, 1024>{});
+  const hipError_t e = pieces <= 2048 ? launch(integral_constant<int, 256>{}) : launch(integral_constant<int, 512>{});
   if (e != hipSuccess || used == 1) return e;
   hipLaunchKernelGGL((logprob_join_kernel<T>), dim3(a.rows), dim3(NTJ), 0, s, a, used, rec, keys);
   return hipGetLastError();
@@ -625,7 +695,8 @@ template <typename T> hipError_t grad_launch(const LogprobArgs& a, hipStream_t s
 
 template <typename T> hipError_t values(const LogprobArgs& a, bool forced, void* scratch, hipStream_t s) {
   const int parts = parts_of<T>(a, forced);
-  return a.top > 0 ? values_launch<T, true>(a, parts, scratch, s) : values_launch<T, false>(a, parts, scratch, s);
+  if (a.top > 0) return a.entropy ? values_launch<T, true, true>(a, parts, scratch, s) : values_launch<T, true, false>(a, parts, scratch, s);
+  return a.entropy ? values_launch<T, false, true>(a, parts, scratch, s) : values_launch<T, false, false>(a, parts, scratch, s);
 }
 template <typename T> hipError_t both(const LogprobArgs& a, bool forced, void* scratch, hipStream_t s) {
   if (a.top == 0 && parts_of<T>(a, forced) == 1 && a.vocab <= MOST_PIECES * vec<T>())
