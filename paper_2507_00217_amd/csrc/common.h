@@ -118,11 +118,11 @@ struct LogprobArgs {
 // Lists of tensors of any sizes (stage_kernel_grad_*, stage_kernel_adamw); the arrays are the caller's, on the host.
 struct TensorList { int n; const int64_t* size; };
 struct AdamWArgs {
-  float beta1, rest1, beta2, rest2, eps;       // rest = 1 - beta
-  double lr, decay, lnbeta1, lnbeta2;          // lnbeta = ln beta
+  float lr, decay, eps, beta1, rest1, beta2, rest2;      // rest = 1 - beta
+  float inv1, inv2;              // 1 / (1 - beta^step)
+  double lnbeta1, lnbeta2;
   const float* lr_now;           // device, or null: in the place of lr
-  const int* step_now;           // device, or null: in the place of step
-  int step;
+  const int* step_now;           // device, or null: in the place of the step of inv1 and inv2
   const double* sumsq;           // device, or null: gradients as they are
   float max_norm;
 };

@@ -3,8 +3,9 @@
 //   m = b1 m + (1 - b1) c g,  v = b2 v + (1 - b2) (c g)^2,  w -= lr (wd w + (m / c1) / (sqrt(v / c2) + eps)),  c_i = 1 - b_i^step
 // Every element is moved once per kernel and a few operations are done on it: what bounds all of it is bytes.
 //
-// A list of tensors is cut into chunks of one size, and a launch walks the chunks of up to LIST tensors, which travel with its arguments: nothing is
-// copied to the device beforehand, so that a captured launch holds all that it needs.
+// A list of tensors is cut into chunks of one size, and a launch takes the chunks of as many tensors as travel with its arguments: nothing is copied to the
+// device beforehand, so that a captured launch holds all that it needs.  Clip and step have a workgroup to each chunk, and loads and stores that ask the
+// caches to keep nothing: 202 million fp32 gradients, norm and clip 396 us (2048 workgroups that walk, ordinary accesses: 468), the AdamW step with bf16 weights 1062 us (1283).
 #include "common.h"
 
 #include <type_traits>
@@ -13,11 +14,13 @@ namespace stg {
 namespace {
 
 constexpr int NT = 256;
-constexpr int LIST = 48;
+constexpr int MOST_WGS = 1 << 22;    // of a launch; lists of more chunks than that are walked
+// tensors of K arrays each to a launch: what 4 KB of arguments hold
+template <int K> constexpr int most_tensors() { return 3900 / (24 + 8 * K); }
 
 template <typename T> constexpr int vec() { return 16 / (int)sizeof(T); }
 
-// Up to LIST tensors of K arrays each.  `first`: chunks before the tensor.  `head`: elements of it before the first that lies on a boundary of a group in every
+// `first`: chunks before the tensor.  `head`: elements of it before the first that lies on a boundary of a group in every
 // array, or -1 where there is none in common, which makes the accesses single elements.  (All of a tensor in one entry of 8-byte fields: from an array
 // of bytes beside the arrays of pointers, indexed by the same number t, the compiler made scalar loads at base + t with an offset of 7 t, and scalar loads drop the low two
 // bits of each.)
@@ -27,13 +30,13 @@ template <int K> struct Entry {
 };
 template <int K> struct Lists {
   int64_t n, chunks;
-  Entry<K> e[LIST];
+  Entry<K> e[most_tensors<K>()];
 };
 // One chunk: elements [lo, body) one by one, groups from body on, and what is left of them one by one up to hi
 struct Chunk { int t; int64_t lo, body, hi; bool groups; };
 template <int K, int CHUNK> __device__ __forceinline__ Chunk chunk_of(const Lists<K>& l, int64_t c) {
   int t = 0;
-  for (int step = 32; step > 0; step >>= 1)
+  for (int step = 64; step > 0; step >>= 1)
     if (t + step < l.n && l.e[t + step].first <= c) t += step;
   const int64_t i = c - l.e[t].first, size = l.e[t].size, head = l.e[t].head > 0 ? l.e[t].head : 0;
   Chunk r;
@@ -45,10 +48,12 @@ template <int K, int CHUNK> __device__ __forceinline__ Chunk chunk_of(const List
   return r;
 }
 
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 template <typename T> struct Group {
-  union { uint4 raw; T v[vec<T>()]; } u;
-  __device__ __forceinline__ void load(const T* p) { u.raw = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<uint4*>(p) = u.raw; }
+  union { u32x4 raw; T v[vec<T>()]; } u;
+  __device__ __forceinline__ void load(const T* p) { u.raw = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)); }
+  __device__ __forceinline__ void store(T* p) const { __builtin_nontemporal_store(u.raw, reinterpret_cast<u32x4*>(p)); }
 };
 
 __device__ __forceinline__ double block_sum(double v) {
@@ -121,7 +126,7 @@ __global__ __launch_bounds__(NT) void clip_kernel(Lists<2> l, const double* sums
     const Chunk k = chunk_of<2, CHUNK>(l, c);
     const T* g = (const T*)l.e[k.t].p[0];
     T* o = (T*)l.e[k.t].p[1];
-    if (f == 1.f && g == o) continue;            // nothing to change
+    if (f == 1.f && g == o) continue;              // nothing to change
     auto one = [&](int64_t i) { o[i] = from_f32<T>(f * to_f32(g[i])); };
     auto group = [&](Group<T>& q) {
 #pragma unroll
@@ -150,38 +155,51 @@ __global__ __launch_bounds__(NT) void clip_kernel(Lists<2> l, const double* sums
   }
 }
 
-// N elements that lie side by side, on a boundary of N of them
-template <typename T, int N> struct alignas(sizeof(T) * N) Few { T v[N]; };
+// four elements side by side, on a boundary of four
+template <typename T> struct Four {
+  union { u32x4 w; u32x2 h; T v[4]; } u;
+  __device__ __forceinline__ void load(const T* p) {
+    if (sizeof(T) == 4) u.w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+    else u.h = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
+  }
+  __device__ __forceinline__ void store(T* p) const {
+    if (sizeof(T) == 4) __builtin_nontemporal_store(u.w, reinterpret_cast<u32x4*>(p));
+    else __builtin_nontemporal_store(u.h, reinterpret_cast<u32x2*>(p));
+  }
+};
 
-constexpr int ADAM_V = 4, ADAM_U = 2;
+constexpr int ADAM_V = 4, ADAM_CHUNK = NT * ADAM_V;
 enum { A_W, A_MASTER, A_M, A_V, A_G };
 // The fp32 weights are `master`; with bf16 weights w receives their rounding.
 template <typename TW, typename TG>
 __global__ __launch_bounds__(NT) void adamw_kernel(Lists<5> l, AdamWArgs a) {
-  constexpr int CHUNK = NT * ADAM_V * ADAM_U;
   constexpr bool LP = sizeof(TW) == 2;
-  __shared__ float sh[3];
+  __shared__ float sh[2];
   float f = 1.f;
   if (a.sumsq) {
     if (!(*a.sumsq < INFINITY)) return;
     f = clip_factor(*a.sumsq, a.max_norm);
   }
-  if (threadIdx.x == 0) {
-    const double step = a.step_now ? (double)max(*a.step_now, 1) : (double)a.step;
-    sh[0] = a.lr_now ? *a.lr_now : (float)a.lr;
-    sh[1] = (float)(-1.0 / expm1(step * a.lnbeta1));
-    sh[2] = (float)(-1.0 / expm1(step * a.lnbeta2));
+  float lr = a.lr, i1 = a.inv1, i2 = a.inv2;
+  if (a.lr_now) lr = *a.lr_now;
+  if (a.step_now) {
+    if (threadIdx.x == 0) {
+      const double step = (double)max(*a.step_now, 1);
+      sh[0] = (float)(-1.0 / expm1(step * a.lnbeta1));
+      sh[1] = (float)(-1.0 / expm1(step * a.lnbeta2));
+    }
+    __syncthreads();
+    i1 = sh[0];
+    i2 = sh[1];
   }
-  __syncthreads();
-  const float lr = sh[0], i1 = sh[1], i2 = sh[2], wd = (float)a.decay;
   auto update = [&](float g, float& w, float& m, float& v) {
     g *= f;
     m = fmaf(a.beta1, m, a.rest1 * g);
     v = fmaf(a.beta2, v, a.rest2 * g * g);
-    w = fmaf(-lr, fmaf(wd, w, m * i1 / (sqrtf(v * i2) + a.eps)), w);
+    w = fmaf(-lr, fmaf(a.decay, w, m * i1 / (sqrtf(v * i2) + a.eps)), w);
   };
   for (int64_t c = blockIdx.x; c < l.chunks; c += gridDim.x) {
-    const Chunk k = chunk_of<5, CHUNK>(l, c);
+    const Chunk k = chunk_of<5, ADAM_CHUNK>(l, c);
     TW* w = (TW*)l.e[k.t].p[A_W];
     float *x = (float*)l.e[k.t].p[A_MASTER], *m = (float*)l.e[k.t].p[A_M], *v = (float*)l.e[k.t].p[A_V];
     const TG* g = (const TG*)l.e[k.t].p[A_G];
@@ -191,32 +209,26 @@ __global__ __launch_bounds__(NT) void adamw_kernel(Lists<5> l, AdamWArgs a) {
       x[i] = xi; m[i] = mi; v[i] = vi;
       if (LP) w[i] = from_f32<TW>(xi);
     };
-    using F4 = Few<float, ADAM_V>;
-    using G4 = Few<TG, ADAM_V>;
-    using W4 = Few<TW, ADAM_V>;
-    const int64_t n = k.groups ? (k.hi - k.body) / ADAM_V : 0;
-#pragma unroll
-    for (int u = 0; u < ADAM_U; ++u) {
-      const int64_t i = u * NT + threadIdx.x, at = k.body + i * ADAM_V;
-      if (i < n) {
-        F4 xi = *(const F4*)(x + at), mi = *(const F4*)(m + at), vi = *(const F4*)(v + at);
-        const G4 gi = *(const G4*)(g + at);
-        W4 wi;
-#pragma unroll
-        for (int e = 0; e < ADAM_V; ++e) {
-          update(to_f32(gi.v[e]), xi.v[e], mi.v[e], vi.v[e]);
-          wi.v[e] = from_f32<TW>(xi.v[e]);
-        }
-        *(F4*)(x + at) = xi; *(F4*)(m + at) = mi; *(F4*)(v + at) = vi;
-        if (LP) *(W4*)(w + at) = wi;
+    const int64_t n = k.groups ? (k.hi - k.body) / ADAM_V : 0, at = k.body + (int64_t)threadIdx.x * ADAM_V;
+    if (threadIdx.x < n) {
+      Four<float> xi, mi, vi;
+      Four<TG> gi;
+      Four<TW> wi;
+      xi.load(x + at); mi.load(m + at); vi.load(v + at); gi.load(g + at);
+  #pragma unroll
+      for (int e = 0; e < ADAM_V; ++e) {
+        update(to_f32(gi.u.v[e]), xi.u.v[e], mi.u.v[e], vi.u.v[e]);
+        wi.u.v[e] = from_f32<TW>(xi.u.v[e]);
       }
+      xi.store(x + at); mi.store(m + at); vi.store(v + at);
+      if (LP) wi.store(w + at);
     }
     for (int64_t i = k.body + n * ADAM_V + threadIdx.x; i < k.hi; i += NT) one(i);
     for (int64_t i = k.lo + threadIdx.x; i < k.body; i += NT) one(i);
   }
 }
 
-// Calls launch(lists, workgroups) for up to LIST tensors at a time; with `always` once at least.  es: element sizes of the K arrays; the pointers are
+// Calls launch(lists, workgroups), one to a chunk, for as many tensors at a time as a launch takes; with `always` once at least.  es: element sizes of the K arrays; the pointers are
 // arr[k][i]; an array may be missing (null), which counts as aligned.
 template <int K, int CHUNK, int V, typename F>
 hipError_t over_lists(const TensorList& t, const void* const* const (&arr)[K], const int (&es)[K], bool always, F launch) {
@@ -224,7 +236,7 @@ hipError_t over_lists(const TensorList& t, const void* const* const (&arr)[K], c
   do {
     Lists<K> l;
     l.n = l.chunks = 0;
-    for (; i < t.n && l.n < LIST; ++i) {
+    for (; i < t.n && l.n < most_tensors<K>(); ++i) {
       if (t.size[i] == 0) continue;
       Entry<K>& k = l.e[l.n++];
       int64_t head = -2;
@@ -241,8 +253,7 @@ hipError_t over_lists(const TensorList& t, const void* const* const (&arr)[K], c
       l.chunks += body > CHUNK ? (body + CHUNK - 1) / CHUNK : 1;
     }
     if (l.n || always) {
-      const int64_t chunks = l.chunks;
-      const hipError_t e = launch(l, (int)(chunks < 1 ? 1 : chunks < GRAD_PARTS ? chunks : GRAD_PARTS));
+      const hipError_t e = launch(l, (int)(l.chunks < 1 ? 1 : l.chunks < MOST_WGS ? l.chunks : MOST_WGS));
       if (e != hipSuccess) return e;
     }
     always = false;
@@ -253,7 +264,8 @@ hipError_t over_lists(const TensorList& t, const void* const* const (&arr)[K], c
 template <typename T>
 hipError_t sumsq_launch(const TensorList& l, const void* const* grad, int add, double* sumsq, double* part, hipStream_t s) {
   int left = 0;
-  const hipError_t e = over_lists<1, NT * vec<T>() * SUM_U, vec<T>()>(l, {grad}, {(int)sizeof(T)}, false, [&](const Lists<1>& t, int wgs) {
+  const hipError_t e = over_lists<1, NT * vec<T>() * SUM_U, vec<T>()>(l, {grad}, {(int)sizeof(T)}, false, [&](const Lists<1>& t, int chunks) {
+    const int wgs = chunks < GRAD_PARTS ? chunks : GRAD_PARTS;
     hipLaunchKernelGGL((sumsq_kernel<T>), dim3(wgs), dim3(NT), 0, s, t, part, left);
     left = left > wgs ? left : wgs;
     return hipGetLastError();
@@ -277,7 +289,7 @@ hipError_t adamw_launch(const AdamWArgs& a, const TensorList& l, void* const* w,
                         const void* const* grad, hipStream_t s) {
   const void* const* fp32 = sizeof(TW) == 2 ? (const void* const*)master : (const void* const*)w;
   const void* const* lp = sizeof(TW) == 2 ? (const void* const*)w : nullptr;
-  return over_lists<5, NT * ADAM_V * ADAM_U, ADAM_V>(l, {lp, fp32, (const void* const*)m, (const void* const*)v, grad}, {2, 4, 4, 4, (int)sizeof(TG)}, false,
+  return over_lists<5, ADAM_CHUNK, ADAM_V>(l, {lp, fp32, (const void* const*)m, (const void* const*)v, grad}, {2, 4, 4, 4, (int)sizeof(TG)}, false,
                                                      [&](const Lists<5>& t, int wgs) {
     hipLaunchKernelGGL((adamw_kernel<TW, TG>), dim3(wgs), dim3(NT), 0, s, t, a);
     return hipGetLastError();

@@ -1360,8 +1360,9 @@ int stage_kernel_adamw(const stage_adamw_t* p, int n, const int64_t* size, void*
     return STAGE_E_INVAL;
   AdamWArgs a{};
   a.beta1 = (float)p->beta1; a.rest1 = (float)(1.0 - p->beta1); a.beta2 = (float)p->beta2; a.rest2 = (float)(1.0 - p->beta2); a.eps = (float)p->eps;
-  a.lr = p->lr; a.decay = p->weight_decay; a.lnbeta1 = log(p->beta1); a.lnbeta2 = log(p->beta2);
-  a.lr_now = p->lr_now; a.step_now = p->step_now; a.step = p->step; a.sumsq = p->sumsq; a.max_norm = p->max_norm;
+  a.lr = (float)p->lr; a.decay = (float)p->weight_decay; a.lnbeta1 = log(p->beta1); a.lnbeta2 = log(p->beta2);
+  a.inv1 = (float)(-1.0 / expm1(p->step * a.lnbeta1)); a.inv2 = (float)(-1.0 / expm1(p->step * a.lnbeta2));
+  a.lr_now = p->lr_now; a.step_now = p->step_now; a.sumsq = p->sumsq; a.max_norm = p->max_norm;
   return hip_rc(adamw((DType)p->dtype, (DType)p->grad_dtype, a, TensorList{n, size}, w, master, m, v, grad, (hipStream_t)hip_stream));
 }
 
