@@ -261,6 +261,17 @@ bool attn32_supported(const AttnArgs& a);
 hipError_t attn32_fwd(const AttnArgs& a, hipStream_t s);
 hipError_t attn32_bwd(const AttnArgs& a, hipStream_t s);
 
+// 16 and 8 bytes; ONCE: the caches are asked to keep nothing of them
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+template <bool ONCE, typename V> __device__ __forceinline__ V fetch(const void* p) {
+  return ONCE ? __builtin_nontemporal_load((const V*)p) : *(const V*)p;
+}
+template <bool ONCE, typename V> __device__ __forceinline__ void put(void* p, V v) {
+  if (ONCE) __builtin_nontemporal_store(v, (V*)p);
+  else *(V*)p = v;
+}
+
 // scalar conversions
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(bf16 v) { return (float)v; }

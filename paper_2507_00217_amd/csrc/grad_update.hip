@@ -48,12 +48,11 @@ template <int K, int CHUNK> __device__ __forceinline__ Chunk chunk_of(const List
   return r;
 }
 
-typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-template <typename T> struct Group {
+// ONCE: a list beyond what the last-level cache holds, of which nothing will be found there
+template <typename T, bool ONCE> struct Group {
   union { u32x4 raw; T v[vec<T>()]; } u;
-  __device__ __forceinline__ void load(const T* p) { u.raw = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)); }
-  __device__ __forceinline__ void store(T* p) const { __builtin_nontemporal_store(u.raw, reinterpret_cast<u32x4*>(p)); }
+  __device__ __forceinline__ void load(const T* p) { u.raw = fetch<ONCE, u32x4>(p); }
+  __device__ __forceinline__ void store(T* p) const { put<ONCE>(p, u.raw); }
 };
 
 __device__ __forceinline__ double block_sum(double v) {
@@ -70,7 +69,7 @@ __device__ __forceinline__ double block_sum(double v) {
 constexpr int SUM_U = 8;
 // Squares are formed and added in 64 bits: no gradient is too large or too small for them, and the vector units take fp64 as fast as memory brings it.
 // part[workgroup] += its chunks' sum, or = where no launch before has left one (`left` of them have).
-template <typename T>
+template <typename T, bool ONCE>
 __global__ __launch_bounds__(NT) void sumsq_kernel(Lists<1> l, double* part, int left) {
   constexpr int V = vec<T>(), CHUNK = NT * V * SUM_U;
   double acc[4] = {};
@@ -78,12 +77,12 @@ __global__ __launch_bounds__(NT) void sumsq_kernel(Lists<1> l, double* part, int
     const Chunk k = chunk_of<1, CHUNK>(l, c);
     const T* g = (const T*)l.e[k.t].p[0];
     auto one = [&](int64_t i) { const double v = (double)to_f32(g[i]); acc[0] = fma(v, v, acc[0]); };
-    auto group = [&](const Group<T>& q) {
+    auto group = [&](const Group<T, ONCE>& q) {
 #pragma unroll
       for (int e = 0; e < V; ++e) { const double v = (double)to_f32(q.u.v[e]); acc[e & 3] = fma(v, v, acc[e & 3]); }
     };
     if (k.hi - k.body == CHUNK) {
-      Group<T> q[SUM_U];
+      Group<T, ONCE> q[SUM_U];
 #pragma unroll
       for (int u = 0; u < SUM_U; ++u) q[u].load(g + k.body + (int64_t)(u * NT + threadIdx.x) * V);
 #pragma unroll
@@ -91,7 +90,7 @@ __global__ __launch_bounds__(NT) void sumsq_kernel(Lists<1> l, double* part, int
     } else {
       const int64_t n = (k.hi - k.body) / V;
       for (int64_t i = threadIdx.x; i < n; i += NT) {
-        Group<T> q;
+        Group<T, ONCE> q;
         q.load(g + k.body + i * V);
         group(q);
       }
@@ -117,7 +116,7 @@ __device__ __forceinline__ float clip_factor(double sumsq, float max_norm) {
 }
 
 constexpr int CLIP_U = 4;
-template <typename T>
+template <typename T, bool ONCE>
 __global__ __launch_bounds__(NT) void clip_kernel(Lists<2> l, const double* sumsq, float max_norm, float* norm) {
   constexpr int V = vec<T>(), CHUNK = NT * V * CLIP_U;
   const float f = clip_factor(*sumsq, max_norm);
@@ -128,12 +127,12 @@ __global__ __launch_bounds__(NT) void clip_kernel(Lists<2> l, const double* sums
     T* o = (T*)l.e[k.t].p[1];
     if (f == 1.f && g == o) continue;              // nothing to change
     auto one = [&](int64_t i) { o[i] = from_f32<T>(f * to_f32(g[i])); };
-    auto group = [&](Group<T>& q) {
+    auto group = [&](Group<T, ONCE>& q) {
 #pragma unroll
       for (int e = 0; e < V; ++e) q.u.v[e] = from_f32<T>(f * to_f32(q.u.v[e]));
     };
     if (k.groups && k.hi - k.body == CHUNK) {
-      Group<T> q[CLIP_U];
+      Group<T, ONCE> q[CLIP_U];
 #pragma unroll
       for (int u = 0; u < CLIP_U; ++u) q[u].load(g + k.body + (int64_t)(u * NT + threadIdx.x) * V);
 #pragma unroll
@@ -144,7 +143,7 @@ __global__ __launch_bounds__(NT) void clip_kernel(Lists<2> l, const double* sums
     } else {
       const int64_t n = k.groups ? (k.hi - k.body) / V : 0;
       for (int64_t i = threadIdx.x; i < n; i += NT) {
-        Group<T> q;
+        Group<T, ONCE> q;
         q.load(g + k.body + i * V);
         group(q);
         q.store(o + k.body + i * V);
@@ -156,22 +155,22 @@ __global__ __launch_bounds__(NT) void clip_kernel(Lists<2> l, const double* sums
 }
 
 // four elements side by side, on a boundary of four
-template <typename T> struct Four {
+template <typename T, bool ONCE> struct Four {
   union { u32x4 w; u32x2 h; T v[4]; } u;
   __device__ __forceinline__ void load(const T* p) {
-    if (sizeof(T) == 4) u.w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
-    else u.h = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
+    if (sizeof(T) == 4) u.w = fetch<ONCE, u32x4>(p);
+    else u.h = fetch<ONCE, u32x2>(p);
   }
   __device__ __forceinline__ void store(T* p) const {
-    if (sizeof(T) == 4) __builtin_nontemporal_store(u.w, reinterpret_cast<u32x4*>(p));
-    else __builtin_nontemporal_store(u.h, reinterpret_cast<u32x2*>(p));
+    if (sizeof(T) == 4) put<ONCE>(p, u.w);
+    else put<ONCE>(p, u.h);
   }
 };
 
 constexpr int ADAM_V = 4, ADAM_CHUNK = NT * ADAM_V;
 enum { A_W, A_MASTER, A_M, A_V, A_G };
 // The fp32 weights are `master`; with bf16 weights w receives their rounding.
-template <typename TW, typename TG>
+template <typename TW, typename TG, bool ONCE>
 __global__ __launch_bounds__(NT) void adamw_kernel(Lists<5> l, AdamWArgs a) {
   constexpr bool LP = sizeof(TW) == 2;
   __shared__ float sh[2];
@@ -211,9 +210,9 @@ __global__ __launch_bounds__(NT) void adamw_kernel(Lists<5> l, AdamWArgs a) {
     };
     const int64_t n = k.groups ? (k.hi - k.body) / ADAM_V : 0, at = k.body + (int64_t)threadIdx.x * ADAM_V;
     if (threadIdx.x < n) {
-      Four<float> xi, mi, vi;
-      Four<TG> gi;
-      Four<TW> wi;
+      Four<float, ONCE> xi, mi, vi;
+      Four<TG, ONCE> gi;
+      Four<TW, ONCE> wi;
       xi.load(x + at); mi.load(m + at); vi.load(v + at); gi.load(g + at);
   #pragma unroll
       for (int e = 0; e < ADAM_V; ++e) {
@@ -261,14 +260,27 @@ hipError_t over_lists(const TensorList& t, const void* const* const (&arr)[K], c
   return hipSuccess;
 }
 
+// Whether a list's accesses ask the caches to keep nothing: from 256 MB on, what the last-level cache holds.  (4.2 million parameters, 59 MB: AdamW 12.9 us with ordinary
+// accesses, 14.0 without keeping; 202 million, 6.1 GB: 1152 against 1103.)
+bool once(const TensorList& l, int bytes) {
+  int64_t n = 0;
+  for (int i = 0; i < l.n; ++i) n += l.size[i];
+  return n * bytes > (int64_t)256 << 20;
+}
+template <typename F> hipError_t by_size(bool large, F f) { return large ? f(std::true_type{}) : f(std::false_type{}); }
+
 template <typename T>
 hipError_t sumsq_launch(const TensorList& l, const void* const* grad, int add, double* sumsq, double* part, hipStream_t s) {
   int left = 0;
+  const bool large = once(l, sizeof(T));
   const hipError_t e = over_lists<1, NT * vec<T>() * SUM_U, vec<T>()>(l, {grad}, {(int)sizeof(T)}, false, [&](const Lists<1>& t, int chunks) {
     const int wgs = chunks < GRAD_PARTS ? chunks : GRAD_PARTS;
-    hipLaunchKernelGGL((sumsq_kernel<T>), dim3(wgs), dim3(NT), 0, s, t, part, left);
+    const hipError_t r = by_size(large, [&](auto o) {
+      hipLaunchKernelGGL((sumsq_kernel<T, o()>), dim3(wgs), dim3(NT), 0, s, t, part, left);
+      return hipGetLastError();
+    });
     left = left > wgs ? left : wgs;
-    return hipGetLastError();
+    return r;
   });
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(sumsq_total_kernel, dim3(1), dim3(NT), 0, s, part, left, add, sumsq);
@@ -277,10 +289,14 @@ hipError_t sumsq_launch(const TensorList& l, const void* const* grad, int add, d
 
 template <typename T>
 hipError_t clip_launch(const TensorList& l, const void* const* grad, void* const* out, const double* sumsq, float max_norm, float* norm, hipStream_t s) {
+  const bool large = once(l, 2 * sizeof(T));
   return over_lists<2, NT * vec<T>() * CLIP_U, vec<T>()>(l, {grad, (const void* const*)out}, {(int)sizeof(T), (int)sizeof(T)}, norm != nullptr, [&](const Lists<2>& t, int wgs) {
-    hipLaunchKernelGGL((clip_kernel<T>), dim3(wgs), dim3(NT), 0, s, t, sumsq, max_norm, norm);
+    const hipError_t r = by_size(large, [&](auto o) {
+      hipLaunchKernelGGL((clip_kernel<T, o()>), dim3(wgs), dim3(NT), 0, s, t, sumsq, max_norm, norm);
+      return hipGetLastError();
+    });
     norm = nullptr;
-    return hipGetLastError();
+    return r;
   });
 }
 
@@ -289,10 +305,13 @@ hipError_t adamw_launch(const AdamWArgs& a, const TensorList& l, void* const* w,
                         const void* const* grad, hipStream_t s) {
   const void* const* fp32 = sizeof(TW) == 2 ? (const void* const*)master : (const void* const*)w;
   const void* const* lp = sizeof(TW) == 2 ? (const void* const*)w : nullptr;
+  const bool large = once(l, 24 + sizeof(TG));
   return over_lists<5, ADAM_CHUNK, ADAM_V>(l, {lp, fp32, (const void* const*)m, (const void* const*)v, grad}, {2, 4, 4, 4, (int)sizeof(TG)}, false,
                                                      [&](const Lists<5>& t, int wgs) {
-    hipLaunchKernelGGL((adamw_kernel<TW, TG>), dim3(wgs), dim3(NT), 0, s, t, a);
-    return hipGetLastError();
+    return by_size(large, [&](auto o) {
+      hipLaunchKernelGGL((adamw_kernel<TW, TG, o()>), dim3(wgs), dim3(NT), 0, s, t, a);
+      return hipGetLastError();
+    });
   });
 }
 

@@ -24,7 +24,6 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float FAR = -1e4f;           // an exponent below which 2^x is zero many times over, and x still a number
 constexpr float EDGE = 1e6f;          // magnitude of c m up to which its rounding, 2^-24 of it, is far from a whole exponent
 constexpr int CAND = 512;
-constexpr int BARS = 256;              // groups of threads whose maxima are compared
 constexpr int MAX_PARTS = 64;
 typedef unsigned long long u64;
 
@@ -37,7 +36,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {     // fmaxf 
 }
 template <typename T> struct Piece;
 template <> struct Piece<bf16> {
-  uint4 w;
+  u32x4 w;
   __device__ __forceinline__ void get(float (&f)[8]) const {
     const unsigned d[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -46,19 +45,21 @@ template <> struct Piece<bf16> {
       f[2 * i + 1] = __builtin_bit_cast(float, d[i] & 0xffff0000u);
     }
   }
-  __device__ __forceinline__ void none() { w = make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }
+  __device__ __forceinline__ void none() { w = u32x4{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u}; }
 };
 template <> struct Piece<float> {
-  uint4 w;
+  u32x4 w;
   __device__ __forceinline__ void get(float (&f)[4]) const {
-    f[0] = __builtin_bit_cast(float, w.x); f[1] = __builtin_bit_cast(float, w.y); f[2] = __builtin_bit_cast(float, w.z); f[3] = __builtin_bit_cast(float, w.w);
+    const unsigned d[4] = {w.x, w.y, w.z, w.w};    // (a bit_cast of w.y itself gives w.x)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = __builtin_bit_cast(float, d[i]);
   }
-  __device__ __forceinline__ void none() { w = make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }
+  __device__ __forceinline__ void none() { w = u32x4{0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u}; }
 };
 // From here on the pieces are taken for others: what was unpacked of them is not kept for a later pass, which would be twice the registers.
-template <typename P> __device__ __forceinline__ void forget(P& p) { asm volatile("" : "+v"(p.w.x), "+v"(p.w.y), "+v"(p.w.z), "+v"(p.w.w)); }
+template <typename P> __device__ __forceinline__ void forget(P& p) { asm volatile("" : "+v"(p.w)); }
 template <typename T> union Out {
-  uint4 w;
+  u32x4 w;
   T v[vec<T>()];
 };
 
@@ -126,7 +127,7 @@ template <bool H> __device__ __forceinline__ void piece_out(const float (&f)[8],
     const f32x2 g = {grad_of<H>(f[2 * i], m, c, log2s, w), grad_of<H>(f[2 * i + 1], m, c, log2s, w)};
     d[i] = __builtin_bit_cast(unsigned, __builtin_convertvector(g, bf16x2));
   }
-  o.w = make_uint4(d[0], d[1], d[2], d[3]);
+  o.w = u32x4{d[0], d[1], d[2], d[3]};
 }
 template <bool H> __device__ __forceinline__ void piece_out(const float (&f)[4], float m, float c, float log2s, const Weights& w, Out<float>& o) {
 #pragma unroll
@@ -137,8 +138,8 @@ template <typename T, bool H> __device__ __forceinline__ void piece_grad(const P
   p.get(f);
   piece_out<H>(f, m, c, log2s, w, o);
 }
-template <typename T> __device__ __forceinline__ void put_apart(T* to, const Out<T>& o, bool together) {
-  if (together) *reinterpret_cast<uint4*>(to) = o.w;
+template <bool ONCE, typename T> __device__ __forceinline__ void put_apart(T* to, const Out<T>& o, bool together) {
+  if (together) put<ONCE>(to, o.w);
   else
 #pragma unroll
     for (int e = 0; e < vec<T>(); ++e) to[e] = o.v[e];
@@ -185,12 +186,12 @@ __device__ __forceinline__ float max_of(float a, float b) { return fmaxf(a, b); 
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
 
 // One row, or part `blockIdx.x % parts` of one, whose findings go to rec (m, S, T) and keys.  WALK pieces of every thread are loaded while the WALK before them are worked on.
-// (Workgroups that go on to a next row, whose first pieces they load before the sums are joined, take registers that leave six wavefronts to a SIMD in the place of eight:
-// 2048 rows x 128000 with 20 alternatives 112 us against 118, but 4000 x 32000 75 against 58.)
-constexpr int WALK = 4;
-template <typename T, int NT, bool TOP, bool H>
+// (Four pieces in the place of two: 2000 rows x 50000 46.8 us against 42.5.  Workgroups that go on to a next row, whose first pieces they load before the sums are joined, take
+// registers that leave six wavefronts to a SIMD in the place of eight: 4000 x 32000 with 20 alternatives 75 us against 58.)
+constexpr int WALK = 2;
+template <typename T, int NT, bool TOP, bool H, bool ONCE>
 __global__ __launch_bounds__(NT, 8) void logprob_kernel(LogprobArgs a, int parts, int cols, float4* rec, u64* keys) {
-  constexpr int V = vec<T>(), WAVES = NT / 64;
+  constexpr int V = vec<T>(), WAVES = NT / 64, BARS = NT < 256 ? NT : 256;      // BARS: groups of threads whose maxima are compared
   extern __shared__ float group_max[];             // TOP: [groups][NT]
   __shared__ float gmax[BARS], red[2][WAVES];
   __shared__ u64 cand[TOP ? CAND : 1], best[TOP ? WAVES : 1];
@@ -205,10 +206,10 @@ __global__ __launch_bounds__(NT, 8) void logprob_kernel(LogprobArgs a, int parts
 #pragma unroll
     for (int u = 0; u < WALK; ++u) {
       const int i = (g * WALK + u) * NT + t;
-      if ((g + 1) * WALK * NT <= sp.full) v[u].w = *reinterpret_cast<const uint4*>(x + sp.lead + i * V);
+      if ((g + 1) * WALK * NT <= sp.full) v[u].w = fetch<ONCE, u32x4>(x + sp.lead + i * V);
       else {
         v[u].none();
-        if (i < sp.full) v[u].w = *reinterpret_cast<const uint4*>(x + sp.lead + i * V);
+        if (i < sp.full) v[u].w = fetch<ONCE, u32x4>(x + sp.lead + i * V);
       }
     }
   };
@@ -288,7 +289,7 @@ __global__ __launch_bounds__(NT, 8) void logprob_kernel(LogprobArgs a, int parts
     for (int i = t; i < sp.full; i += NT) {
       Piece<T> p;
       float f[V];
-      p.w = *reinterpret_cast<const uint4*>(x + sp.lead + i * V);
+      p.w = fetch<ONCE, u32x4>(x + sp.lead + i * V);
       p.get(f);
 #pragma unroll
       for (int e = 0; e < V; ++e) far_term(f[e]);
@@ -412,7 +413,7 @@ __global__ __launch_bounds__(NT, 8) void logprob_kernel(LogprobArgs a, int parts
       for (int i = t; i < sp.full; i += NT) {
         Piece<T> p;
         float f[V];
-        p.w = *reinterpret_cast<const uint4*>(x + sp.lead + i * V);
+        p.w = fetch<ONCE, u32x4>(x + sp.lead + i * V);
         p.get(f);
 #pragma unroll
         for (int e = 0; e < V; ++e) look(f[e], sp.lead + i * V + e);
@@ -433,17 +434,17 @@ __global__ __launch_bounds__(NT, 8) void logprob_kernel(LogprobArgs a, int parts
 }
 
 // Values and gradient of whole rows, blockIdx.x and every gridDim.x-th behind it.  H: with the entropy.
-template <typename T, int NT, int NV, bool H>
-__global__ __launch_bounds__(NT) void logprob_both_kernel(LogprobArgs a) {
+template <typename T, int NT, int NV, bool H, bool ONCE>
+__global__ __launch_bounds__(NT, 4) void logprob_both_kernel(LogprobArgs a) {
   constexpr int V = vec<T>(), WAVES = NT / 64;
   __shared__ float red[3][WAVES];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const float c = a.scale * LOG2E;
   auto load = [&](Piece<T>& p, const T* x, const Span<T>& sp, int k) {
-    if ((k + 1) * NT <= sp.full) p.w = *reinterpret_cast<const uint4*>(x + sp.lead + (k * NT + t) * V);
+    if ((k + 1) * NT <= sp.full) p.w = fetch<ONCE, u32x4>(x + sp.lead + (k * NT + t) * V);
     else {
       p.none();
-      if (k * NT + t < sp.full) p.w = *reinterpret_cast<const uint4*>(x + sp.lead + (k * NT + t) * V);
+      if (k * NT + t < sp.full) p.w = fetch<ONCE, u32x4>(x + sp.lead + (k * NT + t) * V);
     }
   };
   Piece<T> v[NV];
@@ -515,7 +516,7 @@ __global__ __launch_bounds__(NT) void logprob_both_kernel(LogprobArgs a) {
           Out<T> o;
           forget(v[k]);
           piece_grad<T, H>(v[k], at, c, log2s, w, o);
-          *reinterpret_cast<uint4*>(dx + sp.lead + (k * NT + t) * V) = o.w;
+          put<ONCE>(dx + sp.lead + (k * NT + t) * V, o.w);
         }
         load(v[k], xn, spn, k);
       }
@@ -526,8 +527,8 @@ __global__ __launch_bounds__(NT) void logprob_both_kernel(LogprobArgs a) {
           Out<T> o;
           forget(v[k]);
           piece_grad<T, H>(v[k], at, c, log2s, w, o);
-          if (none) o.w = make_uint4(0, 0, 0, 0);
-          put_apart(dx + sp.lead + (k * NT + t) * V, o, together);
+          if (none) o.w = u32x4{0, 0, 0, 0};
+          put_apart<ONCE>(dx + sp.lead + (k * NT + t) * V, o, together);
         }
         load(v[k], xn, spn, k);
       }
@@ -596,7 +597,7 @@ __global__ __launch_bounds__(NTJ) void logprob_join_kernel(LogprobArgs a, int pa
 
 // The gradient from a row's statistics: GV pieces of a row to each thread.
 constexpr int NTG = 256, GV = 4;
-template <typename T, bool H>
+template <typename T, bool H, bool ONCE>
 __global__ __launch_bounds__(NTG) void logprob_grad_kernel(LogprobArgs a, int chunks) {
   constexpr int V = vec<T>();
   const int t = threadIdx.x;
@@ -620,7 +621,7 @@ __global__ __launch_bounds__(NTG) void logprob_grad_kernel(LogprobArgs a, int ch
   if (!none) {
 #pragma unroll
     for (int k = 0; k < GV; ++k)
-      if (first + k * NTG < sp.full) v[k].w = *reinterpret_cast<const uint4*>(x + sp.lead + (int64_t)(first + k * NTG) * V);
+      if (first + k * NTG < sp.full) v[k].w = fetch<false, u32x4>(x + sp.lead + (int64_t)(first + k * NTG) * V);
     if (ecol >= 0) xe = to_f32(x[ecol]);
     if (owner) xt = to_f32(x[w.token]);
   }
@@ -628,9 +629,9 @@ __global__ __launch_bounds__(NTG) void logprob_grad_kernel(LogprobArgs a, int ch
   for (int k = 0; k < GV; ++k) {
     if (first + k * NTG >= sp.full) continue;
     Out<T> o;
-    if (none) o.w = make_uint4(0, 0, 0, 0);
+    if (none) o.w = u32x4{0, 0, 0, 0};
     else piece_grad<T, H>(v[k], m, c, log2s, w, o);
-    put_apart(dx + sp.lead + (int64_t)(first + k * NTG) * V, o, together);
+    put_apart<ONCE>(dx + sp.lead + (int64_t)(first + k * NTG) * V, o, together);
   }
   if (ecol >= 0) dx[ecol] = from_f32<T>(none ? 0.f : grad_of<H>(xe, m, c, log2s, w));
   if (owner) dx[w.token] = from_f32<T>(grad_of<H>(xt, m, c, log2s, w) + w.w);
@@ -638,7 +639,7 @@ __global__ __launch_bounds__(NTG) void logprob_grad_kernel(LogprobArgs a, int ch
 
 // Parts of a row: where the rows do not fill the chip up to a workgroup per compute unit, none below 512 pieces; and so many that a part's group maxima take at most 32 KiB.
 template <typename T> int parts_of(const LogprobArgs& a, int forced) {
-  const int most = 8192 * WALK * vec<T>(), need = (a.vocab + most - 1) / most;
+  const int most = 8192 * WALK * vec<T>(), need = a.top > 0 ? (a.vocab + most - 1) / most : 1;
   const int fill = a.rows < 256 ? 256 / a.rows : 1, room = a.vocab / (512 * vec<T>());
   int p = fill < room ? fill : room;
   p = p > need ? p : need;
@@ -648,6 +649,12 @@ template <typename T> int parts_of(const LogprobArgs& a, int forced) {
 size_t part_bytes(const LogprobArgs& a, int parts) { return parts > 1 ? (size_t)a.rows * parts * (sizeof(float4) + a.top * sizeof(u64)) : 0; }
 
 using std::integral_constant;
+// Whether accesses ask the caches to keep nothing.  Values: logits of more than the last-level cache's 256 MB, which leave nothing in it for a backward (2048 rows x 128000 with
+// alternatives 125 us against 131; a backward that finds 103 MB of logits there takes 37 us, 46 otherwise).  Values and gradient: both of more than that together (4096 x 32000
+// 109 us against 116).  The gradient by itself: its stores, from the 32 MB on that the L2s hold (1023 x 50333 in two calls 66 us against 73).
+template <typename T> bool more_than(const LogprobArgs& a, int64_t mb) { return (int64_t)a.rows * a.vocab * (int64_t)sizeof(T) > mb << 20; }
+template <typename F> hipError_t by_size(bool large, F f) { return large ? f(std::true_type{}) : f(std::false_type{}); }
+
 template <typename T, bool TOP, bool H>
 hipError_t values_launch(const LogprobArgs& a, int parts, void* scratch, hipStream_t s) {
   // columns of a part: whole pieces, so that the last parts may have none left
@@ -658,10 +665,19 @@ hipError_t values_launch(const LogprobArgs& a, int parts, void* scratch, hipStre
   auto launch = [&](auto nt) {
     constexpr int NT = decltype(nt)::value;
     const int groups = (pieces + NT * WALK - 1) / (NT * WALK);
-    hipLaunchKernelGGL((logprob_kernel<T, NT, TOP, H>), dim3((unsigned)((int64_t)a.rows * used)), dim3(NT), TOP ? groups * NT * sizeof(float) : 0, s, a, used, cols, rec, keys);
-    return hipGetLastError();
+    return by_size(more_than<T>(a, 256), [&](auto o) {
+      hipLaunchKernelGGL((logprob_kernel<T, NT, TOP, H, o()>), dim3((unsigned)((int64_t)a.rows * used)), dim3(NT), TOP ? groups * NT * sizeof(float) : 0, s, a, used, cols, rec,
+                         keys);
+      return hipGetLastError();
+    });
   };
-  const hipError_t e = pieces <= 2048 ? launch(integral_constant<int, 256>{}) : launch(integral_constant<int, 512>{});
+  // One wavefront a row up to 512 pieces (8192 rows x 2000 10.4 us; in 256 threads 18.9), without alternatives up to 1024 where there are rows enough (8192 x 5000 18.9 us, in 256
+  // threads 23.6; with alternatives 8192 x 8000 49 against 41).  256 threads up to 4096 (5882 x 17000 43.7 us, in 512 50.0), but 512 from 2048 on where the rows do not
+  // fill the chip with them (64 x 128000 in four parts each 14.7 against 18.4).
+  const int64_t units = (int64_t)a.rows * used;
+  const hipError_t e = pieces <= 512 || (!TOP && pieces <= 1024 && units >= 4096)  ? launch(integral_constant<int, 64>{})
+                       : pieces <= 2048 || (pieces <= 4096 && units >= 1024)       ? launch(integral_constant<int, 256>{})
+                                                                                   : launch(integral_constant<int, 512>{});
   if (e != hipSuccess || used == 1) return e;
   hipLaunchKernelGGL((logprob_join_kernel<T>), dim3(a.rows), dim3(NTJ), 0, s, a, used, rec, keys);
   return hipGetLastError();
@@ -673,24 +689,47 @@ template <typename T, bool H> hipError_t both_launch(const LogprobArgs& a, hipSt
   auto launch = [&](auto nt, auto nv, int per_cu) {
     constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
     const int wgs = cu_count() * per_cu;
-    hipLaunchKernelGGL((logprob_both_kernel<T, NT, NV, H>), dim3(a.rows < wgs ? a.rows : wgs), dim3(NT), 0, s, a);
-    return hipGetLastError();
+    return by_size(more_than<T>(a, 128), [&](auto o) {
+      hipLaunchKernelGGL((logprob_both_kernel<T, NT, NV, H, o()>), dim3(a.rows < wgs ? a.rows : wgs), dim3(NT), 0, s, a);
+      return hipGetLastError();
+    });
   };
   const int pieces = (a.vocab + vec<T>() - 1) / vec<T>();
-  return pieces <= 256    ? launch(integral_constant<int, 256>{}, integral_constant<int, 1>{}, 8)
+  // One wavefront a row as far as it goes without giving up registers (8192 rows x 2000 16.3 us, in 256 threads 22); two workgroups of 512 to a compute unit rather than one of
+  // 1024 (2000 x 50000 88.5 us against 98.5), as long as 64 registers of each thread hold the row.
+  return pieces <= 64     ? launch(integral_constant<int, 64>{}, integral_constant<int, 1>{}, 32)
+         : pieces <= 256  ? launch(integral_constant<int, 64>{}, integral_constant<int, 4>{}, 32)
+         : pieces <= 512  ? launch(integral_constant<int, 64>{}, integral_constant<int, 8>{}, 24)
          : pieces <= 1024 ? launch(integral_constant<int, 256>{}, integral_constant<int, 4>{}, 8)
          : pieces <= 2048 ? launch(integral_constant<int, 256>{}, integral_constant<int, 8>{}, 6)
          : pieces <= 4096 ? launch(integral_constant<int, 512>{}, integral_constant<int, 8>{}, 3)
-         : pieces <= 8192 ? launch(integral_constant<int, 1024>{}, integral_constant<int, 8>{}, 1)
+         : pieces <= 8192 ? launch(integral_constant<int, 512>{}, integral_constant<int, 16>{}, 2)
                           : launch(integral_constant<int, 1024>{}, integral_constant<int, 16>{}, 1);
 }
 
-template <typename T> hipError_t grad_launch(const LogprobArgs& a, hipStream_t s) {
-  const int per = NTG * GV * vec<T>(), chunks = (a.vocab + per - 1) / per;
-  const dim3 grid((unsigned)((int64_t)a.rows * chunks));
-  if (a.dentropy) hipLaunchKernelGGL((logprob_grad_kernel<T, true>), grid, dim3(NTG), 0, s, a, chunks);
-  else hipLaunchKernelGGL((logprob_grad_kernel<T, false>), grid, dim3(NTG), 0, s, a, chunks);
-  return hipGetLastError();
+template <typename T> hipError_t grad_launch(LogprobArgs a, hipStream_t s) {
+  const int per = NTG * GV * vec<T>(), chunks = (a.vocab + per - 1) / per, most = (1 << 23) / chunks;
+  const bool large = more_than<T>(a, 32);
+  // up to 2^23 workgroups a launch: logits of more than 137 GB take more than one
+  for (int left = a.rows; left > 0; left -= most) {
+    a.rows = left < most ? left : most;
+    const hipError_t e = by_size(large, [&](auto o) {
+      const dim3 grid(a.rows * chunks);
+      if (a.dentropy) hipLaunchKernelGGL((logprob_grad_kernel<T, true, o()>), grid, dim3(NTG), 0, s, a, chunks);
+      else hipLaunchKernelGGL((logprob_grad_kernel<T, false, o()>), grid, dim3(NTG), 0, s, a, chunks);
+      return hipGetLastError();
+    });
+    if (e != hipSuccess) return e;
+    a.x = (const T*)a.x + most * a.ldx;
+    a.dx = (T*)a.dx + most * a.lddx;
+    a.stats += 2 * (int64_t)most;
+    a.target = a.target ? a.target + most : nullptr;
+    a.entropy = a.entropy ? a.entropy + most : nullptr;
+    a.dlogp = a.dlogp ? a.dlogp + most : nullptr;
+    a.dentropy = a.dentropy ? a.dentropy + most : nullptr;
+    a.dlse = a.dlse ? a.dlse + most : nullptr;
+  }
+  return hipSuccess;
 }
 
 template <typename T> hipError_t values(const LogprobArgs& a, bool forced, void* scratch, hipStream_t s) {

@@ -20,4 +20,4 @@ def test_scalar_loads_at_a_register_start_at_the_arguments(code_objects):  # noq
             for base in re.findall(r"s_load_dword\w* s\S+, s\[(\d+:\d+)\], s\d+", code):
                 loads += 1
                 assert base == "0:1", (name, base)
-    assert kernels == 2 + 2 + 4 and loads >= kernels
+    assert kernels == 2 * (2 + 2 + 4) and loads >= kernels
