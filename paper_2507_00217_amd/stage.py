@@ -344,6 +344,65 @@ class Stage:
         self._chk(lib().stage_run_subschedule(self.h, make_subops(ops), len(ops), p(X), p(dY), p(Y), p(dX)),
                   "stage_run_subschedule")
 
+    # -- between iterations: the gradients' norm, the clip, the update ------------------------
+    def tensors(self) -> List[Tuple[str, int, int]]:
+        """(name, first element, elements) of every parameter tensor in the flat weight and gradient buffers."""
+        out = []
+        for li in range(self.cfg["n_layers"]):
+            for name in PARAM_IDS:
+                off, r, c = stage_param_layout(self.cfg, li, name)
+                if r * c:
+                    out.append((name, off, r * c))
+        return out
+
+    def grad_sumsq(self, sumsq, add: bool = False):
+        """sumsq (fp64, one element, on the device) = or += the sum of the squares of this stage's gradients: what the stages of a pipeline add up for
+        their common norm."""
+        g = self.grads_tensor()
+        scratch = self._update_scratch()
+        with self.torch.cuda.device(self.device):
+            self._chk(lib().stage_kernel_grad_sumsq(DTYPE["fp32"], 1, (C.c_int64 * 1)(g.numel()), (C.c_void_p * 1)(g.data_ptr()), int(add), sumsq.data_ptr(),
+                                                    scratch.data_ptr(), scratch.numel(), self.stream.cuda_stream), "stage_kernel_grad_sumsq")
+
+    def _update_scratch(self):
+        if getattr(self, "_sumsq_scratch", None) is None:
+            with self.torch.cuda.stream(self.stream):
+                self._sumsq_scratch = self.torch.empty(lib().stage_kernel_grad_sumsq_scratch_bytes(), dtype=self.torch.uint8, device=self.device)
+        return self._sumsq_scratch
+
+    def clip_grads(self, sumsq, max_norm: float, norm=None):
+        """Scales the gradients to a common norm of at most max_norm; norm (fp32, one element) receives what it was."""
+        g = self.grads_tensor()
+        p = (C.c_void_p * 1)(g.data_ptr())
+        with self.torch.cuda.device(self.device):
+            self._chk(lib().stage_kernel_grad_clip(DTYPE["fp32"], 1, (C.c_int64 * 1)(g.numel()), p, p, sumsq.data_ptr(), max_norm,
+                                                   norm.data_ptr() if norm is not None else None, self.stream.cuda_stream), "stage_kernel_grad_clip")
+
+    def adamw_state(self) -> Dict[str, object]:
+        """Moments of zero and, for bf16 weights, their fp32 values, laid out like the gradients; made on the stage's stream."""
+        torch, n = self.torch, self.grads_tensor().numel()
+        with torch.cuda.stream(self.stream):
+            out = {k: torch.zeros(n, dtype=torch.float32, device=self.device) for k in "mv"}
+            if self.tdtype != torch.float32:
+                out["master"] = self._weights.view(self.tdtype)[:n].float()
+        return out
+
+    def adamw(self, state, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.95, eps: float = 1e-8, weight_decay: float = 0.0, sumsq=None,
+              max_norm: float = 0.0):
+        """One AdamW step from the stage's gradients; norm weights and biases do not decay.  With sumsq the gradients are taken scaled to max_norm (they
+        stay as they are themselves), and where it is not finite the step is left out."""
+        g, w, es = self.grads_tensor(), self._weights, self._weights.view(self.tdtype).element_size()
+        tensors = self.tensors()
+        for decays in (True, False):
+            group = [t for t in tensors if (t[0][0] == "w") == decays]
+            n = len(group)
+            at = lambda base, size: (C.c_void_p * n)(*[base.data_ptr() + off * size for _, off, _ in group])
+            p = AdamW(dtype=DTYPE[self.cfg["dtype"]], grad_dtype=DTYPE["fp32"], lr=lr, beta1=beta1, beta2=beta2, eps=eps, weight_decay=weight_decay if decays else 0.0,
+                      sumsq=sumsq.data_ptr() if sumsq is not None else None, step=step, max_norm=max_norm)
+            with self.torch.cuda.device(self.device):
+                self._chk(lib().stage_kernel_adamw(C.byref(p), n, (C.c_int64 * n)(*[size for _, _, size in group]), at(w, es), at(state["master"], 4) if "master" in state else None,
+                                                   at(state["m"], 4), at(state["v"], 4), at(g, 4), self.stream.cuda_stream), "stage_kernel_adamw")
+
     def zero_grads(self):
         self._chk(lib().stage_zero_grads(self.h), "stage_zero_grads")
 
