@@ -433,12 +433,26 @@ __global__ __launch_bounds__(NT, 8) void logprob_kernel(LogprobArgs a, int parts
   }
 }
 
-// Values and gradient of whole rows, blockIdx.x and every gridDim.x-th behind it.  H: with the entropy.
-template <typename T, int NT, int NV, bool H, bool ONCE>
+// 16 bytes of every lane to LDS, lane l's to lds_addr + 16 l; what lies beyond the buffer's bytes comes as zeros.  Inline assembly because the compiler would wait for such a load
+// before any access to LDS; it is awaited by hand.
+typedef int rsrc_words __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char lds_char;
+__device__ __forceinline__ rsrc_words raw_rsrc(const void* base, unsigned bytes) {
+  const uint64_t a = (uint64_t)base;
+  return rsrc_words{(int)(unsigned)a, (int)(unsigned)((a >> 32) & 0xffffu), (int)bytes, 0x00020000};
+}
+__device__ __forceinline__ void load_to_lds(rsrc_words rsrc, unsigned lds_addr, unsigned offset) {
+  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_addr), "v"(offset), "s"(rsrc) : "memory");
+}
+
+// Values and gradient of whole rows, blockIdx.x and every gridDim.x-th behind it.  H: with the entropy.  The next row's last NL pieces are on their way to LDS while this one's
+// exponentials are summed, the others while its gradient is stored.
+template <typename T, int NT, int NV, int NL, bool H, bool ONCE>
 __global__ __launch_bounds__(NT, 4) void logprob_both_kernel(LogprobArgs a) {
   constexpr int V = vec<T>(), WAVES = NT / 64;
   __shared__ float red[3][WAVES];
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  __shared__ u32x4 ahead[NL > 0 ? NL : 1][NL > 0 ? NT : 1];
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const float c = a.scale * LOG2E;
   auto load = [&](Piece<T>& p, const T* x, const Span<T>& sp, int k) {
     if ((k + 1) * NT <= sp.full) p.w = fetch<ONCE, u32x4>(x + sp.lead + (k * NT + t) * V);
@@ -451,18 +465,28 @@ __global__ __launch_bounds__(NT, 4) void logprob_both_kernel(LogprobArgs a) {
   int64_t row = blockIdx.x;
   const T* x = (const T*)a.x + row * a.ldx;
   Span<T> sp(x, a.vocab);
+  int ecol = sp.edge(t);
+  float xe = ecol >= 0 ? to_f32(x[ecol]) : -INFINITY;
+  Weights w = weights_of(a, row, H);
+  float xt = w.token >= 0 ? to_f32(x[w.token]) : 0.f;
 #pragma unroll
   for (int k = 0; k < NV; ++k) load(v[k], x, sp, k);
   for (;;) {
-    const int ecol = sp.edge(t);
-    const float xe = ecol >= 0 ? to_f32(x[ecol]) : -INFINITY;
-    Weights w = weights_of(a, row, H);
-    float xt = w.token >= 0 ? to_f32(x[w.token]) : 0.f;
-
     float m = xe;
 #pragma unroll
     for (int k = 0; k < NV; ++k)
       if (k * NT < sp.full) m = max_of(m, piece_max(v[k]));
+    // the token's has arrived before any thread puts a gradient in its place, and no load that the compiler counts is behind those to LDS
+    asm volatile("" : "+v"(xt), "+v"(m));
+    const int64_t after = row + gridDim.x;
+    const bool more = after < a.rows;
+    const T* xn = more ? (const T*)a.x + after * a.ldx : x;
+    const Span<T> spn(xn, more ? a.vocab : 0);
+    if (NL > 0 && more) {
+      const rsrc_words rsrc = raw_rsrc(xn + spn.lead, (unsigned)spn.full * 16u);
+#pragma unroll
+      for (int l = 0; l < NL; ++l) load_to_lds(rsrc, (unsigned)(size_t)((lds_char*)&ahead[l][0] + wave * 1024), (unsigned)((NV - NL + l) * NT + t) * 16u);
+    }
     m = wave_max(m);
     if (lane == 0) red[2][wave] = m;
     __syncthreads();
@@ -488,7 +512,6 @@ __global__ __launch_bounds__(NT, 4) void logprob_both_kernel(LogprobArgs a) {
     s = wave_sum(s);
     if (H) h = wave_sum(h);
     if (lane == 0) { red[0][wave] = s; red[1][wave] = h; }
-    asm volatile("" : "+v"(xt));                   // has arrived before any thread puts a gradient in its place
     __syncthreads();
     s = wave_sum(lane < WAVES ? red[0][lane] : 0.f);
     if (H) h = wave_sum(lane < WAVES ? red[1][lane] : 0.f);
@@ -505,10 +528,18 @@ __global__ __launch_bounds__(NT, 4) void logprob_both_kernel(LogprobArgs a) {
     if (H) w.h = entropy;
     const bool none = w.none || m == -INFINITY, together = (((uintptr_t)dx ^ (uintptr_t)x) & 15) == 0;
     const float log2s = ln * LOG2E;
-    const int64_t after = row + gridDim.x;
-    const bool more = after < a.rows;
-    const T* xn = more ? (const T*)a.x + after * a.ldx : x;
-    Span<T> spn(xn, more ? a.vocab : 0);
+    if (NL > 0) __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0): the pieces in LDS have landed
+    const int ecoln = spn.edge(t);
+    const float xen = ecoln >= 0 ? to_f32(xn[ecoln]) : -INFINITY;
+    const Weights wn = weights_of(a, more ? after : row, H);
+    const float xtn = more && wn.token >= 0 ? to_f32(xn[wn.token]) : 0.f;
+    auto next = [&](int k) {
+      if (k < NV - NL) load(v[k], xn, spn, k);
+      else {
+        v[k].none();
+        if (k * NT + t < spn.full) v[k].w = ahead[k - (NV - NL)][t];
+      }
+    };
     if (together && !none) {
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
@@ -518,7 +549,7 @@ __global__ __launch_bounds__(NT, 4) void logprob_both_kernel(LogprobArgs a) {
           piece_grad<T, H>(v[k], at, c, log2s, w, o);
           put<ONCE>(dx + sp.lead + (k * NT + t) * V, o.w);
         }
-        load(v[k], xn, spn, k);
+        next(k);
       }
     } else {
 #pragma unroll
@@ -530,7 +561,7 @@ __global__ __launch_bounds__(NT, 4) void logprob_both_kernel(LogprobArgs a) {
           if (none) o.w = u32x4{0, 0, 0, 0};
           put_apart<ONCE>(dx + sp.lead + (k * NT + t) * V, o, together);
         }
-        load(v[k], xn, spn, k);
+        next(k);
       }
     }
     if (ecol >= 0) dx[ecol] = from_f32<T>(none ? 0.f : grad_of<H>(xe, at, c, log2s, w));
@@ -542,6 +573,10 @@ __global__ __launch_bounds__(NT, 4) void logprob_both_kernel(LogprobArgs a) {
     row = after;
     x = xn;
     sp = spn;
+    ecol = ecoln;
+    xe = xen;
+    w = wn;
+    xt = xtn;
   }
 }
 
@@ -686,11 +721,14 @@ hipError_t values_launch(const LogprobArgs& a, int parts, void* scratch, hipStre
 // Rows in registers: at most this many pieces
 constexpr int MOST_PIECES = 1024 * 16;
 template <typename T, bool H> hipError_t both_launch(const LogprobArgs& a, hipStream_t s) {
+#ifndef PNL
+#define PNL 2
+#endif
   auto launch = [&](auto nt, auto nv, int per_cu) {
-    constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
+    constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value, NL = PNL == 0 ? 0 : NV >= 8 ? NV / PNL : 0;
     const int wgs = cu_count() * per_cu;
     return by_size(more_than<T>(a, 128), [&](auto o) {
-      hipLaunchKernelGGL((logprob_both_kernel<T, NT, NV, H, o()>), dim3(a.rows < wgs ? a.rows : wgs), dim3(NT), 0, s, a);
+      hipLaunchKernelGGL((logprob_both_kernel<T, NT, NV, NL, H, o()>), dim3(a.rows < wgs ? a.rows : wgs), dim3(NT), 0, s, a);
       return hipGetLastError();
     });
   };

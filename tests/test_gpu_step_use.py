@@ -363,7 +363,7 @@ def test_the_rules_reach_every_kernel():
     short = {re.sub(r"^.*?(logprob\w*?_kernel)I(.*?)EEv.*$", r"\1 \2", n) for n in found}
     flag = ("Lb0E", "Lb1E")
     want = {f"logprob_kernel {t}Li{nt}E{a}{b}{c}" for t in ("DF16b", "f") for nt in (64, 256, 512) for a in flag for b in flag for c in flag}
-    want |= {f"logprob_both_kernel {t}Li{nt}ELi{nv}E{a}{b}" for t in ("DF16b", "f") for nt, nv in ((64, 1), (64, 4), (64, 8), (256, 4), (256, 8), (512, 8), (512, 16), (1024, 16))
+    want |= {f"logprob_both_kernel {t}Li{nt}ELi{nv}ELi{nl}E{a}{b}" for t in ("DF16b", "f") for nt, nv, nl in ((64, 1, 0), (64, 4, 0), (64, 8, 4), (256, 4, 0), (256, 8, 4), (512, 8, 4), (512, 16, 8), (1024, 16, 8))
              for a in flag for b in flag}
     want |= {f"logprob_grad_kernel {t}{a}{b}" for t in ("DF16b", "f") for a in flag for b in flag}
     assert want <= short, sorted(want - short)
