@@ -8,7 +8,7 @@
 // by more than their own thread, and little is held in registers.  Rows that are too few to fill the chip are cut into parts, and a second launch joins what the parts found.
 //
 // With the gradient in the same call a row lies in the registers of one workgroup: up to 128 Ki columns of bf16 in 64 registers of each of 1024 threads, half of a compute
-// unit's registers.  The logits are read once, and as soon as a piece's gradient is stored its registers take a piece of the workgroup's next row.
+// unit's registers.  The logits are read once; half of the workgroup's next row comes to LDS during the sums, the rest into the registers whose gradient has been stored.
 //
 // Alternatives: the k-th largest of the maxima of 256 groups of threads is a lower bound of the k-th largest logit, found bit by bit with ballots.  The walk has left the maximum
 // of every 16 or 32 columns in LDS; the few that reach the bound are read again, their elements that reach it go to a list in LDS, and each one's rank is the number of
@@ -446,7 +446,8 @@ __device__ __forceinline__ void load_to_lds(rsrc_words rsrc, unsigned lds_addr, 
 }
 
 // Values and gradient of whole rows, blockIdx.x and every gridDim.x-th behind it.  H: with the entropy.  The next row's last NL pieces are on their way to LDS while this one's
-// exponentials are summed, the others while its gradient is stored.
+// exponentials are summed, the others while its gradient is stored.  (4096 rows x 128000: 410 us with half of the pieces by LDS, 429 with a quarter; 446 with none, when memory
+// rests during the sums, since all compute units come to them together; 420 with every second piece instead of the last ones.)
 template <typename T, int NT, int NV, int NL, bool H, bool ONCE>
 __global__ __launch_bounds__(NT, 4) void logprob_both_kernel(LogprobArgs a) {
   constexpr int V = vec<T>(), WAVES = NT / 64;
@@ -721,11 +722,8 @@ hipError_t values_launch(const LogprobArgs& a, int parts, void* scratch, hipStre
 // Rows in registers: at most this many pieces
 constexpr int MOST_PIECES = 1024 * 16;
 template <typename T, bool H> hipError_t both_launch(const LogprobArgs& a, hipStream_t s) {
-#ifndef PNL
-#define PNL 2
-#endif
   auto launch = [&](auto nt, auto nv, int per_cu) {
-    constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value, NL = PNL == 0 ? 0 : NV >= 8 ? NV / PNL : 0;
+    constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value, NL = NV >= 8 ? NV / 2 : 0;
     const int wgs = cu_count() * per_cu;
     return by_size(more_than<T>(a, 128), [&](auto o) {
       hipLaunchKernelGGL((logprob_both_kernel<T, NT, NV, NL, H, o()>), dim3(a.rows < wgs ? a.rows : wgs), dim3(NT), 0, s, a);
