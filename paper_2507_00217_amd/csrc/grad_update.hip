@@ -55,14 +55,14 @@ template <typename T, bool ONCE> struct Group {
   __device__ __forceinline__ void store(T* p) const { put<ONCE>(p, u.raw); }
 };
 
-__device__ __forceinline__ double block_sum(double v) {
-  __shared__ double red[NT / 64];
+template <int N> __device__ __forceinline__ double block_sum(double v) {
+  __shared__ double red[N / 64];
   for (int w = 32; w > 0; w >>= 1) v += __shfl_xor(v, w, 64);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
   v = red[0];
-  for (int w = 1; w < NT / 64; ++w) v += red[w];
+  for (int w = 1; w < N / 64; ++w) v += red[w];
   return v;
 }
 
@@ -98,15 +98,16 @@ __global__ __launch_bounds__(NT) void sumsq_kernel(Lists<1> l, double* part, int
     }
     for (int64_t i = k.lo + threadIdx.x; i < k.body; i += NT) one(i);
   }
-  const double s = block_sum((acc[0] + acc[1]) + (acc[2] + acc[3]));
+  const double s = block_sum<NT>((acc[0] + acc[1]) + (acc[2] + acc[3]));
   if (threadIdx.x == 0) part[blockIdx.x] = ((int)blockIdx.x < left ? part[blockIdx.x] : 0.0) + s;
 }
 
-__global__ __launch_bounds__(NT) void sumsq_total_kernel(const double* part, int parts, int add, double* sumsq) {
-  double s = 0.0;
-  for (int i = threadIdx.x; i < parts; i += NT) s += part[i];
-  s = block_sum(s);
-  if (threadIdx.x == 0) sumsq[0] = add ? sumsq[0] + s : s;
+constexpr int NTT = 1024;
+__global__ __launch_bounds__(NTT) void sumsq_total_kernel(const double* part, int parts, int add, double* sumsq) {
+  static_assert(GRAD_PARTS == 2 * NTT, "two of them to a thread");
+  const int i = threadIdx.x;
+  const double a = i < parts ? part[i] : 0.0, b = i + NTT < parts ? part[i + NTT] : 0.0, s = block_sum<NTT>(a + b);
+  if (i == 0) sumsq[0] = add ? sumsq[0] + s : s;
 }
 
 // the factor that brings a norm down to max_norm; 1 where the norm is not finite
@@ -283,7 +284,7 @@ hipError_t sumsq_launch(const TensorList& l, const void* const* grad, int add, d
     return r;
   });
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(sumsq_total_kernel, dim3(1), dim3(NT), 0, s, part, left, add, sumsq);
+  hipLaunchKernelGGL(sumsq_total_kernel, dim3(1), dim3(NTT), 0, s, part, left, add, sumsq);
   return hipGetLastError();
 }
 

@@ -10,8 +10,8 @@
 // With the gradient in the same call a row lies in the registers of one workgroup: up to 128 Ki columns of bf16 in 64 registers of each of 1024 threads, half of a compute
 // unit's registers.  The logits are read once; half of the workgroup's next row comes to LDS during the sums, the rest into the registers whose gradient has been stored.
 //
-// Alternatives: the k-th largest of the maxima of 256 groups of threads is a lower bound of the k-th largest logit, found bit by bit with ballots.  The walk has left the maximum
-// of every 16 or 32 columns in LDS; the few that reach the bound are read again, their elements that reach it go to a list in LDS, and each one's rank is the number of
+// Alternatives: the k-th largest of the maxima of 256 (64) groups of threads is a lower bound of the k-th largest logit, found bit by bit with ballots.  The walk has left the maximum
+// of every two pieces in LDS; the few that reach the bound are read again, their elements that reach it go to a list in LDS, and each one's rank is the number of
 // list entries before it.  No more than k groups reach the bound, so lists that overflow are rows of ties, which have a way of their own, and rows made for it.
 #include "common.h"
 
@@ -448,8 +448,9 @@ __device__ __forceinline__ void load_to_lds(rsrc_words rsrc, unsigned lds_addr, 
 // Values and gradient of whole rows, blockIdx.x and every gridDim.x-th behind it.  H: with the entropy.  The next row's last NL pieces are on their way to LDS while this one's
 // exponentials are summed, the others while its gradient is stored.  (4096 rows x 128000: 410 us with half of the pieces by LDS, 429 with a quarter; 446 with none, when memory
 // rests during the sums, since all compute units come to them together; 420 with every second piece instead of the last ones.)
+constexpr int waves_of(int nv) { return nv > 8 ? 4 : nv > 4 ? 6 : 8; }      // wavefronts to a SIMD whose registers hold nv pieces each
 template <typename T, int NT, int NV, int NL, bool H, bool ONCE>
-__global__ __launch_bounds__(NT, 4) void logprob_both_kernel(LogprobArgs a) {
+__global__ __launch_bounds__(NT, waves_of(NV)) void logprob_both_kernel(LogprobArgs a) {
   constexpr int V = vec<T>(), WAVES = NT / 64;
   __shared__ float red[3][WAVES];
   __shared__ u32x4 ahead[NL > 0 ? NL : 1][NL > 0 ? NT : 1];
@@ -721,26 +722,31 @@ hipError_t values_launch(const LogprobArgs& a, int parts, void* scratch, hipStre
 
 // Rows in registers: at most this many pieces
 constexpr int MOST_PIECES = 1024 * 16;
+constexpr int FEW = 256;               // pieces up to which few rows are spread over 256 threads each
 template <typename T, bool H> hipError_t both_launch(const LogprobArgs& a, hipStream_t s) {
-  auto launch = [&](auto nt, auto nv, int per_cu) {
+  const auto launch = [&](auto nt, auto nv) {
     constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value, NL = NV >= 8 ? NV / 2 : 0;
-    const int wgs = cu_count() * per_cu;
-    return by_size(more_than<T>(a, 128), [&](auto o) {
+    const int wgs = cu_count() * (waves_of(NV) * 256 / NT);
+    const auto go = [&](auto o) {
       hipLaunchKernelGGL((logprob_both_kernel<T, NT, NV, NL, H, o()>), dim3(a.rows < wgs ? a.rows : wgs), dim3(NT), 0, s, a);
       return hipGetLastError();
-    });
+    };
+    if constexpr (NT == FEW && NV == 1) return go(std::false_type{});        // 2 MB at most
+    else return by_size(more_than<T>(a, 128), go);
   };
   const int pieces = (a.vocab + vec<T>() - 1) / vec<T>();
-  // One wavefront a row as far as it goes without giving up registers (8192 rows x 2000 16.3 us, in 256 threads 22); two workgroups of 512 to a compute unit rather than one of
+  // One wavefront a row as far as it goes without giving up registers (8192 rows x 2000 16.3 us, in 256 threads 22), but for few rows
+  // (512 x 2000 5.3 us, in 256 threads 4.6); two workgroups of 512 to a compute unit rather than one of
   // 1024 (2000 x 50000 88.5 us against 98.5), as long as 64 registers of each thread hold the row.
-  return pieces <= 64     ? launch(integral_constant<int, 64>{}, integral_constant<int, 1>{}, 32)
-         : pieces <= 256  ? launch(integral_constant<int, 64>{}, integral_constant<int, 4>{}, 32)
-         : pieces <= 512  ? launch(integral_constant<int, 64>{}, integral_constant<int, 8>{}, 24)
-         : pieces <= 1024 ? launch(integral_constant<int, 256>{}, integral_constant<int, 4>{}, 8)
-         : pieces <= 2048 ? launch(integral_constant<int, 256>{}, integral_constant<int, 8>{}, 6)
-         : pieces <= 4096 ? launch(integral_constant<int, 512>{}, integral_constant<int, 8>{}, 3)
-         : pieces <= 8192 ? launch(integral_constant<int, 512>{}, integral_constant<int, 16>{}, 2)
-                          : launch(integral_constant<int, 1024>{}, integral_constant<int, 16>{}, 1);
+  return pieces <= 64     ? launch(integral_constant<int, 64>{}, integral_constant<int, 1>{})
+         : pieces <= 256 && a.rows <= 512 ? launch(integral_constant<int, 256>{}, integral_constant<int, 1>{})
+         : pieces <= 256  ? launch(integral_constant<int, 64>{}, integral_constant<int, 4>{})
+         : pieces <= 512  ? launch(integral_constant<int, 64>{}, integral_constant<int, 8>{})
+         : pieces <= 1024 ? launch(integral_constant<int, 256>{}, integral_constant<int, 4>{})
+         : pieces <= 2048 ? launch(integral_constant<int, 256>{}, integral_constant<int, 8>{})
+         : pieces <= 4096 ? launch(integral_constant<int, 512>{}, integral_constant<int, 8>{})
+         : pieces <= 8192 ? launch(integral_constant<int, 512>{}, integral_constant<int, 16>{})
+                          : launch(integral_constant<int, 1024>{}, integral_constant<int, 16>{});
 }
 
 template <typename T> hipError_t grad_launch(LogprobArgs a, hipStream_t s) {
