@@ -10,7 +10,7 @@
 // With the gradient in the same call a row lies in the registers of one workgroup: up to 128 Ki columns of bf16 in 64 registers of each of 1024 threads, half of a compute
 // unit's registers.  The logits are read once; half of the workgroup's next row comes to LDS during the sums, the rest into the registers whose gradient has been stored.
 //
-// Alternatives: the k-th largest of the maxima of 256 (64) groups of threads is a lower bound of the k-th largest logit, found bit by bit with ballots.  The walk has left the maximum
+// Alternatives: the k-th largest of the maxima of 256 (64) groups of columns is a lower bound of the k-th largest logit, found bit by bit with ballots.  The walk has left the maximum
 // of every two pieces in LDS; the few that reach the bound are read again, their elements that reach it go to a list in LDS, and each one's rank is the number of
 // list entries before it.  No more than k groups reach the bound, so lists that overflow are rows of ties, which have a way of their own, and rows made for it.
 #include "common.h"
@@ -66,18 +66,17 @@ template <typename T> union Out {
 template <int CTRL> __device__ __forceinline__ float dpp(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
 }
-// over the lanes of a group (a 64th of the workgroup), and over a wavefront
-template <int LANES, typename Op> __device__ __forceinline__ float lanes(float v, Op op) {
+template <typename Op> __device__ __forceinline__ float over_wave(float v, Op op) {
   v = op(v, dpp<0xB1>(v));                        // the neighbour
   v = op(v, dpp<0x4E>(v));                        // the other two of four
-  if (LANES >= 8) v = op(v, dpp<0x141>(v));       // mirrored in eight
-  if (LANES >= 16) v = op(v, dpp<0x140>(v));      // mirrored in sixteen
-  if (LANES >= 32) v = op(v, __shfl_xor(v, 16, 64));
-  if (LANES >= 64) v = op(v, __shfl_xor(v, 32, 64));
-  return v;
+  v = op(v, dpp<0x141>(v));                       // mirrored in eight
+  v = op(v, dpp<0x140>(v));                       // mirrored in sixteen
+  v = op(v, __shfl_xor(v, 16, 64));
+  return op(v, __shfl_xor(v, 32, 64));
 }
-__device__ __forceinline__ float wave_max(float v) { return lanes<64>(v, [](float a, float b) { return fmaxf(a, b); }); }
-__device__ __forceinline__ float wave_sum(float v) { return lanes<64>(v, [](float a, float b) { return a + b; }); }
+__device__ __forceinline__ float max_of(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ float wave_max(float v) { return over_wave(v, max_of); }
+__device__ __forceinline__ float wave_sum(float v) { return over_wave(v, [](float a, float b) { return a + b; }); }
 
 // an order of fp32 numbers as one of unsigned ones; zeros of both signs are one
 __device__ __forceinline__ unsigned ordered(float f) {
@@ -181,7 +180,6 @@ template <typename T> __device__ __forceinline__ float piece_max(const Piece<T>&
   for (int e = 3; e < V; e += 2) m = max3(m, f[e], e + 1 < V ? f[e + 1] : f[e]);
   return m;
 }
-__device__ __forceinline__ float max_of(float a, float b) { return fmaxf(a, b); }
 // what exponents are taken from: the maximum, or zero where there is nothing but -inf
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
 
@@ -192,7 +190,8 @@ constexpr int WALK = 2;
 template <typename T, int NT, bool TOP, bool H, bool ONCE>
 __global__ __launch_bounds__(NT, 8) void logprob_kernel(LogprobArgs a, int parts, int cols, float4* rec, u64* keys) {
   constexpr int V = vec<T>(), WAVES = NT / 64, BARS = NT < 256 ? NT : 256;      // BARS: groups of threads whose maxima are compared
-  extern __shared__ float group_max[];             // TOP: [groups][NT]
+  constexpr int KEPT = NT == 64 ? WALK : 1;         // maxima that are kept of a thread's WALK pieces
+  extern __shared__ float group_max[];             // TOP: [groups * KEPT][NT]
   __shared__ float gmax[BARS], red[2][WAVES];
   __shared__ u64 cand[TOP ? CAND : 1], best[TOP ? WAVES : 1];
   __shared__ int ncand;
@@ -247,10 +246,14 @@ __global__ __launch_bounds__(NT, 8) void logprob_kernel(LogprobArgs a, int parts
   for (int g = 0; g < groups; ++g) {
     Piece<T> next[WALK];
     if (g + 1 < groups) load(next, g + 1);
-    float m = piece_max(now[0]);
+    float m = -INFINITY;
 #pragma unroll
-    for (int u = 1; u < WALK; ++u) m = max_of(m, piece_max(now[u]));
-    if (TOP) group_max[g * NT + t] = m;
+    for (int u = 0; u < WALK; ++u) {
+      const float q = piece_max(now[u]);
+      m = u ? max_of(m, q) : q;
+      if (TOP && KEPT > 1) group_max[(g * WALK + u) * NT + t] = q;
+    }
+    if (TOP && KEPT == 1) group_max[g * NT + t] = m;
     move(max_of(tm, m));
 #pragma unroll
     for (int u = 0; u < WALK; ++u) {
@@ -304,13 +307,18 @@ __global__ __launch_bounds__(NT, 8) void logprob_kernel(LogprobArgs a, int parts
   };
   // the elements that reach the bar, or are beyond it
   auto collect = [&](auto wanted) {
-    for (int g = 0; g < groups; ++g) {
+    for (int g = 0; g < groups * KEPT; ++g) {
       if (!wanted(group_max[g * NT + t])) continue;
-      Piece<T> p[WALK];
-      load(p, g);
+      Piece<T> p[WALK / KEPT];
 #pragma unroll
-      for (int u = 0; u < WALK; ++u) {
-        const int i = (g * WALK + u) * NT + t;
+      for (int u = 0; u < WALK / KEPT; ++u) {
+        const int i = (g * (WALK / KEPT) + u) * NT + t;
+        p[u].none();
+        if (i < sp.full) p[u].w = fetch<ONCE, u32x4>(x + sp.lead + i * V);
+      }
+#pragma unroll
+      for (int u = 0; u < WALK / KEPT; ++u) {
+        const int i = (g * (WALK / KEPT) + u) * NT + t;
         if (!(i < sp.full && wanted(piece_max(p[u])))) continue;
         float f[V];
         p[u].get(f);
@@ -322,15 +330,49 @@ __global__ __launch_bounds__(NT, 8) void logprob_kernel(LogprobArgs a, int parts
     if (ecol >= 0 && wanted(xe)) offer(xe, ecol);
   };
   if (TOP) {
-    unsigned reach = 0, mine[BARS / 64];           // the k-th largest group's maximum, which bf16 has in its leading 16 bits
+    // The k-th largest of the groups' maxima, which bf16 has in its leading 16 bits.  One wavefront: of its 64 lanes, or, for more alternatives than half of them, of
+    // four groups to a lane: pairs of pieces, pieces, halves or quarters of one (4096 rows x 4000 with 64 alternatives 23 us; by lanes, which leave some 4.7 x 64 elements to the
+    // bound and one time in fifty more than the list takes, 230).
+    const bool many = NT > 64 || a.top > 32;
+    unsigned reach = 0, mine[4];
+    if (NT == 64) {
+      mine[0] = ordered(group[0]);
+      if (many && sp.full <= 128) {
+        Piece<T> p[WALK];
+        load(p, 0);
+        float q[2][4];
 #pragma unroll
-    for (int i = 0; i < BARS / 64; ++i) mine[i] = ordered(group[i]);
+        for (int u = 0; u < 2; ++u) {
+          float f[V];
+          p[u].get(f);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) q[u][i] = max_of(f[i * V / 4], f[i * V / 4 + V / 4 - 1]);
+        }
+        const bool two = sp.full > 64;
+        mine[0] = ordered(max3(xe, q[0][0], two ? q[0][1] : q[0][0]));
+        mine[1] = ordered(two ? max_of(q[0][2], q[0][3]) : q[0][1]);
+        mine[2] = ordered(two ? max_of(q[1][0], q[1][1]) : q[0][2]);
+        mine[3] = ordered(two ? max_of(q[1][2], q[1][3]) : q[0][3]);
+      } else if (many) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int step = sp.full <= 256 ? 1 : 2;
+          float f = i ? -INFINITY : xe;
+          if (i * step < groups * KEPT) f = max3(f, group_max[i * step * NT + t], group_max[(i * step + step - 1) * NT + t]);
+          mine[i] = ordered(f);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < BARS / 64; ++i) mine[i] = ordered(group[i]);
+    }
 #pragma unroll
     for (int b = 31; b >= (sizeof(T) == 2 ? 16 : 0); --b) {
       const unsigned next = reach | 1u << b;
-      int n = 0;
+      int n = __builtin_popcountll(__ballot(mine[0] >= next));
+      if (many)
 #pragma unroll
-      for (int i = 0; i < BARS / 64; ++i) n += __builtin_popcountll(__ballot(mine[i] >= next));
+        for (int i = 1; i < 4; ++i) n += __builtin_popcountll(__ballot(mine[i] >= next));
       if (n >= a.top) reach = next;
     }
     bar = reach <= 0x007fffffu ? -INFINITY : disordered(reach);
@@ -703,7 +745,7 @@ hipError_t values_launch(const LogprobArgs& a, int parts, void* scratch, hipStre
     constexpr int NT = decltype(nt)::value;
     const int groups = (pieces + NT * WALK - 1) / (NT * WALK);
     return by_size(more_than<T>(a, 256), [&](auto o) {
-      hipLaunchKernelGGL((logprob_kernel<T, NT, TOP, H, o()>), dim3((unsigned)((int64_t)a.rows * used)), dim3(NT), TOP ? groups * NT * sizeof(float) : 0, s, a, used, cols, rec,
+      hipLaunchKernelGGL((logprob_kernel<T, NT, TOP, H, o()>), dim3((unsigned)((int64_t)a.rows * used)), dim3(NT), TOP ? groups * (NT == 64 ? WALK : 1) * NT * sizeof(float) : 0, s, a, used, cols, rec,
                          keys);
       return hipGetLastError();
     });

@@ -116,7 +116,7 @@ def test_rows_at_the_edge(kernel_set, dtype, vocab, scale):
 
 @pytest.mark.parametrize("kernel_set", SETS)
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
-@pytest.mark.parametrize("vocab,top", [(5000, 64), (40000, 20), (40000, 64)])
+@pytest.mark.parametrize("vocab,top", [(3300, 64), (5000, 64), (40000, 20), (40000, 64)])
 @pytest.mark.parametrize("how", ["equal", "rising", "falling", "two values", "few left", "one run"])
 def test_alternatives_of_odd_rows(kernel_set, dtype, vocab, top, how):
     """Ties everywhere, orders that put the largest side by side, and rows with fewer tokens left than alternatives."""
@@ -128,6 +128,22 @@ def test_alternatives_of_odd_rows(kernel_set, dtype, vocab, top, how):
          "one run": np.where((j > 3000) & (j < 3200), 5 + rng.normal(0, 1, vocab), rng.normal(0, 1, vocab))}[how]
     x = rnd(np.stack((x, x)), dtype)
     pr = Logprob(dtype, x, [1, vocab - 1], 1.0, top)
+    assert pr.fwd(kernel_set) == 0
+    sync()
+    pr.check_values()
+
+
+@pytest.mark.parametrize("kernel_set", SETS)
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("vocab", [65, 130, 257, 300, 513, 520, 600, 1000, 1030, 1500, 2100, 4090])
+@pytest.mark.parametrize("top", [16, 32, 33, 64])
+@pytest.mark.parametrize("shift", [0, 3])
+def test_alternatives_of_short_rows(kernel_set, dtype, vocab, top, shift):
+    """As many as a good part of the row's columns, of rows that one wavefront takes, coarse values and so ties among them."""
+    x, target, _ = logits(12, vocab, dtype, vocab + top, banned=0.2)
+    x[6:] = np.round(x[6:])
+    x[11] = np.where(np.arange(vocab) % 64 < 40, -np.inf, x[11])
+    pr = Logprob(dtype, x, np.full(12, -1), 1.0, top, pads=(1, 0), shifts=(shift, 0))
     assert pr.fwd(kernel_set) == 0
     sync()
     pr.check_values()
