@@ -309,6 +309,7 @@ __global__ __launch_bounds__(NT, 8) void logprob_kernel(LogprobArgs a, int parts
   auto collect = [&](auto wanted) {
     for (int g = 0; g < groups * KEPT; ++g) {
       if (!wanted(group_max[g * NT + t])) continue;
+      if (*(volatile int*)&ncand > CAND) break;        // it will not be used
       Piece<T> p[WALK / KEPT];
 #pragma unroll
       for (int u = 0; u < WALK / KEPT; ++u) {
