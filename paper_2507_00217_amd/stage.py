@@ -359,10 +359,15 @@ class Stage:
         """sumsq (fp64, one element, on the device) = or += the sum of the squares of this stage's gradients: what the stages of a pipeline add up for
         their common norm."""
         g = self.grads_tensor()
+        self._operand(sumsq, self.torch.float64, 1, "grad_sumsq: sumsq")
         scratch = self._update_scratch()
         with self.torch.cuda.device(self.device):
             self._chk(lib().stage_kernel_grad_sumsq(DTYPE["fp32"], 1, (C.c_int64 * 1)(g.numel()), (C.c_void_p * 1)(g.data_ptr()), int(add), sumsq.data_ptr(),
                                                     scratch.data_ptr(), scratch.numel(), self.stream.cuda_stream), "stage_kernel_grad_sumsq")
+
+    def _operand(self, t, dtype, n, what):
+        if t.dtype != dtype or t.device != self._grads.device or t.numel() < n or not t.is_contiguous():
+            raise StageError(E_INVAL, f"{what}: {t.numel()} of {t.dtype} on {t.device}, wanted {n} of {dtype} on {self._grads.device}, contiguous")
 
     def _update_scratch(self):
         if getattr(self, "_sumsq_scratch", None) is None:
@@ -374,6 +379,9 @@ class Stage:
         """Scales the gradients to a common norm of at most max_norm; norm (fp32, one element) receives what it was."""
         g = self.grads_tensor()
         p = (C.c_void_p * 1)(g.data_ptr())
+        self._operand(sumsq, self.torch.float64, 1, "clip_grads: sumsq")
+        if norm is not None:
+            self._operand(norm, self.torch.float32, 1, "clip_grads: norm")
         with self.torch.cuda.device(self.device):
             self._chk(lib().stage_kernel_grad_clip(DTYPE["fp32"], 1, (C.c_int64 * 1)(g.numel()), p, p, sumsq.data_ptr(), max_norm,
                                                    norm.data_ptr() if norm is not None else None, self.stream.cuda_stream), "stage_kernel_grad_clip")
@@ -393,6 +401,10 @@ class Stage:
         stay as they are themselves), and where it is not finite the step is left out."""
         g, w, es = self.grads_tensor(), self._weights, self._weights.view(self.tdtype).element_size()
         tensors = self.tensors()
+        for k in state:
+            self._operand(state[k], self.torch.float32, g.numel(), f"adamw: {k}")
+        if sumsq is not None:
+            self._operand(sumsq, self.torch.float64, 1, "adamw: sumsq")
         for decays in (True, False):
             group = [t for t in tensors if (t[0][0] == "w") == decays]
             n = len(group)

@@ -120,6 +120,19 @@ def test_an_iteration_of_the_last_stage(cfg, vocab):
     sync()
     assert abs(float(got) - norm) <= 2 * E * norm
     assert np.abs(to_np(stage.grads_tensor()) - factor * to_np(kept)).max() <= 4 * E * factor * np.abs(to_np(kept)).max()
+    # operands of another type, size or place are refused before anything is launched
+    n = kept.numel()
+    kept, weights = stage.grads_tensor().clone(), stage._weights.clone()
+    short = {k: state[k][:n - 1] for k in state}
+    for call in (lambda: stage.grad_sumsq(total.float()), lambda: stage.grad_sumsq(total.cpu()), lambda: stage.grad_sumsq(total[:0]),
+                 lambda: stage.clip_grads(total.float(), most), lambda: stage.clip_grads(total, most, got.double()), lambda: stage.clip_grads(total, 0.0),
+                 lambda: stage.adamw(short, step=1, **hyper), lambda: stage.adamw({k: state[k].double() for k in state}, step=1, **hyper),
+                 lambda: stage.adamw(state, step=1, sumsq=total.float(), max_norm=most, **hyper), lambda: stage.adamw(state, step=0, **hyper),
+                 lambda: stage.adamw({k: state[k].new_zeros(2 * n)[::2] for k in state}, step=1, **hyper)):
+        with pytest.raises(S.StageError):
+            call()
+    sync()
+    assert torch.equal(kept, stage.grads_tensor()) and torch.equal(weights, stage._weights)
     stage.zero_grads()
     stage.grad_sumsq(total)
     sync()
