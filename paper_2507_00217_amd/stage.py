@@ -347,13 +347,14 @@ class Stage:
     # -- between iterations: the gradients' norm, the clip, the update ------------------------
     def tensors(self) -> List[Tuple[str, int, int]]:
         """(name, first element, elements) of every parameter tensor in the flat weight and gradient buffers."""
-        out = []
-        for li in range(self.cfg["n_layers"]):
-            for name in PARAM_IDS:
-                off, r, c = stage_param_layout(self.cfg, li, name)
-                if r * c:
-                    out.append((name, off, r * c))
-        return out
+        if getattr(self, "_tensors", None) is None:              # 13 us a tensor: 0.8 ms for 8 layers
+            self._tensors = []
+            for li in range(self.cfg["n_layers"]):
+                for name in PARAM_IDS:
+                    off, r, c = stage_param_layout(self.cfg, li, name)
+                    if r * c:
+                        self._tensors.append((name, off, r * c))
+        return list(self._tensors)
 
     def grad_sumsq(self, sumsq, add: bool = False):
         """sumsq (fp64, one element, on the device) = or += the sum of the squares of this stage's gradients: what the stages of a pipeline add up for
