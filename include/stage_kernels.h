@@ -168,8 +168,8 @@ size_t stage_kernel_score_attention_bwd_scratch_bytes(const stage_score_attentio
 /* What rows of logits say of their tokens, and the gradient of it: where the output head's product ends and the last stage's dY begins.
  * With m the largest logit x_j of a row and S = sum over j of exp(scale * (x_j - m)):
  *   logp_j = scale * (x_j - m) - ln S,   p_j = exp(logp_j),   lse = scale * m + ln S,   H = -sum of p_j logp_j.
- * A logit of -inf is a token that cannot be: p_j = 0.  A row of nothing else has log probabilities of -inf, H = 0 and a gradient of zeros; one with a NaN
- * or +inf has NaN for its log probabilities, ln S, H and gradient, and -1 for its alternatives. */
+ * A logit of -inf is a token that cannot be: p_j = 0.  A row of nothing else has log probabilities, m and ln S of -inf, H = 0 and a gradient of zeros; one with
+ * a NaN or +inf has NaN for its log probabilities, ln S, H and gradient (its m says nothing), and -1 for its alternatives. */
 typedef struct {
   int32_t dtype;             /* of the logits and their gradient */
   int32_t rows;              /* >= 1, at most 2^21 */

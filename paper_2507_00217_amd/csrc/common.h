@@ -217,6 +217,9 @@ hipError_t score32_fwd(const ScoreArgs& a, hipStream_t s);
 hipError_t score32_bwd(const ScoreArgs& a, hipStream_t s);
 hipError_t score_bwd_mfma(const ScoreArgs& a, float* part, int width, hipStream_t s);
 
+// Whether a row of logits is nothing but -inf, from its statistics: maxima pass NaN over, so that a row of NaN has -inf for m as well, but ln S is NaN there.
+__device__ __forceinline__ bool empty_row(float m, float ln) { return m == -INFINITY && ln == ln; }
+
 // log probabilities: plain kernels
 hipError_t logprob_ref(DType dt, const LogprobArgs& a, hipStream_t s);
 hipError_t logprob_grad_ref(DType dt, const LogprobArgs& a, hipStream_t s);

@@ -571,7 +571,7 @@ __global__ __launch_bounds__(NT, waves_of(NV)) void logprob_both_kernel(LogprobA
 
     T* dx = (T*)a.dx + row * a.lddx;
     if (H) w.h = entropy;
-    const bool none = w.none || m == -INFINITY, together = (((uintptr_t)dx ^ (uintptr_t)x) & 15) == 0;
+    const bool none = w.none || empty_row(m, ln), together = (((uintptr_t)dx ^ (uintptr_t)x) & 15) == 0;
     const float log2s = ln * LOG2E;
     if (NL > 0) __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0): the pieces in LDS have landed
     const int ecoln = spn.edge(t);
@@ -690,9 +690,9 @@ __global__ __launch_bounds__(NTG) void logprob_grad_kernel(LogprobArgs a, int ch
   T* dx = (T*)a.dx + row * a.lddx;
   const Span<T> sp(x, a.vocab);
   Weights w = weights_of(a, row, H);
-  const float m = a.stats[2 * row], log2s = a.stats[2 * row + 1] * LOG2E, c = a.scale * LOG2E;
+  const float m = a.stats[2 * row], ln = a.stats[2 * row + 1], log2s = ln * LOG2E, c = a.scale * LOG2E;
   if (H) w.h = a.entropy[row];
-  const bool none = w.none || m == -INFINITY, together = (((uintptr_t)dx ^ (uintptr_t)x) & 15) == 0;
+  const bool none = w.none || empty_row(m, ln), together = (((uintptr_t)dx ^ (uintptr_t)x) & 15) == 0;
   const int first = chunk * NTG * GV + t;
   Piece<T> v[GV];
   const int ecol = chunk == chunks - 1 ? sp.edge(t) : -1;

@@ -84,7 +84,7 @@ __global__ __launch_bounds__(NT) void logprob_grad_ref_kernel(LogprobArgs a) {
   const int id = a.target ? a.target[row] : -1;
   const float w = a.dlogp && id >= 0 && id < a.vocab ? a.dlogp[row] : 0.f, dh = a.dentropy ? a.dentropy[row] : 0.f, dl = a.dlse ? a.dlse[row] : 0.f;
   const float m = a.stats[2 * row], ln = a.stats[2 * row + 1], h = a.dentropy ? a.entropy[row] : 0.f;
-  const bool none = (w == 0.f && dh == 0.f && dl == 0.f) || m == -INFINITY;
+  const bool none = (w == 0.f && dh == 0.f && dl == 0.f) || empty_row(m, ln);
   for (int j = threadIdx.x; j < a.vocab; j += NT) {
     float g = 0.f;
     if (!none) {
