@@ -1,4 +1,4 @@
-"""Log probabilities and the logits' gradient on rows and sizes where kernels part: rows of nothing but NaN."""
+"""Log probabilities and the logits' gradient on rows and sizes where kernels part: rows of nothing but NaN, ties below zero."""
 import math
 
 import numpy as np
@@ -71,3 +71,46 @@ def test_a_row_of_nan_in_a_share_of_the_vocabulary():
         assert pr.bwd(kernel_set) == 0
         sync()
         assert bool(pr.dx[0].isnan().all()) and bool((pr.dx[1] == 0).all())
+
+
+def tied(how, vocab, dtype):
+    """One row whose alternatives are decided among equal logits"""
+    import torch
+    from tests.gpu_util import rnd
+    rng, low = np.random.default_rng(3), float(torch.finfo(torch.float32 if dtype == "fp32" else torch.bfloat16).min)
+    left = np.isin(np.arange(vocab), rng.integers(0, vocab, 9))
+    kinds = {"constant": np.full(vocab, -1.0), "small": np.full(vocab, -1e-30), "two values": np.where(rng.random(vocab) < 0.5, -1.0, -2.0), "lowest": np.full(vocab, low),
+             "few left": np.where(left, rng.normal(0, 1, vocab), -1e4), "few left, lowest": np.where(left, rng.normal(0, 1, vocab), low),
+             "few left, negative": np.where(left, rng.normal(-9, 1, vocab), -1e4), "above": np.full(vocab, 1.0), "zero": np.zeros(vocab)}
+    return rnd(kinds[how], dtype)
+
+
+TIES = ["constant", "small", "two values", "lowest", "few left", "few left, lowest", "few left, negative"]
+
+
+@pytest.mark.parametrize("kernel_set", SETS)
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("vocab,top", [(700, 40), (3300, 64), (5000, 64), (40000, 20)])
+@pytest.mark.parametrize("how", TIES)
+def test_ties_below_zero(kernel_set, dtype, vocab, top, how):
+    x = tied(how, vocab, dtype)
+    pr = Logprob(dtype, np.stack((x, x)), [1, vocab - 1], 1.0, top)
+    assert pr.fwd(kernel_set) == 0
+    sync()
+    pr.check_values()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("how", TIES)
+def test_what_ties_take(dtype, how):
+    """The way made for ties finds them in one more pass over a row: twice what rows of zeros take is room for another share of rows that take it (or the walk a second time, which the lowest values make).
+    One by one, `top` passes, was 8 times and more."""
+    import torch
+    from tests.test_gpu_score_odd import once
+    rows, vocab, top = 512, 40000, 40
+    time = {}
+    for kind in ("zero", how):
+        pr = Logprob(dtype, np.broadcast_to(tied(kind, vocab, dtype), (rows, vocab)), None, 1.0, top)
+        stream = torch.cuda.current_stream().cuda_stream
+        time[kind] = once(lambda: pr.fwd(0, stream))
+    assert time[how] <= 2 * time["zero"], time
