@@ -214,8 +214,8 @@ size_t stage_kernel_token_logprob_scratch_bytes(const stage_token_logprob_t* p);
 int stage_kernel_grad_sumsq(int dtype, int n, const int64_t* size, const void* const* grad, int add, double* sumsq, void* scratch,
                             size_t scratch_bytes, void* hip_stream);
 size_t stage_kernel_grad_sumsq_scratch_bytes(void);
-/* out[i] = grad[i] * min(1, max_norm / sqrt(sumsq)), each rounded once; out[i] may be grad[i], otherwise they overlap nothing.  max_norm is finite, > 0.
- * norm (device, or NULL): receives sqrt(sumsq).  Where sumsq is not finite (a gradient is not) the gradients stay as they are. */
+/* out[i] = grad[i] * min(1, max_norm / sqrt(sumsq)), the factor to 24 bits whatever the norm is; out[i] may be grad[i], otherwise they overlap nothing.  max_norm is finite, > 0.
+ * norm (device, or NULL): receives sqrt(sumsq) (inf where fp32 does not hold it).  Where sumsq is not finite (a gradient is not) the gradients stay as they are. */
 int stage_kernel_grad_clip(int dtype, int n, const int64_t* size, const void* const* grad, void* const* out, const double* sumsq, float max_norm,
                            float* norm, void* hip_stream);
 

@@ -110,27 +110,33 @@ __global__ __launch_bounds__(NTT) void sumsq_total_kernel(const double* part, in
   if (i == 0) sumsq[0] = add ? sumsq[0] + s : s;
 }
 
-// the factor that brings a norm down to max_norm; 1 where the norm is not finite
-__device__ __forceinline__ float clip_factor(double sumsq, float max_norm) {
-  const double norm = sqrt(sumsq);
-  return norm > (double)max_norm && norm < INFINITY ? (float)((double)max_norm / norm) : 1.f;
+// The factor that brings a norm down to max_norm; 1 where the norm is not finite.  Norms that are more than 2^100 times max_norm have their factor in two, the first of
+// which fp32 holds in all of its bits: the second is a power of two, and for all others 1, by which nothing changes.
+struct Factor {
+  float f, then;
+  __device__ __forceinline__ float operator()(float g) const { return g * f * then; }
+};
+__device__ __forceinline__ Factor clip_factor(double sumsq, float max_norm) {
+  const double norm = sqrt(sumsq), r = norm > (double)max_norm && norm < INFINITY ? (double)max_norm / norm : 1.0;
+  const bool low = r < 0x1p-100;
+  return {(float)(low ? r * 0x1p64 : r), low ? 0x1p-64f : 1.f};
 }
 
 constexpr int CLIP_U = 4;
 template <typename T, bool ONCE>
 __global__ __launch_bounds__(NT) void clip_kernel(Lists<2> l, const double* sumsq, float max_norm, float* norm) {
   constexpr int V = vec<T>(), CHUNK = NT * V * CLIP_U;
-  const float f = clip_factor(*sumsq, max_norm);
+  const Factor f = clip_factor(*sumsq, max_norm);
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)sqrt(*sumsq);
   for (int64_t c = blockIdx.x; c < l.chunks; c += gridDim.x) {
     const Chunk k = chunk_of<2, CHUNK>(l, c);
     const T* g = (const T*)l.e[k.t].p[0];
     T* o = (T*)l.e[k.t].p[1];
-    if (f == 1.f && g == o) continue;              // nothing to change
-    auto one = [&](int64_t i) { o[i] = from_f32<T>(f * to_f32(g[i])); };
+    if (f.f == 1.f && g == o) continue;              // nothing to change
+    auto one = [&](int64_t i) { o[i] = from_f32<T>(f(to_f32(g[i]))); };
     auto group = [&](Group<T, ONCE>& q) {
 #pragma unroll
-      for (int e = 0; e < V; ++e) q.u.v[e] = from_f32<T>(f * to_f32(q.u.v[e]));
+      for (int e = 0; e < V; ++e) q.u.v[e] = from_f32<T>(f(to_f32(q.u.v[e])));
     };
     if (k.groups && k.hi - k.body == CHUNK) {
       Group<T, ONCE> q[CLIP_U];
@@ -175,7 +181,7 @@ template <typename TW, typename TG, bool ONCE>
 __global__ __launch_bounds__(NT) void adamw_kernel(Lists<5> l, AdamWArgs a) {
   constexpr bool LP = sizeof(TW) == 2;
   __shared__ float sh[2];
-  float f = 1.f;
+  Factor f = {1.f, 1.f};
   if (a.sumsq) {
     if (!(*a.sumsq < INFINITY)) return;
     f = clip_factor(*a.sumsq, a.max_norm);
@@ -193,7 +199,7 @@ __global__ __launch_bounds__(NT) void adamw_kernel(Lists<5> l, AdamWArgs a) {
     i2 = sh[1];
   }
   auto update = [&](float g, float& w, float& m, float& v) {
-    g *= f;
+    g = f(g);
     m = fmaf(a.beta1, m, a.rest1 * g);
     v = fmaf(a.beta2, v, a.rest2 * g * g);
     w = fmaf(-lr, fmaf(a.decay, w, m * i1 / (sqrtf(v * i2) + a.eps)), w);
