@@ -225,7 +225,7 @@ int stage_kernel_grad_clip(int dtype, int n, const int64_t* size, const void* co
 typedef struct {
   int32_t dtype;             /* of the weights w */
   int32_t grad_dtype;
-  double lr, beta1, beta2, eps, weight_decay;      /* all >= 0 and finite; betas < 1 */
+  double lr, beta1, beta2, eps, weight_decay;      /* betas 0 .. below 1, others 0 .. 1e38; eps 0 or at least 1e-37 (0: moments of zero give 0 / 0, NaN) */
   const double* sumsq;       /* device, or NULL: gradients are taken as they are (and have to be finite) */
   const float* lr_now;       /* device, or NULL: read in the place of lr, so that a captured call can be replayed with another */
   const int32_t* step_now;   /* device, or NULL: read in the place of step */

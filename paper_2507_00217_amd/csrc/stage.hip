@@ -1351,9 +1351,9 @@ int stage_kernel_grad_clip(int dtype, int n, const int64_t* size, const void* co
 int stage_kernel_adamw(const stage_adamw_t* p, int n, const int64_t* size, void* const* w, float* const* master, float* const* m, float* const* v,
                        const void* const* grad, void* hip_stream) {
   const auto list = [&](const void* const* q, int es) { return tensor_list(n, size, q, es); };
-  const auto hyper = [](double x) { return x >= 0.0 && std::isfinite(x); };
+  const auto hyper = [](double x) { return x >= 0.0 && x <= 1e38; };        // in fp32 too
   if (!p || !dtype_ok(p->dtype) || !dtype_ok(p->grad_dtype) || !hyper(p->lr) || !hyper(p->beta1) || !hyper(p->beta2) || p->beta1 >= 1.0 || p->beta2 >= 1.0 ||
-      !hyper(p->eps) || !hyper(p->weight_decay) || ((uintptr_t)p->sumsq & 7) || ((uintptr_t)p->lr_now & 3) || ((uintptr_t)p->step_now & 3) || p->step < 1 ||
+      !hyper(p->eps) || (p->eps > 0.0 && p->eps < 1e-37) || !hyper(p->weight_decay) || ((uintptr_t)p->sumsq & 7) || ((uintptr_t)p->lr_now & 3) || ((uintptr_t)p->step_now & 3) || p->step < 1 ||
       (p->sumsq && (!(p->max_norm > 0.f) || !std::isfinite(p->max_norm))) || !tensor_sizes(n, size) ||
       !list((const void* const*)w, bytes_of(p->dtype)) || !list((const void* const*)m, 4) || !list((const void* const*)v, 4) || !list(grad, bytes_of(p->grad_dtype)) ||
       (p->dtype == STAGE_DTYPE_FP32 ? master != nullptr : !list((const void* const*)master, 4)))
