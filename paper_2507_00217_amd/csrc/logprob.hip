@@ -576,7 +576,10 @@ __global__ __launch_bounds__(NT, waves_of(NV)) void logprob_both_kernel(LogprobA
     if (H) w.h = entropy;
     const bool none = w.none || empty_row(m, ln), together = (((uintptr_t)dx ^ (uintptr_t)x) & 15) == 0;
     const float log2s = ln * LOG2E;
-    if (NL > 0) __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0): the pieces in LDS have landed
+    if (NL > 0) {
+      __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0): the pieces in LDS have landed
+      asm volatile("" ::: "memory");               // and none is read before: the wait by itself names no memory
+    }
     const int ecoln = spn.edge(t);
     const float xen = ecoln >= 0 ? to_f32(xn[ecoln]) : -INFINITY;
     const Weights wn = weights_of(a, more ? after : row, H);
