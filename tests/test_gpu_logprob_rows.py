@@ -114,3 +114,107 @@ def test_what_ties_take(dtype, how):
         stream = torch.cuda.current_stream().cuda_stream
         time[kind] = once(lambda: pr.fwd(0, stream))
     assert time[how] <= 2 * time["zero"], time
+
+
+# ---------------------------------------------------------------------------
+# values and gradient in one call, in every form of the kernel that holds rows in registers
+# ---------------------------------------------------------------------------
+# threads of a workgroup, pieces of 16 bytes to each, rows, columns in bf16 (half as many in fp32).  Rows are more than the workgroups that are launched, but where the form is for few rows.
+FORMS = {"64x1": (64, 1, 8500, 333), "256x1": (256, 1, 300, 1501), "64x4": (64, 4, 8300, 1203), "64x8": (64, 8, 6200, 3001), "256x4": (256, 4, 2100, 6001), "256x8": (256, 8, 1600, 9001),
+         "512x8": (512, 8, 800, 17001), "512x16": (512, 16, 700, 40001), "1024x16": (1024, 16, 300, 70001),
+         # the widest rows, and more logits and gradient than the caches are asked to keep
+         "1024x16 full": (1024, 16, 515, 131072), "512x8 large": (512, 8, 2200, 32003)}
+
+
+class OneCall:
+    """Logits made on the GPU, an offset and a spread of their own to each row; some rows are odd.  ld: columns from one row to the next; dx_shift: where the gradient's buffer starts."""
+
+    def __init__(self, dtype, rows, vocab, pad=0, shift=0, dx_pad=0, dx_shift=0, in_place=False, entropy=True, odd=True, scale=0.8, seed=0):
+        import ctypes as C
+
+        import torch
+        from paper_2507_00217_amd import stage as S
+        from tests.score_util import DT
+        self.C, self.S, td = C, S, torch.float32 if dtype == "fp32" else torch.bfloat16
+        g = torch.Generator(device="cuda:0").manual_seed(seed)
+        normal = lambda *s: torch.randn(*s, generator=g, device="cuda:0")
+        self.buf = torch.full((rows, shift + vocab + pad), math.nan, dtype=td, device="cuda:0")
+        self.x = self.buf[:, shift:shift + vocab]
+        std = torch.rand(rows, 1, generator=g, device="cuda:0") * 4.0 + 0.5
+        self.x.copy_(normal(rows, vocab).mul_(std).add_(normal(rows, 1) * 4.0))
+        self.target = torch.randint(-1, vocab, (rows,), generator=g, device="cuda:0", dtype=torch.int32)
+        self.w, self.dh, self.dl = normal(rows), normal(rows) if entropy else None, normal(rows)
+        if odd:                                        # early rows, and late ones, which a workgroup comes to behind others
+            last = vocab - 1
+            for base in (3, rows - 13):
+                self.x[base] = math.nan
+                self.x[base + 1] = -math.inf
+                self.x[base + 2, last] = math.inf
+                self.x[base + 3, vocab // 2] = math.nan
+                self.x[base + 4, 1:] = -math.inf
+                self.x[base + 4, 0] = 2.0
+                self.x[base + 5, ::2] = -math.inf
+                self.x[base + 6] = -1.5
+                self.x[base + 7, vocab // 3] = 200.0         # certain
+                self.target[base:base + 8] = torch.tensor([0, last, 1, 2, 0, 1, last, vocab // 3], dtype=torch.int32)
+                for v in (self.w, self.dh, self.dl):
+                    if v is not None:
+                        v[base + 8] = v[base + 9] = 0.0      # zeros, whatever the logits are
+                self.x[base + 9] = math.nan
+        self.kept = self.x.clone()
+        if in_place:
+            self.dbuf, self.dx = self.buf, self.x
+        else:
+            self.dbuf = torch.full((rows, dx_shift + vocab + dx_pad), math.nan, dtype=td, device="cuda:0")
+            self.dx = self.dbuf[:, dx_shift:dx_shift + vocab]
+            self.dx.fill_(7.0)
+        self.outside = torch.ones(self.dbuf.shape[1], dtype=torch.bool, device="cuda:0")
+        self.outside[self.dx.storage_offset():self.dx.storage_offset() + vocab] = False
+        self.scale, self.rows, self.vocab = scale, rows, vocab
+        self.p = S.TokenLogprob(dtype=DT[dtype], rows=rows, vocab=vocab, top=0, scale=scale, target=self.target.data_ptr())
+        self.out = dict(logp=torch.full((rows,), -9.0, device="cuda:0"), stats=torch.full((rows, 2), -9.0, device="cuda:0"))
+        if entropy:
+            self.out["entropy"] = torch.full((rows,), -9.0, device="cuda:0")
+        self.scratch = torch.empty(S.lib().stage_kernel_token_logprob_scratch_bytes(C.byref(self.p)) + 16, dtype=torch.uint8, device="cuda:0")
+
+    def grad(self, stream):
+        ptr = lambda t: None if t is None else t.data_ptr()
+        o = self.out
+        return self.S.lib().stage_kernel_token_logprob_grad(self.C.byref(self.p), ptr(self.x), self.x.stride(0), ptr(self.w), ptr(self.dh), ptr(self.dl), ptr(self.dx), self.dx.stride(0), ptr(o["logp"]),
+                                                            ptr(o["stats"]), ptr(o.get("entropy")), None, None, ptr(self.scratch), self.scratch.numel(), 0, stream)
+
+    def check(self, chain):
+        from tests.step_exact import Rows
+        rows, block = self.rows, max(1, (1 << 25) // self.vocab)
+        for i in range(0, rows, block):
+            at = slice(i, min(rows, i + block))
+            ref = Rows(self.kept[at], self.scale, self.target[at], chain)
+            ref.check_values(**{k: v[at] for k, v in self.out.items()})
+            ref.check_grad(self.dx[at], *(None if v is None else v[at] for v in (self.w, self.dh, self.dl)))
+        assert bool(self.dbuf[:, self.outside].isnan().all())
+
+
+LAYOUTS = {"dense": {}, "odd, apart": dict(pad=3, shift=1, dx_pad=2, dx_shift=2), "odd, alike": dict(pad=2, shift=3, dx_pad=2, dx_shift=3), "in place": dict(pad=1, shift=1, in_place=True)}
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("entropy", [False, True])
+@pytest.mark.parametrize("layout", LAYOUTS)
+def test_one_call_in_every_form(form, dtype, entropy, layout):
+    """Every form holds the row that it is made for, goes on to next rows whose first pieces lie elsewhere, and stores the gradient in whole pieces, element by element and over the logits; rows that
+    are not finite, that have no token and that have no weights are among the first and the last ones.  Additions behind one another: a thread's elements and two edges, 12 of lanes and wavefronts."""
+    import re
+
+    import torch
+    from tests.gpu_util import launches
+    threads, pieces, rows, vocab = FORMS[form]
+    if dtype == "fp32":
+        vocab = (vocab + 1) // 2
+    q = OneCall(dtype, rows, vocab, entropy=entropy, seed=len(form) + vocab, **LAYOUTS[layout])
+    ((name, groups, _),) = launches(q.grad)
+    assert re.search(rf"logprob_both_kernelI(DF16b|f)Li{threads}ELi{pieces}ELi\d+ELb{int(entropy)}ELb{int('large' in form or 'full' in form)}E", name), name
+    assert groups < rows or pieces == 1 and rows <= 512, (groups, rows)
+    assert q.grad(torch.cuda.current_stream().cuda_stream) == 0
+    sync()
+    q.check(pieces * (4 if dtype == "fp32" else 8) + 14)
