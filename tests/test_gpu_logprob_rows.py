@@ -1,4 +1,5 @@
-"""Log probabilities and the logits' gradient on rows and sizes where kernels part: rows of nothing but NaN, ties below zero."""
+"""Log probabilities and the logits' gradient on rows and sizes where kernels part: rows of nothing but NaN, ties below zero; and every form of the kernels
+at sizes that come to it by themselves."""
 import math
 
 import numpy as np
@@ -129,7 +130,7 @@ FORMS = {"64x1": (64, 1, 8500, 333), "256x1": (256, 1, 300, 1501), "64x4": (64, 
 class OneCall:
     """Logits made on the GPU, an offset and a spread of their own to each row; some rows are odd.  ld: columns from one row to the next; dx_shift: where the gradient's buffer starts."""
 
-    def __init__(self, dtype, rows, vocab, pad=0, shift=0, dx_pad=0, dx_shift=0, in_place=False, entropy=True, odd=True, scale=0.8, seed=0):
+    def __init__(self, dtype, rows, vocab, pad=0, shift=0, dx_pad=0, dx_shift=0, in_place=False, entropy=True, odd=True, scale=0.8, seed=0, top=0):
         import ctypes as C
 
         import torch
@@ -171,27 +172,36 @@ class OneCall:
         self.outside = torch.ones(self.dbuf.shape[1], dtype=torch.bool, device="cuda:0")
         self.outside[self.dx.storage_offset():self.dx.storage_offset() + vocab] = False
         self.scale, self.rows, self.vocab = scale, rows, vocab
-        self.p = S.TokenLogprob(dtype=DT[dtype], rows=rows, vocab=vocab, top=0, scale=scale, target=self.target.data_ptr())
+        self.p = S.TokenLogprob(dtype=DT[dtype], rows=rows, vocab=vocab, top=top, scale=scale, target=self.target.data_ptr())
         self.out = dict(logp=torch.full((rows,), -9.0, device="cuda:0"), stats=torch.full((rows, 2), -9.0, device="cuda:0"))
         if entropy:
             self.out["entropy"] = torch.full((rows,), -9.0, device="cuda:0")
+        if top:
+            self.out.update(top_id=torch.full((rows, top), -7, dtype=torch.int32, device="cuda:0"), top_logp=torch.full((rows, top), -9.0, device="cuda:0"))
         self.scratch = torch.empty(S.lib().stage_kernel_token_logprob_scratch_bytes(C.byref(self.p)) + 16, dtype=torch.uint8, device="cuda:0")
 
-    def grad(self, stream):
+    def values(self):
         ptr = lambda t: None if t is None else t.data_ptr()
-        o = self.out
-        return self.S.lib().stage_kernel_token_logprob_grad(self.C.byref(self.p), ptr(self.x), self.x.stride(0), ptr(self.w), ptr(self.dh), ptr(self.dl), ptr(self.dx), self.dx.stride(0), ptr(o["logp"]),
-                                                            ptr(o["stats"]), ptr(o.get("entropy")), None, None, ptr(self.scratch), self.scratch.numel(), 0, stream)
+        return [ptr(self.out.get(k)) for k in ("logp", "stats", "entropy", "top_id", "top_logp")] + [ptr(self.scratch), self.scratch.numel()]
 
-    def check(self, chain):
+    def fwd(self, stream, kernel_set=0):
+        return self.S.lib().stage_kernel_token_logprob_fwd(self.C.byref(self.p), self.x.data_ptr(), self.x.stride(0), *self.values(), kernel_set, stream)
+
+    def grad(self, stream, kernel_set=0):
+        return self.S.lib().stage_kernel_token_logprob_grad(self.C.byref(self.p), self.x.data_ptr(), self.x.stride(0), *(None if v is None else v.data_ptr() for v in (self.w, self.dh, self.dl)),
+                                                            self.dx.data_ptr(), self.dx.stride(0), *self.values(), kernel_set, stream)
+
+    def check(self, chain, grad=True):
         from tests.step_exact import Rows
         rows, block = self.rows, max(1, (1 << 25) // self.vocab)
         for i in range(0, rows, block):
             at = slice(i, min(rows, i + block))
             ref = Rows(self.kept[at], self.scale, self.target[at], chain)
-            ref.check_values(**{k: v[at] for k, v in self.out.items()})
-            ref.check_grad(self.dx[at], *(None if v is None else v[at] for v in (self.w, self.dh, self.dl)))
-        assert bool(self.dbuf[:, self.outside].isnan().all())
+            ref.check_values(**{k: self.out[k][at] for k in ("logp", "stats", "entropy") if k in self.out})
+            if grad:
+                ref.check_grad(self.dx[at], *(None if v is None else v[at] for v in (self.w, self.dh, self.dl)))
+        if grad:
+            assert bool(self.dbuf[:, self.outside].isnan().all())
 
 
 LAYOUTS = {"dense": {}, "odd, apart": dict(pad=3, shift=1, dx_pad=2, dx_shift=2), "odd, alike": dict(pad=2, shift=3, dx_pad=2, dx_shift=3), "in place": dict(pad=1, shift=1, in_place=True)}
@@ -218,3 +228,91 @@ def test_one_call_in_every_form(form, dtype, entropy, layout):
     assert q.grad(torch.cuda.current_stream().cuda_stream) == 0
     sync()
     q.check(pieces * (4 if dtype == "fp32" else 8) + 14)
+
+
+@pytest.mark.parametrize("form", ["64x8", "256x8", "512x8", "512x16", "1024x16"])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_two_calls_at_once_and_again(form, dtype):
+    """The forms that bring the next row to LDS: two problems on two streams, over the logits too, and replayed from a graph, always the same bits."""
+    import torch
+    _, _, rows, vocab = FORMS[form]
+    both = [OneCall(dtype, rows, vocab, in_place=i == 1, pad=1, shift=1, entropy=i == 0, seed=i) for i in (0, 1)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    want = None
+    bits = lambda q: [v.contiguous().view(torch.uint8).clone() for v in (q.dx, *q.out.values())]
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        for q in both:
+            assert q.grad(torch.cuda.current_stream().cuda_stream) == 0
+    for turn in range(6):
+        for q in both:
+            q.x.copy_(q.kept)
+            for v in q.out.values():
+                v.fill_(-5.0)
+        sync()
+        if turn % 2 == 0:
+            for q, s in zip(both, streams):
+                assert q.grad(s.cuda_stream) == 0
+        else:
+            graph.replay()
+        sync()
+        got = [bits(q) for q in both]
+        want = want or got
+        for a, b in zip(want, got):
+            assert all(torch.equal(u, v) for u, v in zip(a, b)), turn
+
+
+# rows beyond what registers hold, and few wide ones; additions behind one another: a thread's elements, six roundings for each group of two pieces that the walk comes to, 28 of edges, lanes,
+# wavefronts and parts
+WIDE = [("bf16", 300, 140001, 35 * 8 + 18 * 6 + 28), ("fp32", 300, 70001, 35 * 4 + 18 * 6 + 28), ("bf16", 40, 200001, 3 * 8 + 2 * 6 + 28), ("fp32", 40, 131073, 3 * 8 + 2 * 6 + 28),
+        ("bf16", 20, 1 << 22, 32 * 8 + 16 * 6 + 28), ("fp32", 20, 1 << 22, 64 * 4 + 32 * 6 + 28)]
+
+
+@pytest.mark.parametrize("kernel_set", [0, 2])
+@pytest.mark.parametrize("dtype,rows,vocab,chain", WIDE)
+@pytest.mark.parametrize("layout", ["dense", "odd, apart", "in place"])
+def test_one_call_of_wide_rows(kernel_set, dtype, rows, vocab, chain, layout):
+    """In three launches: the walk (in parts, joined), then the gradient from its statistics."""
+    import torch
+    q = OneCall(dtype, rows, vocab, seed=vocab, **LAYOUTS[layout])
+    assert q.grad(torch.cuda.current_stream().cuda_stream, kernel_set) == 0
+    sync()
+    q.check(chain)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("entropy", [False, True])
+@pytest.mark.parametrize("rows,vocab,threads", [(21000, 6500, 256), (17000, 8500, 256), (65000, 2200, 64), (1100, 131071, 512)])
+@pytest.mark.parametrize("top", [0, 20])
+def test_values_of_more_logits_than_the_caches_keep(dtype, entropy, rows, vocab, threads, top):
+    """The walk's form for more than 256 MB of logits, with alternatives and without; a part of the rows' alternatives against a stable sort."""
+    import re
+
+    import torch
+    from tests.gpu_util import launches
+    if dtype == "fp32":
+        vocab = (vocab + 1) // 2
+    if vocab * (2 if dtype == "fp32" else 1) <= 8192 and top == 0:      # without alternatives one wavefront goes further
+        threads = 64
+    q = OneCall(dtype, rows, vocab, pad=1, shift=1, entropy=entropy, seed=rows + top, top=top, in_place=True)
+    ((name, _, _),) = launches(q.fwd)
+    assert re.search(rf"14logprob_kernelI(DF16b|f)Li{threads}ELb{int(top > 0)}ELb{int(entropy)}ELb1E", name), name
+    assert q.fwd(torch.cuda.current_stream().cuda_stream) == 0
+    sync()
+    each = -(-vocab // (threads * (4 if dtype == "fp32" else 8)))
+    q.check((each + 1) * (4 if dtype == "fp32" else 8) + (each // 2 + 1) * 6 + 28, grad=False)
+    if top:
+        from tests.step_exact import E
+        some = torch.cat((torch.arange(0, 40), torch.arange(40, rows - 40, rows // 40), torch.arange(rows - 40, rows))).to("cuda:0")
+        x, ids, lp = q.x[some].float(), q.out["top_id"][some].long(), q.out["top_logp"][some]
+        bad = (x.isnan() | (x == math.inf)).any(1)
+        assert bool((ids[bad] == -1).all()) and bool(lp[bad].isnan().all()) and int(bad.sum()) >= 6
+        best, where = torch.sort(x[~bad], dim=1, descending=True, stable=True)
+        assert torch.equal(ids[~bad], where[:, :top])
+        # z - ln S from the kernel's own ln S, which is checked above: three roundings of z, one of the difference
+        m, ln = (q.out["stats"][some][~bad][:, i:i + 1].double() for i in (0, 1))
+        z = float(np.float32(q.scale)) * (best[:, :top].double() - torch.where(m == -math.inf, 0.0, m))
+        want = torch.where(z == -math.inf, z, z - ln)
+        got = lp[~bad].double()
+        same = (got == want) | ((got - want).abs() <= 3 * E * z.abs() + E * want.abs())
+        assert bool(same.all()), (got[~same][:4], want[~same][:4])
