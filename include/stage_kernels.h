@@ -190,7 +190,7 @@ int stage_kernel_token_logprob_fwd(const stage_token_logprob_t* p, const void* l
 /* dlogits [rows, vocab] (row stride ldd) from the rows' gradients with respect to logp (ignored where a row has no token), H and lse, each [rows] fp32 or
  * NULL for zeros, not all NULL (dlogp: only with targets; dentropy: only with entropy, which is H from the forward):
  *   dlogits_j = scale * (p_j * (dlse - dlogp - dentropy * (logp_j + H)) + dlogp * [j is the row's token]).
- * A row whose three are all zero gets zeros, whatever its logits are.  dlogits may be logits (with ldd = ld); otherwise they must not overlap.
+ * A row whose three are all zero gets zeros, whatever its logits are; scale times any of them is a number in fp32.  dlogits may be logits (with ldd = ld); otherwise they must not overlap.
  * stats and entropy may be those of a wider vocabulary of which logits are some columns (m the largest of all, S over all), as on each of several GPUs
  * that a vocabulary is spread over; a row whose token lies on another one then has dlse - dlogp for its dlse. */
 int stage_kernel_token_logprob_bwd(const stage_token_logprob_t* p, const void* logits, int64_t ld, const float* stats, const float* entropy,

@@ -5,7 +5,8 @@
 //
 // A list of tensors is cut into chunks of one size, and a launch takes the chunks of as many tensors as travel with its arguments: nothing is copied to the
 // device beforehand, so that a captured launch holds all that it needs.  Clip and step have a workgroup to each chunk, and loads and stores that ask the
-// caches to keep nothing: 202 million fp32 gradients, norm and clip 396 us (2048 workgroups that walk, ordinary accesses: 468), the AdamW step with bf16 weights 1062 us (1283).
+// caches to keep nothing: 202 million fp32 gradients, norm and clip 378 us (ordinary accesses 423, and in 2048 workgroups that walk 468), the AdamW step with bf16 weights 1037 to
+// 1055 us (1283 in workgroups that walk).
 #include "common.h"
 
 #include <type_traits>
@@ -268,7 +269,7 @@ hipError_t over_lists(const TensorList& t, const void* const* const (&arr)[K], c
 }
 
 // Whether a list's accesses ask the caches to keep nothing: from 256 MB on, what the last-level cache holds.  (4.2 million parameters, 59 MB: AdamW 12.9 us with ordinary
-// accesses, 14.0 without keeping; 202 million, 6.1 GB: 1152 against 1103.)
+// accesses, 14.0 without keeping; 202 million, 6.1 GB: 1129 against 1099; norm and clip of 151 million bf16 gradients 308 against 269.)
 bool once(const TensorList& l, int bytes) {
   int64_t n = 0;
   for (int i = 0; i < l.n; ++i) n += l.size[i];

@@ -739,8 +739,9 @@ size_t part_bytes(const LogprobArgs& a, int parts) { return parts > 1 ? (size_t)
 
 using std::integral_constant;
 // Whether accesses ask the caches to keep nothing.  Values: logits of more than the last-level cache's 256 MB, which leave nothing in it for a backward (2048 rows x 128000 with
-// alternatives 125 us against 131; a backward that finds 103 MB of logits there takes 37 us, 46 otherwise).  Values and gradient: both of more than that together (4096 x 32000
-// 109 us against 116).  The gradient by itself: its stores, from the 32 MB on that the L2s hold (1023 x 50333 in two calls 66 us against 73).
+// alternatives 100 us against 109, 4096 x 64000 in two calls 277 against 287; but 1023 x 50333 in two calls, 103 MB that the backward finds there, 63 against 56).  Values and
+// gradient: both of more than that together (4096 x 32000 92 us against 108).  The gradient by itself: its stores, from the 32 MB on that the L2s hold (1023 x 50333 in two
+// calls 56 us against 64, 4000 x 32000 127 against 156; 400 x 50333, 40 MB, 27.2 either way).
 template <typename T> bool more_than(const LogprobArgs& a, int64_t mb) { return (int64_t)a.rows * a.vocab * (int64_t)sizeof(T) > mb << 20; }
 template <typename F> hipError_t by_size(bool large, F f) { return large ? f(std::true_type{}) : f(std::false_type{}); }
 
